@@ -377,6 +377,160 @@ psd_status psd_generate(const psd_params *params, const psd_toy_lm *lm, int32_t 
                         int32_t check_every, int32_t use_graph, int32_t *out_blocks, uint32_t *out_status,
                         hipStream_t stream);
 
+/* ---- the target's pass over a block's new tokens ------------------------------ */
+
+/* Keys and values in pages.  A pool holds `pages` pages of `page_tokens` tokens for
+ * `heads` heads of `head_dim` elements: element d of (layer l, page p, place i, head g)
+ * lies at l * stride_layer + p * stride_page + i * stride_token + g * stride_head + d,
+ * for keys from k and for values from v (any order of pages, places and heads; offsets
+ * are 64-bit).  Pointers and strides are multiples of 16 bytes.  k and v do not
+ * overlap, nor do two elements of a pool. */
+typedef struct {
+    void *k;              /* device */
+    void *v;              /* device */
+    int32_t dtype;        /* psd_dtype of the pools, the new keys and values, queries and outputs */
+    int32_t heads;        /* G, 1..PSD_MAX_HEADS: key/value heads */
+    int32_t head_dim;     /* D, a multiple of 8, 8..PSD_MAX_HEAD_DIM */
+    int32_t page_tokens;  /* P, 1..65536 */
+    int32_t pages;        /* pages of the pool, >= 1 */
+    int32_t layers;       /* psd_kv_keep: layers moved by one call, >= 1.  psd_kv_append and
+                             psd_attention work on layer 0 */
+    int64_t stride_layer; /* elements; read with layers > 1 */
+    int64_t stride_page;
+    int64_t stride_token;
+    int64_t stride_head;
+} psd_cache;
+
+#define PSD_MAX_HEADS 1024    /* query heads H and key/value heads G */
+#define PSD_MAX_HEAD_DIM 256  /* D */
+#define PSD_MAX_KV (1 << 30)  /* cached tokens of a sequence */
+#define PSD_MAX_ROWS (1 << 23) /* T, packed rows of a call */
+
+/* The sequences of one call.  Sequence b has n_b = new_start[b+1] - new_start[b] new
+ * tokens, packed rows [new_start[b], new_start[b+1]) of the call's row buffers, and
+ * kv_len[b] cached tokens, the new ones included: new token i sits at cache position
+ * kv_len[b] - n_b + i, and position c on page table[b][c / P], place c % P.
+ * Lengths live on the device and may change from call to call (also between replays
+ * of a captured graph) below the host's bounds rows, max_new, max_kv, which size the
+ * launches: rows past `rows`, new tokens past max_new and positions past max_kv or past
+ * the table's width are not computed.  A new token whose position is negative or whose
+ * page lies outside [0, pages) is not appended; cached tokens on such a page are seen by
+ * no row.  n_b = 0 and kv_len[b] = 0 are lengths like others. */
+typedef struct {
+    int32_t batch;         /* B, 1..PSD_MAX_BATCH */
+    int32_t rows;          /* T, 1..PSD_MAX_ROWS: packed rows of the call (an upper bound of new_start[B]) */
+    int32_t max_new;       /* >= 1: upper bound of n_b */
+    int32_t max_kv;        /* 1..PSD_MAX_KV: upper bound of kv_len[b] */
+    int32_t table_width;   /* >= 1: entries of a table row */
+    int64_t table_stride;  /* entries from one row of the table to the next */
+    const int32_t *new_start; /* device [B+1], nondecreasing */
+    const int32_t *kv_len;    /* device [B] */
+    const int32_t *table;     /* device [B][table_stride] */
+} psd_seqs;
+
+/* Rows of heads: element d of head h of row t at t * stride_row + h * stride_head + d.
+ * Pointer and strides are multiples of 16 bytes (a view into a joint projection's rows
+ * is as good as a tensor of its own). */
+typedef struct {
+    void *data; /* device */
+    int64_t stride_row;
+    int64_t stride_head;
+} psd_rows;
+
+/* Norms and rotation on the way into the cache. */
+typedef struct {
+    int32_t rotary;            /* R: the first R dimensions of each head turn; even, 0..D (0: none) */
+    int32_t interleaved;       /* 0: pairs (r, r + R/2); 1: pairs (2r, 2r + 1), r < R/2 */
+    int32_t positions_max;     /* rows of cos and sin; >= 1 with rotary > 0 */
+    const float *cos;          /* device [positions_max][R/2] */
+    const float *sin;          /* device [positions_max][R/2] */
+    const int32_t *positions;  /* device [T], nullable: a row's rotation position (draft paths: root + depth);
+                                  NULL: its cache position.  Outside [0, positions_max) the turned
+                                  dimensions of the row come out NaN */
+    const void *q_norm;        /* device [D] (dtype), nullable: weights of the queries' norm */
+    const void *k_norm;        /* device [D] (dtype), nullable: weights of the keys' norm */
+    float eps;                 /* norm: x / sqrt(mean(x^2) + eps) * weight; >= 0, finite */
+} psd_rotation;
+
+/* Append the new tokens' keys and values to the cache (layer 0): each head of a key is
+ * normed (k_norm) and turned, values are copied.  With q the queries take the same norm
+ * (q_norm) and turn and go to q_out.  Arithmetic in float32, one rounding at the end.
+ *   k, v    [T][G][D] (dtype);  q, q_out [T][H][D], both or neither; q_heads = H
+ * q_out may be q itself.  One launch. */
+psd_status psd_kv_append(const psd_cache *cache, const psd_seqs *seqs, const psd_rotation *rotation,
+                         const psd_rows *k, const psd_rows *v, const psd_rows *q, const psd_rows *q_out,
+                         int32_t q_heads, hipStream_t stream);
+
+/* Attention of the new tokens over the cache (which already holds them): with
+ * g = h / (H/G) and s_j = scale * sum_d q[t][h][d] k_j[g][d] over the cached tokens j
+ * that row t sees,
+ *   out[t][h] = sum_j exp(s_j - lse) v_j[g],  lse[t][h] = ln sum_j exp(s_j).
+ * The row of new token i, at position c = kv_len - n_b + i, sees
+ *   mask NULL   positions j <= c, with window W > 0 only c - W < j;
+ *   mask        every position before the new tokens, and new token j where bit j % 32 of
+ *               mask[t][j / 32] is set (0 past mask_words; window must be 0): K draft paths
+ *               behind one root share the cache and one call (target_rows = K).
+ * A row that sees nothing gives zeros and lse -inf.  Positions no row sees are not read,
+ * and a masked or unseen token's key and value change nothing, NaN and infinities
+ * included.  A score of +inf or NaN that a row does see gives that row NaN.
+ *   q, out     [T][H][D] (dtype); out may be q itself
+ *   lse        device [T][H] float32, nullable
+ *   mask       device [T][mask_words] uint32, nullable
+ *   workspace  device, psd_attention_workspace_bytes() for this cache, seqs and H, 256-byte
+ *              aligned; may be NULL when that is 0.  Nothing in it needs clearing, and
+ *              nothing in it outlives the call.
+ * Products of bfloat16 values are summed in float32, and softmax weights are rounded to
+ * bfloat16 for the product with the values; float32 inputs are computed in float32. */
+psd_status psd_attention(const psd_cache *cache, const psd_seqs *seqs, const psd_rows *q, int32_t q_heads, float scale,
+                         int32_t window, const uint32_t *mask, int32_t mask_words, const psd_rows *out, float *lse,
+                         void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of workspace psd_attention needs for these bounds (the pointers inside the
+ * structs are not read).  (size_t)-1 for invalid arguments; 0 is a valid size. */
+size_t psd_attention_workspace_bytes(const psd_cache *cache, const psd_seqs *seqs, int32_t q_heads);
+
+/* Keep an accepted path: in every layer, key and value of new token keep[b][i] move to
+ * new token i's position, i < n_keep[b]; the cache then ends behind them, and the next
+ * block's kv_len grows from kv_out.
+ *   keep     device [B][keep_stride] int32, strictly ascending in each row (other orders give
+ *            undefined values); an index outside [0, n_b) moves nothing
+ *   n_keep   device [B] int32, taken as at most keep_width and n_b; at least 0
+ *   kv_out   device [B] int32, nullable: kv_len - n_b + n_keep; not seqs->kv_len itself
+ * 1 <= keep_width <= keep_stride.  One launch. */
+psd_status psd_kv_keep(const psd_cache *cache, const psd_seqs *seqs, const int32_t *keep, int64_t keep_stride,
+                       int32_t keep_width, const int32_t *n_keep, int32_t *kv_out, hipStream_t stream);
+
+/* Verification of drafted tokens from given random numbers: the unkeyed rejection rule
+ * that the paper's races are compared with.  With p_s = softmax(target row s / T_P) and
+ * q_s = softmax(draft row s / T_Q), draft x_s is accepted while
+ *   u_s q_s(x_s) < p_s(x_s);
+ * at the first refusal n the emitted token is argmin_v e_v / max(p_n(v) - q_n(v), 0), an
+ * exponential race over the residual (over p_n where the residual is zero everywhere);
+ * after all drafts are accepted it is argmin_v e_v / p_n(v).  With u uniform on [0, 1)
+ * and e iid Exp(1) the emitted tokens follow p.  Ties go to the lowest token.  Draws from
+ * both rows hold in float32 with each row's maximum taken out before the exponential.
+ *   params         vocab, dtype, temperatures; num_drafts 1, top_k 0 (key, window, mode and
+ *                  clocks are not used)
+ *   target_logits  device [B][gamma+1][V];  draft_logits device [B][gamma][V]
+ *   draft_tokens   device [B][gamma] int32; one outside [0, V) is refused
+ *   n_drafts       device [B] int32, nullable: drafts of each sequence (taken into
+ *                  [0, gamma]); NULL: gamma
+ *   u              device [B][gamma] float32;  e device [B][V] float32, positive and finite
+ *   out_tokens     device [B][gamma+1] int32: the accepted drafts and the emitted token, -1 past
+ *                  out_len; a target row without a finite logit emits -1
+ *   out_len        device [B] int32: accepted + 1
+ *   target_lse     device [B][gamma+1] float32, nullable;  draft_lse [B][gamma], nullable
+ *   workspace      device, psd_verify_given_workspace_bytes(), 256-byte aligned; needs no
+ *                  clearing; one call at a time
+ * batch * (2 gamma + 1) is at most 2^23.  Two launches. */
+psd_status psd_verify_given(const psd_params *params, int32_t batch, int32_t gamma, const void *target_logits,
+                            const void *draft_logits, const int32_t *draft_tokens, const int32_t *n_drafts,
+                            const float *u, const float *e, int32_t *out_tokens, int32_t *out_len, float *target_lse,
+                            float *draft_lse, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of workspace psd_verify_given needs; 0 for invalid arguments. */
+size_t psd_verify_given_workspace_bytes(const psd_params *params, int32_t batch, int32_t gamma);
+
 /* ---- parity exports: the keyed randomness itself ---------------------------- */
 
 /* Philox4x32-10 blocks: out[i][0..3] = Philox(ctr[i][0..3], key[i][0..1]).

@@ -14,6 +14,7 @@
 #include "../../include/psd.h"
 #include "psd_launch.hpp"
 #include "psd_layout.hpp"
+#include "psd_serve.hpp"
 
 namespace {
 
@@ -365,6 +366,88 @@ psd_status run_race(const psd_params* p, psd::RaceArgs& a, hipStream_t stream) {
     if (e != hipSuccess) return hip_fail(e, "race kernel launch");
     return PSD_OK;
 }
+
+// ---- paged cache, attention, verification from given random numbers
+
+constexpr long kMaxGrid = 1L << 23;  // workgroups of up to 256 threads: work-items stay below 2^32
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+
+// Multiples of 16 bytes, small enough that no byte offset passes 62 bits.
+bool good_stride(int64_t elements, int bytes) {
+    return elements >= 0 && elements < (int64_t)1 << 44 && (elements * bytes) % 16 == 0;
+}
+
+psd_status check_cache(const psd_cache* c, bool pointers) {
+    if (!c) return fail(PSD_E_ARG, "cache is NULL");
+    if (c->dtype != PSD_F32 && c->dtype != PSD_BF16) return fail(PSD_E_ARG, "unknown dtype %d", c->dtype);
+    if (c->heads < 1 || c->heads > PSD_MAX_HEADS) return fail(PSD_E_ARG, "heads %d outside [1, %d]", c->heads, PSD_MAX_HEADS);
+    if (c->head_dim < 8 || c->head_dim > PSD_MAX_HEAD_DIM || c->head_dim % 8)
+        return fail(PSD_E_ARG, "head_dim %d is not a multiple of 8 in [8, %d]", c->head_dim, PSD_MAX_HEAD_DIM);
+    if (c->page_tokens < 1 || c->page_tokens > 65536) return fail(PSD_E_ARG, "page_tokens %d outside [1, 65536]", c->page_tokens);
+    if (c->pages < 1) return fail(PSD_E_ARG, "pages must be at least 1");
+    if (c->layers < 1 || c->layers > 65535) return fail(PSD_E_ARG, "layers %d outside [1, 65535]", c->layers);
+    const int bytes = c->dtype == PSD_BF16 ? 2 : 4;
+    if (!good_stride(c->stride_page, bytes) || !good_stride(c->stride_token, bytes) || !good_stride(c->stride_head, bytes) ||
+        (c->layers > 1 && !good_stride(c->stride_layer, bytes)))
+        return fail(PSD_E_ARG, "cache strides must be multiples of 16 bytes");
+    if (!pointers) return PSD_OK;
+    if (!c->k || !c->v) return fail(PSD_E_ARG, "cache k / v is NULL");
+    if (!aligned16(c->k) || !aligned16(c->v)) return fail(PSD_E_ARG, "cache k / v must be 16-byte aligned");
+    return PSD_OK;
+}
+
+psd_status check_seqs(const psd_seqs* s, bool pointers) {
+    if (!s) return fail(PSD_E_ARG, "seqs is NULL");
+    if (s->batch < 1 || s->batch > PSD_MAX_BATCH) return fail(PSD_E_ARG, "batch %d outside [1, %d]", s->batch, PSD_MAX_BATCH);
+    if (s->rows < 1 || s->rows > PSD_MAX_ROWS) return fail(PSD_E_ARG, "rows %d outside [1, %d]", s->rows, PSD_MAX_ROWS);
+    if (s->max_new < 1) return fail(PSD_E_ARG, "max_new must be at least 1");
+    if (s->max_kv < 1 || s->max_kv > PSD_MAX_KV) return fail(PSD_E_ARG, "max_kv %d outside [1, %d]", s->max_kv, PSD_MAX_KV);
+    if (s->table_width < 1) return fail(PSD_E_ARG, "table_width must be at least 1");
+    if (s->table_stride < s->table_width) return fail(PSD_E_ARG, "table_stride is below table_width");
+    if (pointers && (!s->new_start || !s->kv_len || !s->table)) return fail(PSD_E_ARG, "new_start / kv_len / table is NULL");
+    return PSD_OK;
+}
+
+psd_status check_rows(const psd_rows* r, int bytes, const char* what) {
+    if (!r || !r->data) return fail(PSD_E_ARG, "%s is NULL", what);
+    if (!aligned16(r->data) || !good_stride(r->stride_row, bytes) || !good_stride(r->stride_head, bytes))
+        return fail(PSD_E_ARG, "%s: pointer and strides must be multiples of 16 bytes", what);
+    return PSD_OK;
+}
+
+psd_status check_heads(const psd_cache* c, int q_heads) {
+    if (q_heads < 1 || q_heads > PSD_MAX_HEADS || q_heads % c->heads)
+        return fail(PSD_E_ARG, "q_heads %d is not a multiple of the cache's %d heads in [1, %d]", q_heads, c->heads, PSD_MAX_HEADS);
+    return PSD_OK;
+}
+
+psd::CacheArgs cache_args(const psd_cache* c, const psd_seqs* s) {
+    psd::CacheArgs a;
+    a.k = c->k;
+    a.v = c->v;
+    a.stride_layer = c->layers > 1 ? c->stride_layer : 0;
+    a.stride_page = c->stride_page;
+    a.stride_token = c->stride_token;
+    a.stride_head = c->stride_head;
+    a.G = c->heads;
+    a.D = c->head_dim;
+    a.P = c->page_tokens;
+    a.pages = c->pages;
+    a.layers = c->layers;
+    a.B = s->batch;
+    a.rows = s->rows;
+    a.max_new = s->max_new;
+    a.max_kv = s->max_kv;
+    a.table_width = s->table_width;
+    a.table_stride = s->table_stride;
+    a.new_start = s->new_start;
+    a.kv_len = s->kv_len;
+    a.table = s->table;
+    return a;
+}
+
+psd::RowsArgs rows_args(const psd_rows* r) { return psd::RowsArgs{r->data, r->stride_row, r->stride_head}; }
 
 }  // namespace
 
@@ -1049,6 +1132,163 @@ psd_status psd_generate(const psd_params* params, const psd_toy_lm* lm, int32_t 
         if ((st = psd_workspace_errors(ws, stream, &bits)) != PSD_OK) return st;
         *out_status = bits;
     }
+    return PSD_OK;
+}
+
+psd_status psd_kv_append(const psd_cache* cache, const psd_seqs* seqs, const psd_rotation* rotation, const psd_rows* k,
+                         const psd_rows* v, const psd_rows* q, const psd_rows* q_out, int32_t q_heads, hipStream_t stream) {
+    psd_status st;
+    if ((st = check_cache(cache, true)) != PSD_OK || (st = check_seqs(seqs, true)) != PSD_OK) return st;
+    const int bytes = cache->dtype == PSD_BF16 ? 2 : 4;
+    if (!rotation) return fail(PSD_E_ARG, "rotation is NULL");
+    if (rotation->rotary < 0 || rotation->rotary > cache->head_dim || rotation->rotary % 2)
+        return fail(PSD_E_ARG, "rotary %d is not even in [0, %d]", rotation->rotary, cache->head_dim);
+    if (rotation->rotary > 0 && (!rotation->cos || !rotation->sin || rotation->positions_max < 1))
+        return fail(PSD_E_ARG, "rotary > 0 needs cos, sin and positions_max >= 1");
+    if (!(rotation->eps >= 0.f) || !isfinite(rotation->eps)) return fail(PSD_E_ARG, "eps must be finite and >= 0");
+    if (!aligned16(rotation->q_norm) || !aligned16(rotation->k_norm))
+        return fail(PSD_E_ARG, "q_norm / k_norm must be 16-byte aligned");
+    if ((st = check_rows(k, bytes, "k")) != PSD_OK || (st = check_rows(v, bytes, "v")) != PSD_OK) return st;
+    if (!q != !q_out) return fail(PSD_E_ARG, "q and q_out come together");
+    if (q) {
+        if ((st = check_rows(q, bytes, "q")) != PSD_OK || (st = check_rows(q_out, bytes, "q_out")) != PSD_OK) return st;
+        if ((st = check_heads(cache, q_heads)) != PSD_OK) return st;
+    }
+    psd::AppendArgs a;
+    memset(&a, 0, sizeof a);
+    a.c = cache_args(cache, seqs);
+    a.k = rows_args(k);
+    a.v = rows_args(v);
+    if (q) {
+        a.q = rows_args(q);
+        a.q_out = rows_args(q_out);
+        a.H = q_heads;
+    }
+    a.R = rotation->rotary;
+    a.interleaved = rotation->interleaved != 0;
+    a.positions_max = rotation->positions_max;
+    a.cos = rotation->cos;
+    a.sin = rotation->sin;
+    a.positions = rotation->positions;
+    a.q_norm = rotation->q_norm;
+    a.k_norm = rotation->k_norm;
+    a.eps = rotation->eps;
+    const hipError_t e = psd::launch_kv_append(a, cache->dtype == PSD_BF16, stream);
+    if (e != hipSuccess) return hip_fail(e, "append kernel launch");
+    return PSD_OK;
+}
+
+size_t psd_attention_workspace_bytes(const psd_cache* cache, const psd_seqs* seqs, int32_t q_heads) {
+    if (check_cache(cache, false) != PSD_OK || check_seqs(seqs, false) != PSD_OK || check_heads(cache, q_heads) != PSD_OK)
+        return (size_t)-1;
+    return psd::attention_workspace(cache_args(cache, seqs), q_heads, cache->dtype == PSD_BF16);
+}
+
+psd_status psd_attention(const psd_cache* cache, const psd_seqs* seqs, const psd_rows* q, int32_t q_heads, float scale,
+                         int32_t window, const uint32_t* mask, int32_t mask_words, const psd_rows* out, float* lse,
+                         void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    psd_status st;
+    if ((st = check_cache(cache, true)) != PSD_OK || (st = check_seqs(seqs, true)) != PSD_OK) return st;
+    const bool bf16 = cache->dtype == PSD_BF16;
+    if ((st = check_heads(cache, q_heads)) != PSD_OK) return st;
+    if ((st = check_rows(q, bf16 ? 2 : 4, "q")) != PSD_OK || (st = check_rows(out, bf16 ? 2 : 4, "out")) != PSD_OK) return st;
+    if (!isfinite(scale)) return fail(PSD_E_ARG, "scale must be finite");
+    if (window < 0) return fail(PSD_E_ARG, "window must be at least 0");
+    if (mask && mask_words < 1) return fail(PSD_E_ARG, "mask_words must be at least 1");
+    if (mask && window > 0) return fail(PSD_E_ARG, "a mask takes no window");
+    psd::AttentionArgs a;
+    memset(&a, 0, sizeof a);
+    a.c = cache_args(cache, seqs);
+    const size_t need = psd::attention_workspace(a.c, q_heads, bf16);
+    if (need > 0) {
+        if (!workspace) return fail(PSD_E_WORKSPACE, "workspace is NULL");
+        if (((uintptr_t)workspace & 255u) != 0) return fail(PSD_E_WORKSPACE, "workspace must be 256-byte aligned");
+        if (workspace_bytes < need) return fail(PSD_E_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
+    }
+    a.q = rows_args(q);
+    a.out = rows_args(out);
+    a.H = q_heads;
+    a.scale = scale;
+    a.window = window;
+    a.mask = mask;
+    a.mask_words = mask ? mask_words : 0;
+    a.lse = lse;
+    a.workspace = workspace;
+    const hipError_t e = psd::launch_attention(a, bf16, stream);
+    if (e != hipSuccess) return hip_fail(e, "attention kernel launch");
+    return PSD_OK;
+}
+
+psd_status psd_kv_keep(const psd_cache* cache, const psd_seqs* seqs, const int32_t* keep, int64_t keep_stride,
+                       int32_t keep_width, const int32_t* n_keep, int32_t* kv_out, hipStream_t stream) {
+    psd_status st;
+    if ((st = check_cache(cache, true)) != PSD_OK || (st = check_seqs(seqs, true)) != PSD_OK) return st;
+    if (!keep || !n_keep) return fail(PSD_E_ARG, "keep / n_keep is NULL");
+    if (keep_width < 1 || keep_stride < keep_width) return fail(PSD_E_ARG, "keep_width must be in [1, keep_stride]");
+    if (kv_out == seqs->kv_len) return fail(PSD_E_ARG, "kv_out must not be kv_len");
+    const long blocks = (2L * cache->heads * cache->head_dim / 4 + 255) / 256 * seqs->batch;
+    if (blocks > kMaxGrid) return fail(PSD_E_ARG, "call too large (%ld workgroups)", blocks);
+    psd::KeepArgs a;
+    a.c = cache_args(cache, seqs);
+    a.keep = keep;
+    a.keep_stride = keep_stride;
+    a.keep_width = keep_width;
+    a.n_keep = n_keep;
+    a.kv_out = kv_out;
+    const hipError_t e = psd::launch_kv_keep(a, cache->dtype == PSD_BF16, stream);
+    if (e != hipSuccess) return hip_fail(e, "keep kernel launch");
+    return PSD_OK;
+}
+
+static psd_status check_given(const psd_params* p, int32_t batch, int32_t gamma) {
+    psd_status st = check_params(p);
+    if (st != PSD_OK) return st;
+    if (p->num_drafts != 1) return fail(PSD_E_ARG, "verification from given numbers takes num_drafts 1, got %d", p->num_drafts);
+    if (p->top_k != 0) return fail(PSD_E_ARG, "verification from given numbers takes top_k 0, got %d", p->top_k);
+    if (batch < 1 || batch > PSD_MAX_BATCH) return fail(PSD_E_ARG, "batch %d outside [1, %d]", batch, PSD_MAX_BATCH);
+    if (gamma < 1 || gamma > PSD_MAX_GAMMA) return fail(PSD_E_ARG, "gamma %d outside [1, %d]", gamma, PSD_MAX_GAMMA);
+    if ((long)batch * (2 * gamma + 1) > kMaxGrid) return fail(PSD_E_ARG, "batch * (2 gamma + 1) is above %ld", kMaxGrid);
+    return PSD_OK;
+}
+
+size_t psd_verify_given_workspace_bytes(const psd_params* params, int32_t batch, int32_t gamma) {
+    if (check_given(params, batch, gamma) != PSD_OK) return 0;
+    return psd::given_workspace(batch, gamma, params->vocab, params->dtype == PSD_BF16);
+}
+
+psd_status psd_verify_given(const psd_params* params, int32_t batch, int32_t gamma, const void* target_logits,
+                            const void* draft_logits, const int32_t* draft_tokens, const int32_t* n_drafts,
+                            const float* u, const float* e, int32_t* out_tokens, int32_t* out_len, float* target_lse,
+                            float* draft_lse, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    psd_status st = check_given(params, batch, gamma);
+    if (st != PSD_OK) return st;
+    if (!target_logits || !draft_logits) return fail(PSD_E_ARG, "target_logits / draft_logits is NULL");
+    if (!draft_tokens || !u || !e) return fail(PSD_E_ARG, "draft_tokens / u / e is NULL");
+    if (!out_tokens || !out_len) return fail(PSD_E_ARG, "out_tokens / out_len is NULL");
+    const bool bf16 = params->dtype == PSD_BF16;
+    if (!workspace) return fail(PSD_E_WORKSPACE, "workspace is NULL");
+    if (((uintptr_t)workspace & 255u) != 0) return fail(PSD_E_WORKSPACE, "workspace must be 256-byte aligned");
+    const size_t need = psd::given_workspace(batch, gamma, params->vocab, bf16);
+    if (workspace_bytes < need) return fail(PSD_E_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
+    psd::GivenArgs a;
+    a.target = target_logits;
+    a.draft = draft_logits;
+    a.draft_tokens = draft_tokens;
+    a.n_drafts = n_drafts;
+    a.u = u;
+    a.e = e;
+    a.out_tokens = out_tokens;
+    a.out_len = out_len;
+    a.target_lse = target_lse;
+    a.draft_lse = draft_lse;
+    a.workspace = workspace;
+    a.B = batch;
+    a.gamma = gamma;
+    a.V = params->vocab;
+    a.T_target = params->temp_target;
+    a.T_draft = params->temp_draft;
+    const hipError_t err = psd::launch_given(a, bf16, stream);
+    if (err != hipSuccess) return hip_fail(err, "verification kernel launch");
     return PSD_OK;
 }
 

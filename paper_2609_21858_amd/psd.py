@@ -55,6 +55,59 @@ class Block(ctypes.Structure):
     ]
 
 
+class Cache(ctypes.Structure):
+    """psd_cache: keys and values in pages (make_cache)."""
+    _fields_ = [
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("dtype", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("page_tokens", ctypes.c_int32),
+        ("pages", ctypes.c_int32),
+        ("layers", ctypes.c_int32),
+        ("stride_layer", ctypes.c_int64),
+        ("stride_page", ctypes.c_int64),
+        ("stride_token", ctypes.c_int64),
+        ("stride_head", ctypes.c_int64),
+    ]
+
+
+class Seqs(ctypes.Structure):
+    """psd_seqs: the sequences of one call (make_seqs)."""
+    _fields_ = [
+        ("batch", ctypes.c_int32),
+        ("rows", ctypes.c_int32),
+        ("max_new", ctypes.c_int32),
+        ("max_kv", ctypes.c_int32),
+        ("table_width", ctypes.c_int32),
+        ("table_stride", ctypes.c_int64),
+        ("new_start", ctypes.c_void_p),
+        ("kv_len", ctypes.c_void_p),
+        ("table", ctypes.c_void_p),
+    ]
+
+
+class Rows(ctypes.Structure):
+    """psd_rows: packed rows of heads."""
+    _fields_ = [("data", ctypes.c_void_p), ("stride_row", ctypes.c_int64), ("stride_head", ctypes.c_int64)]
+
+
+class Rotation(ctypes.Structure):
+    """psd_rotation: norms and position rotation of psd_kv_append."""
+    _fields_ = [
+        ("rotary", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("positions_max", ctypes.c_int32),
+        ("cos", ctypes.c_void_p),
+        ("sin", ctypes.c_void_p),
+        ("positions", ctypes.c_void_p),
+        ("q_norm", ctypes.c_void_p),
+        ("k_norm", ctypes.c_void_p),
+        ("eps", ctypes.c_float),
+    ]
+
+
 class ToyLM(ctypes.Structure):
     """psd_toy_lm: the synthetic position-indexed model of psd_toy_logits / psd_generate."""
     _fields_ = [
@@ -104,6 +157,13 @@ def _load():
         "psd_generate_workspace_bytes": ([P, i32, i32], sz),
         "psd_generate": ([P, ctypes.POINTER(ToyLM), i32, i32, i32, vp, ctypes.c_int64, vp, sz, i32, i32,
                           ctypes.POINTER(i32), ctypes.POINTER(ctypes.c_uint32), vp], i32),
+        # structs by address: a Cache, Seqs, Rows or Rotation (or None for a NULL pointer) goes in by byref()
+        "psd_kv_append": ([vp, vp, vp, vp, vp, vp, vp, i32, vp], i32),
+        "psd_attention": ([vp, vp, vp, i32, ctypes.c_float, i32, vp, i32, vp, vp, vp, sz, vp], i32),
+        "psd_attention_workspace_bytes": ([vp, vp, i32], sz),
+        "psd_kv_keep": ([vp, vp, vp, ctypes.c_int64, i32, vp, vp, vp], i32),
+        "psd_verify_given": ([P, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp], i32),
+        "psd_verify_given_workspace_bytes": ([P, i32, i32], sz),
     }
     for name, (args, res) in sigs.items():
         f = getattr(lib, name)
@@ -117,7 +177,8 @@ EXPORTS = ("psd_abi_version", "psd_last_error", "psd_workspace_bytes", "psd_work
            "psd_workspace_errors", "psd_draft", "psd_verify", "psd_verify_static", "psd_detect", "psd_detect_pvalue", "psd_philox",
            "psd_context_keys", "psd_clock_values", "psd_set_spin_limit", "psd_detect_scores",
            "psd_detect_scores_pvalue", "psd_detection_rate", "psd_advance", "psd_toy_logits",
-           "psd_generate_workspace_bytes", "psd_generate")
+           "psd_generate_workspace_bytes", "psd_generate", "psd_kv_append", "psd_attention",
+           "psd_attention_workspace_bytes", "psd_kv_keep", "psd_verify_given", "psd_verify_given_workspace_bytes")
 
 
 def lib():
@@ -373,3 +434,188 @@ def generate(params: Params, lm: ToyLM, prompts, n_pos: int, gamma: int, check_e
                              ctypes.byref(bits), _stream(stream)))
     return text, int(blocks.value), int(bits.value)
 
+
+
+# ---------------------------------------------------------------- the target's pass over a block's new tokens
+
+def _need(cond, msg: str):
+    if not cond:
+        raise PsdError(PSD_E_ARG, msg)
+
+
+def _dtype(t) -> int:
+    _need(t.dtype in (torch.bfloat16, torch.float32), f"dtype {t.dtype} is neither bfloat16 nor float32")
+    return PSD_BF16 if t.dtype == torch.bfloat16 else PSD_F32
+
+
+def _ints(t, what: str, dim: int):
+    _need(t.dtype == torch.int32 and t.dim() == dim and (t.shape[-1] <= 1 or t.stride(-1) == 1),
+          f"{what}: int32 with {dim} dimensions, the last one contiguous")
+
+
+def make_cache(k, v) -> Cache:
+    """Pools [pages][page tokens][heads][head dim] (or [layers][pages]...) of any strides with a contiguous
+    last dimension; keeps both tensors alive."""
+    _need(k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype, "k and v pools differ in layout")
+    _need(k.dim() in (4, 5) and k.stride(-1) == 1, "pools are [layers][pages][page tokens][heads][head dim]")
+    pages, page, heads, dim = k.shape[-4:]
+    st = k.stride()
+    c = Cache(k.data_ptr(), v.data_ptr(), _dtype(k), heads, dim, page, pages, k.shape[0] if k.dim() == 5 else 1,
+              st[0] if k.dim() == 5 else 0, st[-4], st[-3], st[-2])
+    c.tensors = (k, v)
+    return c
+
+
+def make_seqs(new_start, kv_len, table, rows: int, max_new: int, max_kv: int) -> Seqs:
+    """Sequences of one call: new_start int32 [B+1], kv_len int32 [B], table int32 [B][width]; rows, max_new and
+    max_kv bound the lengths, which may change on the device.  Keeps the tensors alive."""
+    _ints(new_start, "new_start", 1)
+    _ints(kv_len, "kv_len", 1)
+    _ints(table, "table", 2)
+    B = int(kv_len.shape[0])
+    _need(new_start.shape[0] == B + 1 and table.shape[0] == B, "new_start [B+1], kv_len [B] and table [B][width] disagree")
+    s = Seqs(B, int(rows), int(max_new), int(max_kv), table.shape[1], max(table.stride(0), table.shape[1]),
+             new_start.data_ptr(), kv_len.data_ptr(), table.data_ptr())
+    s.tensors = (new_start, kv_len, table)
+    return s
+
+
+def _rows(t, what: str, cache: Cache, seqs: Seqs, heads: int = 0) -> Rows:
+    _need(t.dim() == 3 and t.shape[0] >= seqs.rows and t.shape[2] == cache.head_dim and
+          (heads == 0 or t.shape[1] == heads) and t.stride(2) == 1,
+          f"{what}: [rows][heads][head dim] with a contiguous last dimension")
+    _need(_dtype(t) == cache.dtype, f"{what}: dtype differs from the cache's")
+    return Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _ref(s):
+    return None if s is None else ctypes.byref(s)
+
+
+def kv_append(cache: Cache, seqs: Seqs, k, v, q=None, q_out=None, cos=None, sin=None, interleaved: bool = False,
+              positions=None, q_norm=None, k_norm=None, eps: float = 1e-6, stream=None):
+    """psd_kv_append: keys (normed with k_norm, turned by cos and sin float32 [positions][R/2]) and values into the
+    cache; returns the queries, treated the same way, in q_out (allocated when missing), or None without q."""
+    rk, rv = _rows(k, "k", cache, seqs, cache.heads), _rows(v, "v", cache, seqs, cache.heads)
+    rq = ro = None
+    H = 0
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        H = int(q.shape[1])
+        rq, ro = _rows(q, "q", cache, seqs), _rows(q_out, "q_out", cache, seqs, H)
+    R = P = 0
+    if cos is not None:
+        _need(sin is not None and cos.shape == sin.shape and cos.dim() == 2 and cos.dtype == sin.dtype == torch.float32
+              and cos.is_contiguous() and sin.is_contiguous(), "cos and sin: contiguous float32 [positions][R/2]")
+        P, R = cos.shape[0], 2 * cos.shape[1]
+    if positions is not None:
+        _ints(positions, "positions", 1)
+        _need(positions.shape[0] >= seqs.rows, "positions: int32 [rows]")
+    for w, what in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+        if w is not None:
+            _need(w.shape == (cache.head_dim,) and w.is_contiguous() and _dtype(w) == cache.dtype,
+                  f"{what}: [head dim] in the cache's dtype")
+    rot = Rotation(R, 1 if interleaved else 0, P, _ptr(cos), _ptr(sin), _ptr(positions), _ptr(q_norm), _ptr(k_norm), eps)
+    _check(_lib.psd_kv_append(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(rot), ctypes.byref(rk),
+                              ctypes.byref(rv), _ref(rq), _ref(ro), H, _stream(stream)))
+    return q_out
+
+
+def attention_workspace_bytes(cache: Cache, seqs: Seqs, q_heads: int) -> int:
+    n = int(_lib.psd_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(seqs), q_heads))
+    if n == ctypes.c_size_t(-1).value:
+        raise PsdError(PSD_E_ARG, (_lib.psd_last_error() or b"").decode())
+    return n
+
+
+def new_attention_workspace(cache: Cache, seqs: Seqs, q_heads: int, device="cuda") -> torch.Tensor:
+    """Device workspace of psd_attention for these bounds (uninitialised; may be empty)."""
+    return torch.empty(attention_workspace_bytes(cache, seqs, q_heads), dtype=torch.uint8, device=device)
+
+
+def attention(cache: Cache, seqs: Seqs, q, ws, scale: float = None, window: int = 0, mask=None, out=None,
+              want_lse: bool = False, lse=None, stream=None):
+    """psd_attention of q [rows][H][head dim] over the cache -> {"out", and "lse" float32 [rows][H] with
+    want_lse}.  mask: int32 [rows][words], bit j % 32 of word j / 32 for new token j (draft paths).  scale
+    defaults to 1 / sqrt(head dim)."""
+    H = int(q.shape[1])
+    rq = _rows(q, "q", cache, seqs)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    ro = _rows(out, "out", cache, seqs, H)
+    o = {"out": out}
+    if want_lse:
+        if lse is None:
+            lse = torch.empty((q.shape[0], H), dtype=torch.float32, device=q.device)
+        _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape[0] >= seqs.rows and lse.shape[1:] == (H,),
+              "lse: contiguous float32 [rows][H]")
+        o["lse"] = lse
+    words = 0
+    if mask is not None:
+        _ints(mask, "mask", 2)
+        _need(mask.shape[0] >= seqs.rows and mask.is_contiguous(), "mask: contiguous int32 [rows][words]")
+        words = int(mask.shape[1])
+    if scale is None:
+        scale = cache.head_dim ** -0.5
+    _check(_lib.psd_attention(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(rq), H, scale, window, _ptr(mask), words,
+                              ctypes.byref(ro), _ptr(o.get("lse")), _ptr(ws), 0 if ws is None else ws.numel(),
+                              _stream(stream)))
+    return o
+
+
+def kv_keep(cache: Cache, seqs: Seqs, keep, n_keep, kv_out=None, stream=None):
+    """psd_kv_keep: new tokens keep[b][i] (int32 [B][width], strictly ascending), i < n_keep[b] (int32 [B]), move to the
+    first new positions in every layer of the cache; returns the sequences' new lengths (int32 [B])."""
+    _ints(keep, "keep", 2)
+    _ints(n_keep, "n_keep", 1)
+    _need(keep.shape[0] == seqs.batch and n_keep.shape[0] == seqs.batch, "keep [B][width], n_keep [B]")
+    if kv_out is None:
+        kv_out = torch.empty((seqs.batch,), dtype=torch.int32, device=keep.device)
+    _ints(kv_out, "kv_out", 1)
+    _need(kv_out.shape[0] >= seqs.batch, "kv_out: int32 [B]")
+    _check(_lib.psd_kv_keep(ctypes.byref(cache), ctypes.byref(seqs), _ptr(keep), max(keep.stride(0), keep.shape[1]),
+                            keep.shape[1], _ptr(n_keep), _ptr(kv_out), _stream(stream)))
+    return kv_out
+
+
+# ---------------------------------------------------------------- verification from given random numbers
+
+def verify_given_workspace_bytes(params: Params, batch: int, gamma: int) -> int:
+    return int(_lib.psd_verify_given_workspace_bytes(ctypes.byref(params), batch, gamma))
+
+
+def new_verify_given_workspace(params: Params, batch: int, gamma: int, device="cuda") -> torch.Tensor:
+    """Device workspace of psd_verify_given (uninitialised)."""
+    n = verify_given_workspace_bytes(params, batch, gamma)
+    if n == 0:
+        raise PsdError(PSD_E_ARG, (_lib.psd_last_error() or b"").decode())
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def verify_given(params: Params, ws, target_logits, draft_logits, draft_tokens, u, e, n_drafts=None,
+                 want_lse: bool = False, out=None, stream=None):
+    """psd_verify_given: target rows [B][gamma+1][V], draft rows [B][gamma][V], drafts int32 [B][gamma], u float32
+    [B][gamma], e float32 [B][V] -> {"out_tokens" int32 [B][gamma+1], "out_len" int32 [B], and with want_lse
+    "target_lse", "draft_lse"}."""
+    B, gamma = int(draft_tokens.shape[0]), int(draft_tokens.shape[1])
+    V, dev = params.vocab, draft_tokens.device
+    for t, shape, what in ((target_logits, (B, gamma + 1, V), "target_logits"), (draft_logits, (B, gamma, V), "draft_logits")):
+        _need(t.shape == shape and t.is_contiguous() and _dtype(t) == params.dtype, f"{what}: contiguous {shape} in params' dtype")
+    _need(draft_tokens.dtype == torch.int32 and draft_tokens.is_contiguous(), "draft_tokens: contiguous int32 [B][gamma]")
+    for t, shape, what in ((u, (B, gamma), "u"), (e, (B, V), "e")):
+        _need(t.shape == shape and t.is_contiguous() and t.dtype == torch.float32, f"{what}: contiguous float32 {shape}")
+    if n_drafts is not None:
+        _ints(n_drafts, "n_drafts", 1)
+        _need(n_drafts.shape[0] == B, "n_drafts: int32 [B]")
+    o = {} if out is None else dict(out)
+    o.setdefault("out_tokens", torch.empty((B, gamma + 1), dtype=torch.int32, device=dev))
+    o.setdefault("out_len", torch.empty((B,), dtype=torch.int32, device=dev))
+    if want_lse:
+        o.setdefault("target_lse", torch.empty((B, gamma + 1), dtype=torch.float32, device=dev))
+        o.setdefault("draft_lse", torch.empty((B, gamma), dtype=torch.float32, device=dev))
+    _check(_lib.psd_verify_given(ctypes.byref(params), B, gamma, _ptr(target_logits), _ptr(draft_logits), _ptr(draft_tokens),
+                                 _ptr(n_drafts), _ptr(u), _ptr(e), _ptr(o["out_tokens"]), _ptr(o["out_len"]),
+                                 _ptr(o.get("target_lse")), _ptr(o.get("draft_lse")), _ptr(ws), ws.numel(),
+                                 _stream(stream)))
+    return o
