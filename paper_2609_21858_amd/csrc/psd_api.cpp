@@ -1199,7 +1199,7 @@ psd_status psd_attention(const psd_cache* cache, const psd_seqs* seqs, const psd
     psd::AttentionArgs a;
     memset(&a, 0, sizeof a);
     a.c = cache_args(cache, seqs);
-    if (!psd::attention_fits(a.c, q_heads) || (long)seqs->rows * q_heads / 4 >= kMaxGrid)
+    if (!psd::attention_fits(a.c, q_heads, bf16) || (long)seqs->rows * q_heads / 4 >= kMaxGrid)
         return fail(PSD_E_ARG, "call too large: batch %d, rows %d, max_new %d", seqs->batch, seqs->rows, seqs->max_new);
     const size_t need = psd::attention_workspace(a.c, q_heads, bf16);
     if (need > 0) {

@@ -509,6 +509,332 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
     }
 }
 
+// ---------------------------------------------------------------- many rows
+
+// One workgroup: 128 rows of one (sequence, key/value head), 32 a wave, over one part of its cache.
+// Blocks of 64 tokens go through LDS, which all four waves read: 32x32x16 products, 64 x 32
+// scores a wave in 32 registers, the outputs in D/2 more.  Two buffers, one barrier a block: while
+// block n is computed, block n + 1 is on its way into registers, and is stored behind the
+// arithmetic.  Two workgroups a CU (two waves a SIMD), so one wave's exponentials overlap
+// the other's products.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <int DP>
+struct TileShape {
+    static constexpr int TOK = 64;
+    static constexpr int ROWS = 128;
+    static constexpr int LPR = DP / 8;              // 16-byte pieces of a token
+    static constexpr int TPP = kThreads / LPR;      // tokens of one load of the workgroup
+    static constexpr int N = TOK / TPP;             // loads a block
+    // Row pitches (elements): 8 lanes reading 16 bytes of 8 consecutive keys, and the 4-token by
+    // 64-byte tiles of the transposing reads, fall on different banks.
+    static constexpr int KP = DP + 8, VP = DP + 32;
+    static constexpr int BYTES = TOK * (KP + VP) * 2;
+};
+
+template <int DP>
+__global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(AttentionArgs a, Plan p) {
+    using S = TileShape<DP>;
+    constexpr int KK = DP / 16, DB = DP / 32;
+    __shared__ __align__(16) char s_mem[2 * S::BYTES];  // two buffers of keys and values
+    __shared__ int64_t s_off[4][S::TOK];                // written two blocks ahead, read in two
+    __shared__ uint64_t s_there[4];
+    __shared__ int s_odd[2];
+
+    const CacheArgs& c = a.c;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int r = lane & 31, hi = lane >> 5;
+    int x = blockIdx.x;
+    const int g = x % c.G;
+    x /= c.G;
+    const int tile = p.tiles - 1 - x % p.tiles;  // causal rows: the longest first
+    x /= p.tiles;
+    const int b = x % c.B, part = x / c.B;
+
+    const Seq s = load_seq(c, b);
+    const int row0 = tile * S::ROWS;
+    const int rows = min(s.n * p.h - row0, S::ROWS);
+    if (rows <= 0) return;
+    const int i_lo = row0 / p.h, i_hi = (row0 + rows - 1) / p.h;
+    const Range range = tile_range(a, s, i_lo, i_hi);
+    const int n_parts = max((range.hi - range.lo + p.chunk - 1) / p.chunk, 1);
+    if (part >= n_parts) return;
+    const int c0 = range.lo + part * p.chunk, c1 = min(c0 + p.chunk, range.hi);
+    const int blocks = (c1 - c0 + S::TOK - 1) / S::TOK;
+    const int32_t* table = c.table + (int64_t)b * c.table_stride;
+
+    // this wave's rows: new tokens [w_lo, w_hi]; a wave without rows keeps company with zeros
+    const int mine = min(max(rows - wave * 32, 0), 32);
+    const int w_lo = (row0 + min(wave * 32, rows - 1)) / p.h, w_hi = (row0 + min(wave * 32 + 31, rows - 1)) / p.h;
+    const bool on = r < mine;
+    const int rr = row0 + wave * 32 + r;
+    const int row_i = on ? rr / p.h : w_lo;
+    const int head = g * p.h + (on ? rr - row_i * p.h : 0);
+    const int64_t t_row = s.row0 + row_i;
+    // scores in units of ln 2; a negative scale goes into the queries' signs, so that a maximum
+    // of products is a maximum of scores
+    const float sc = fmaxf(fabsf(a.scale) * kLog2e, 1.17549435e-38f);
+    const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
+    u32x4 qf[KK];
+    {
+        const char* src = (const char*)a.q.data + (t_row * a.q.stride_row + (int64_t)head * a.q.stride_head) * 2;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            const int d = kk * 16 + hi * 8;
+            qf[kk] = u32x4{0, 0, 0, 0};
+            if (on && d < c.D) {
+                qf[kk] = *(const u32x4*)(src + d * 2);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) qf[kk][e] ^= sign;
+            }
+        }
+    }
+    f32x16 o[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[db][e] = 0.f;
+    float m = kNoScore, l = 0.f;
+
+    const int64_t head_at = (int64_t)g * c.stride_head;
+    const int piece = tid % S::LPR, token = tid / S::LPR;
+    const int d_piece = min(piece * 8, c.D - 8);
+    const bool past = piece * 8 >= c.D;  // keys past the head's end count as zero
+    const char* k_src = (const char*)c.k + (head_at + d_piece) * 2;
+    const char* v_src = (const char*)c.v + (head_at + d_piece) * 2;
+
+    auto locate = [&](int blk) -> int64_t {  // threads of wave 0
+        const int j = c0 + blk * S::TOK + tid;
+        if (blk >= blocks || j >= c1) return -1;
+        return token_offset(c, p, table, j);
+    };
+    auto publish = [&](int blk, int64_t off) {
+        s_off[blk & 3][tid] = max(off, (int64_t)0);
+        const uint64_t bits = __ballot(off >= 0);
+        if (tid == 0) s_there[blk & 3] = bits;
+    };
+    u32x4 kf[S::N], vf[S::N];
+    auto load = [&](int blk) {
+#pragma unroll
+        for (int k = 0; k < S::N; ++k) {
+            const int64_t at = s_off[blk & 3][k * S::TPP + token] * 2;
+            kf[k] = *(const u32x4*)(k_src + at);
+            vf[k] = *(const u32x4*)(v_src + at);
+        }
+    };
+    // Does every row of new tokens [lo, hi] see the whole block?
+    auto whole = [&](int blk, int lo, int top) {
+        const int j0 = c0 + blk * S::TOK;
+        if (s_there[blk & 3] != ~0ull) return false;
+        if (a.mask) return j0 + S::TOK <= s.first;
+        return j0 + S::TOK - 1 <= s.first + lo && (a.window == 0 || j0 > s.first + top - a.window);
+    };
+    auto key_at = [&](int blk) { return s_mem + (blk & 1) * S::BYTES; };
+    auto value_at = [&](int blk) { return s_mem + (blk & 1) * S::BYTES + S::TOK * S::KP * 2; };
+    // Into LDS.  Where rows differ in what they see, values of tokens that are not there are zeroed
+    // and infinite or NaN values taken out (a weight 0 times them is NaN for rows that do not see them).
+    auto store = [&](int blk) {
+        if (past)
+#pragma unroll
+            for (int k = 0; k < S::N; ++k) kf[k] = u32x4{0, 0, 0, 0};
+        if (!whole(blk, i_lo, i_hi)) {
+            const uint64_t there = s_there[blk & 3];
+            bool odd = false;
+#pragma unroll
+            for (int k = 0; k < S::N; ++k) {
+                const bool gone = !((there >> (k * S::TPP + token)) & 1u);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t w = gone ? 0u : vf[k][e];
+                    const bool lo_odd = odd_lo<true>(w), hi_odd = odd_hi(w);
+                    odd |= lo_odd || hi_odd;
+                    if (lo_odd) w &= 0xFFFF0000u;
+                    if (hi_odd) w &= 0xFFFFu;
+                    vf[k][e] = w;
+                }
+            }
+            if (odd) s_odd[blk & 1] = blk + 1;
+        }
+        char* keys = key_at(blk);
+        char* values = value_at(blk);
+#pragma unroll
+        for (int k = 0; k < S::N; ++k) {
+            *(u32x4*)(keys + ((k * S::TPP + token) * S::KP + piece * 8) * 2) = kf[k];
+            *(u32x4*)(values + ((k * S::TPP + token) * S::VP + piece * 8) * 2) = vf[k];
+        }
+    };
+    // this lane's dimension of 32 db + .., tokens 16 ks + {4 hi .., 8 + 4 hi ..}, as an A operand
+    auto value = [&](const char* values, int db, int ks) -> bf16x8 {
+        const int i = lane & 15;
+        const char* at = values + ((16 * ks + 4 * hi + i / 4) * S::VP + db * 32 + ((lane >> 4) & 1) * 16 + (i % 4) * 4) * 2;
+        union {
+            s16x4 half[2];
+            bf16x8 all;
+        } v;
+        v.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
+        v.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * S::VP * 2));
+        return v.all;
+    };
+
+    int64_t off = -1;
+    if (wave == 0) {
+        publish(0, locate(0));
+        off = locate(1);
+    }
+    if (tid < 2) s_odd[tid] = 0;
+    __syncthreads();
+    if (blocks > 0) load(0);
+    if (wave == 0) {
+        publish(1, off);
+        off = locate(2);
+    }
+    if (blocks > 0) store(0);
+    for (int blk = 0; blk < blocks; ++blk) {
+        __syncthreads();
+        const int j0 = c0 + blk * S::TOK;
+        const bool more = blk + 1 < blocks;
+        if (more) load(blk + 1);
+        const bool seen_by_all = whole(blk, w_lo, w_hi);
+        const uint64_t there = s_there[blk & 3];
+        // nothing of the block lies before this wave's last row's end (or behind its window)
+        const bool idle = mine == 0 || (!a.mask && (j0 > s.first + w_hi ||
+                                                    (a.window > 0 && j0 + S::TOK - 1 <= s.first + w_lo - a.window)));
+        uint32_t bits[2] = {~0u, ~0u};
+        if (!idle) {
+            const char* keys = key_at(blk);
+            const char* values = value_at(blk);
+            f32x16 sv[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sv[t][e] = 0.f;
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) {
+                    const u32x4 kv = *(const u32x4*)(keys + ((32 * t + r) * S::KP + kk * 16 + hi * 8) * 2);
+                    sv[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kv),
+                                                                    __builtin_bit_cast(bf16x8, qf[kk]), sv[t], 0, 0, 0);
+                }
+            }
+            if (!seen_by_all) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    // this lane's tokens: 8 (e / 4) + 4 hi + e % 4
+                    bits[t] = ((uint32_t)(there >> (32 * t)) & row_bits(a, s, row_i, (int)t_row, j0 + 32 * t)) >> (4 * hi);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sv[t][e] = bits[t] & (1u << (8 * (e / 4) + e % 4)) ? sv[t][e] : kNoScore;
+                }
+            }
+            float top = sv[0][0];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, sv[t][e]);
+            top *= sc;
+            if (__any(top > m + kSlack)) {
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float next = fmaxf(m, top);
+                const float by = next == kNoScore ? 1.f : exp2_hw(m - next);
+                m = next;
+                l *= by;
+#pragma unroll
+                for (int db = 0; db < DB; ++db) o[db] *= by;
+            }
+            const float from = m == kNoScore ? 0.f : m;
+            u32x4 w[4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    const float w0 = exp2_hw(__builtin_fmaf(sv[t][e], sc, -from));
+                    const float w1 = exp2_hw(__builtin_fmaf(sv[t][e + 1], sc, -from));
+                    l += w0;
+                    l += w1;
+                    w[2 * t + e / 8][(e % 8) / 2] = pack_bf16(w0, w1);
+                }
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(values, db, ks), __builtin_bit_cast(bf16x8, w[ks]), o[db],
+                                                                    0, 0, 0);
+        }
+        if (s_odd[blk & 1] == blk + 1) {
+            // infinite or NaN values were taken out of this block: a product of the largest finite
+            // numbers puts infinity where a row sees one
+            u32x4 again[S::N];
+#pragma unroll
+            for (int k = 0; k < S::N; ++k) again[k] = *(const u32x4*)(v_src + s_off[blk & 3][k * S::TPP + token] * 2);
+            __syncthreads();
+            char* values = value_at(blk);
+#pragma unroll
+            for (int k = 0; k < S::N; ++k) {
+                const bool gone = !((there >> (k * S::TPP + token)) & 1u);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t v = again[k][e];
+                    again[k][e] = gone ? 0u : (odd_lo<true>(v) ? 0x7F7Fu : 0u) | (odd_hi(v) ? 0x7F7F0000u : 0u);
+                }
+                *(u32x4*)(values + ((k * S::TPP + token) * S::VP + piece * 8) * 2) = again[k];
+            }
+            __syncthreads();
+            if (!idle) {
+                u32x4 w[4];
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const int bit = 16 * (ks & 1) + 8 * (e / 4) + e % 4;
+                        w[ks][e / 2] = (bits[ks / 2] >> bit & 1u ? 0x7F7Fu : 0u) | (bits[ks / 2] >> (bit + 1) & 1u ? 0x7F7F0000u : 0u);
+                    }
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks)
+                        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(values, db, ks), __builtin_bit_cast(bf16x8, w[ks]),
+                                                                        o[db], 0, 0, 0);
+            }
+        }
+        if (more) store(blk + 1);
+        if (wave == 0) {
+            publish(blk + 2, off);
+            off = locate(blk + 3);
+        }
+    }
+
+    l += __shfl_xor(l, 32);
+    if (!on) return;
+    if (n_parts == 1) {
+        const float by = m == kNoScore ? 0.f : 1.f / l;
+        char* dst = (char*)a.out.data + (t_row * a.out.stride_row + (int64_t)head * a.out.stride_head) * 2;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const int d = db * 32 + 2 * e + 4 * hi;
+                if (d >= c.D) continue;
+                uint2 y = make_uint2(0, 0);
+                if (m != kNoScore)
+                    y = make_uint2(pack_bf16(o[db][e] * by, o[db][e + 1] * by), pack_bf16(o[db][e + 2] * by, o[db][e + 3] * by));
+                *(uint2*)(dst + d * 2) = y;
+            }
+        if (hi == 0 && a.lse) a.lse[t_row * a.H + head] = m == kNoScore ? kNoScore : (m + log2f(l)) * kLn2;
+    } else {
+        const int64_t at = ((int64_t)part * c.rows + t_row) * a.H + head;
+        float* dst = (float*)a.workspace + at * c.D;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const int d = db * 32 + 2 * e + 4 * hi;
+                if (d < c.D) *(f32x4*)(dst + d) = f32x4{o[db][e], o[db][e + 1], o[db][e + 2], o[db][e + 3]};
+            }
+        if (hi == 0) {
+            float2* ml = (float2*)((float*)a.workspace + (int64_t)p.parts * c.rows * a.H * c.D);
+            ml[at] = make_float2(m, l);
+        }
+    }
+}
+
 // Joins the parts of each (row, head): one wave each, the weights of up to 64 parts in its lanes.
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a, Plan p) {
@@ -562,12 +888,12 @@ constexpr int kMaxParts = 64;   // join_kernel holds a part's weight in a lane
 constexpr int kMinChunk = 128;  // cached tokens of a part at least: a block per wave
 constexpr long kFill = 1024;    // workgroups that fill the device: 4 for each of 256 CUs
 
-Plan make_plan(const CacheArgs& c, int H, int span) {
+Plan make_plan(const CacheArgs& c, int H, bool bf16, int span) {
     Plan p;
     p.h = H / c.G;
     const long most = (long)c.max_new * p.h;
     const int limit = c.D > 128 ? 32 : 64;
-    p.tile_rows = most <= 16 ? 16 : most <= 32 ? 32 : limit;
+    p.tile_rows = most <= 16 ? 16 : most <= 32 ? 32 : bf16 && most > 64 ? 128 : limit;
     p.tiles = (int)((most + p.tile_rows - 1) / p.tile_rows);
     const long groups = (long)c.B * c.G * p.tiles;
     const long want = std::min<long>(std::min<long>((kFill + groups - 1) / groups, (span + kMinChunk - 1) / kMinChunk), kMaxParts);
@@ -593,14 +919,13 @@ void launch_stream(const AttentionArgs& a, const Plan& p, dim3 grid, hipStream_t
 }  // namespace
 
 size_t attention_workspace(const CacheArgs& c, int H, bool bf16) {
-    (void)bf16;
-    const Plan p = make_plan(c, H, c.max_kv);
+    const Plan p = make_plan(c, H, bf16, c.max_kv);
     if (p.parts == 1) return 0;
     return align256((size_t)p.parts * c.rows * H * (c.D + 2) * 4);
 }
 
-bool attention_fits(const CacheArgs& c, int H) {
-    const Plan p = make_plan(c, H, c.max_kv);
+bool attention_fits(const CacheArgs& c, int H, bool bf16) {
+    const Plan p = make_plan(c, H, bf16, c.max_kv);
     return (long)c.B * c.G * p.tiles * p.parts < 1L << 23;
 }
 
@@ -608,9 +933,16 @@ hipError_t launch_attention(const AttentionArgs& a, bool bf16, hipStream_t strea
     const CacheArgs& c = a.c;
     // a windowed row sees at most `window` positions, a tile's rows together max_new - 1 more
     const int span = a.window > 0 ? (int)std::min<long>(c.max_kv, (long)a.window + c.max_new - 1) : c.max_kv;
-    const Plan p = make_plan(c, a.H, span);
+    const Plan p = make_plan(c, a.H, bf16, span);
     const dim3 grid((unsigned)((long)c.B * c.G * p.tiles * p.parts));
-    if (bf16) {
+    if (p.tile_rows == 128) {
+        if (c.D <= 64)
+            hipLaunchKernelGGL(tile_kernel<64>, grid, dim3(kThreads), 0, stream, a, p);
+        else if (c.D <= 128)
+            hipLaunchKernelGGL(tile_kernel<128>, grid, dim3(kThreads), 0, stream, a, p);
+        else
+            hipLaunchKernelGGL(tile_kernel<256>, grid, dim3(kThreads), 0, stream, a, p);
+    } else if (bf16) {
         if (c.D <= 64)
             launch_stream<true, 64>(a, p, grid, stream);
         else if (c.D <= 128)

@@ -64,7 +64,7 @@ struct AttentionArgs {
     void* workspace;
 };
 size_t attention_workspace(const CacheArgs& c, int H, bool bf16);
-bool attention_fits(const CacheArgs& c, int H);  // the launch stays inside a grid's limits
+bool attention_fits(const CacheArgs& c, int H, bool bf16);  // the launch stays inside a grid's limits
 hipError_t launch_attention(const AttentionArgs& a, bool bf16, hipStream_t stream);
 
 struct GivenArgs {
