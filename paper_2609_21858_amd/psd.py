@@ -196,7 +196,8 @@ def _ptr(t):
 
 def _stream(stream=None):
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # the current stream's handle without a Stream object around it (0.1 us instead of 2.8)
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -438,26 +439,34 @@ def generate(params: Params, lm: ToyLM, prompts, n_pos: int, gamma: int, check_e
 
 # ---------------------------------------------------------------- the target's pass over a block's new tokens
 
-def _need(cond, msg: str):
-    if not cond:
-        raise PsdError(PSD_E_ARG, msg)
+# A refusal builds its message only when it refuses: a call's checks cost about a microsecond.
+
+def _refuse(msg: str):
+    raise PsdError(PSD_E_ARG, msg)
+
+
+_DTYPES = {torch.bfloat16: PSD_BF16, torch.float32: PSD_F32}
 
 
 def _dtype(t) -> int:
-    _need(t.dtype in (torch.bfloat16, torch.float32), f"dtype {t.dtype} is neither bfloat16 nor float32")
-    return PSD_BF16 if t.dtype == torch.bfloat16 else PSD_F32
+    d = _DTYPES.get(t.dtype)
+    if d is None:
+        _refuse(f"dtype {t.dtype} is neither bfloat16 nor float32")
+    return d
 
 
-def _ints(t, what: str, dim: int):
-    _need(t.dtype == torch.int32 and t.dim() == dim and (t.shape[-1] <= 1 or t.stride(-1) == 1),
-          f"{what}: int32 with {dim} dimensions, the last one contiguous")
+def _ints(t, what: str, dim: int, rows: int = 0):
+    if t.dtype != torch.int32 or t.dim() != dim or (t.shape[-1] > 1 and t.stride(-1) != 1) or t.shape[0] < rows:
+        _refuse(f"{what}: int32 with {dim} dimensions, at least {rows} long, the last dimension contiguous")
 
 
 def make_cache(k, v) -> Cache:
     """Pools [pages][page tokens][heads][head dim] (or [layers][pages]...) of any strides with a contiguous
     last dimension; keeps both tensors alive."""
-    _need(k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype, "k and v pools differ in layout")
-    _need(k.dim() in (4, 5) and k.stride(-1) == 1, "pools are [layers][pages][page tokens][heads][head dim]")
+    if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+        _refuse("k and v pools differ in layout")
+    if k.dim() not in (4, 5) or k.stride(-1) != 1:
+        _refuse("pools are [layers][pages][page tokens][heads][head dim]")
     pages, page, heads, dim = k.shape[-4:]
     st = k.stride()
     c = Cache(k.data_ptr(), v.data_ptr(), _dtype(k), heads, dim, page, pages, k.shape[0] if k.dim() == 5 else 1,
@@ -473,19 +482,20 @@ def make_seqs(new_start, kv_len, table, rows: int, max_new: int, max_kv: int) ->
     _ints(kv_len, "kv_len", 1)
     _ints(table, "table", 2)
     B = int(kv_len.shape[0])
-    _need(new_start.shape[0] == B + 1 and table.shape[0] == B, "new_start [B+1], kv_len [B] and table [B][width] disagree")
+    if new_start.shape[0] != B + 1 or table.shape[0] != B:
+        _refuse("new_start [B+1], kv_len [B] and table [B][width] disagree")
     s = Seqs(B, int(rows), int(max_new), int(max_kv), table.shape[1], max(table.stride(0), table.shape[1]),
              new_start.data_ptr(), kv_len.data_ptr(), table.data_ptr())
     s.tensors = (new_start, kv_len, table)
     return s
 
 
-def _rows(t, what: str, cache: Cache, seqs: Seqs, heads: int = 0) -> Rows:
-    _need(t.dim() == 3 and t.shape[0] >= seqs.rows and t.shape[2] == cache.head_dim and
-          (heads == 0 or t.shape[1] == heads) and t.stride(2) == 1,
-          f"{what}: [rows][heads][head dim] with a contiguous last dimension")
-    _need(_dtype(t) == cache.dtype, f"{what}: dtype differs from the cache's")
-    return Rows(t.data_ptr(), t.stride(0), t.stride(1))
+def _rows(t, what: str, cache: Cache, rows: int, heads: int) -> Rows:
+    shape, stride = t.shape, t.stride()
+    if (len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != cache.head_dim or stride[2] != 1
+            or _DTYPES.get(t.dtype) != cache.dtype):
+        _refuse(f"{what}: [{rows}][{heads}][{cache.head_dim}] in the cache's dtype with a contiguous last dimension")
+    return Rows(t.data_ptr(), stride[0], stride[1])
 
 
 def _ref(s):
@@ -496,26 +506,27 @@ def kv_append(cache: Cache, seqs: Seqs, k, v, q=None, q_out=None, cos=None, sin=
               positions=None, q_norm=None, k_norm=None, eps: float = 1e-6, stream=None):
     """psd_kv_append: keys (normed with k_norm, turned by cos and sin float32 [positions][R/2]) and values into the
     cache; returns the queries, treated the same way, in q_out (allocated when missing), or None without q."""
-    rk, rv = _rows(k, "k", cache, seqs, cache.heads), _rows(v, "v", cache, seqs, cache.heads)
+    rows, heads = seqs.rows, cache.heads
+    rk, rv = _rows(k, "k", cache, rows, heads), _rows(v, "v", cache, rows, heads)
     rq = ro = None
     H = 0
     if q is not None:
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        H = int(q.shape[1])
-        rq, ro = _rows(q, "q", cache, seqs), _rows(q_out, "q_out", cache, seqs, H)
+        H = q.shape[1]
+        rq, ro = _rows(q, "q", cache, rows, H), _rows(q_out, "q_out", cache, rows, H)
     R = P = 0
     if cos is not None:
-        _need(sin is not None and cos.shape == sin.shape and cos.dim() == 2 and cos.dtype == sin.dtype == torch.float32
-              and cos.is_contiguous() and sin.is_contiguous(), "cos and sin: contiguous float32 [positions][R/2]")
-        P, R = cos.shape[0], 2 * cos.shape[1]
+        if (sin is None or cos.shape != sin.shape or cos.dim() != 2 or cos.dtype != torch.float32
+                or sin.dtype != torch.float32 or not cos.is_contiguous() or not sin.is_contiguous()):
+            _refuse("cos and sin: contiguous float32 [positions][R/2]")
+        P, R = cos.shape
+        R *= 2
     if positions is not None:
-        _ints(positions, "positions", 1)
-        _need(positions.shape[0] >= seqs.rows, "positions: int32 [rows]")
-    for w, what in ((q_norm, "q_norm"), (k_norm, "k_norm")):
-        if w is not None:
-            _need(w.shape == (cache.head_dim,) and w.is_contiguous() and _dtype(w) == cache.dtype,
-                  f"{what}: [head dim] in the cache's dtype")
+        _ints(positions, "positions", 1, rows)
+    for w in (q_norm, k_norm):
+        if w is not None and (w.shape != (cache.head_dim,) or not w.is_contiguous() or _dtype(w) != cache.dtype):
+            _refuse("q_norm and k_norm: [head dim] in the cache's dtype")
     rot = Rotation(R, 1 if interleaved else 0, P, _ptr(cos), _ptr(sin), _ptr(positions), _ptr(q_norm), _ptr(k_norm), eps)
     _check(_lib.psd_kv_append(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(rot), ctypes.byref(rk),
                               ctypes.byref(rv), _ref(rq), _ref(ro), H, _stream(stream)))
@@ -539,23 +550,24 @@ def attention(cache: Cache, seqs: Seqs, q, ws, scale: float = None, window: int 
     """psd_attention of q [rows][H][head dim] over the cache -> {"out", and "lse" float32 [rows][H] with
     want_lse}.  mask: int32 [rows][words], bit j % 32 of word j / 32 for new token j (draft paths).  scale
     defaults to 1 / sqrt(head dim)."""
-    H = int(q.shape[1])
-    rq = _rows(q, "q", cache, seqs)
+    H, rows = q.shape[1], seqs.rows
+    rq = _rows(q, "q", cache, rows, H)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    ro = _rows(out, "out", cache, seqs, H)
+    ro = _rows(out, "out", cache, rows, H)
     o = {"out": out}
     if want_lse:
         if lse is None:
             lse = torch.empty((q.shape[0], H), dtype=torch.float32, device=q.device)
-        _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape[0] >= seqs.rows and lse.shape[1:] == (H,),
-              "lse: contiguous float32 [rows][H]")
+        elif lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape[0] < rows or lse.shape[1:] != (H,):
+            _refuse("lse: contiguous float32 [rows][H]")
         o["lse"] = lse
     words = 0
     if mask is not None:
-        _ints(mask, "mask", 2)
-        _need(mask.shape[0] >= seqs.rows and mask.is_contiguous(), "mask: contiguous int32 [rows][words]")
-        words = int(mask.shape[1])
+        _ints(mask, "mask", 2, rows)
+        if not mask.is_contiguous():
+            _refuse("mask: contiguous int32 [rows][words]")
+        words = mask.shape[1]
     if scale is None:
         scale = cache.head_dim ** -0.5
     _check(_lib.psd_attention(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(rq), H, scale, window, _ptr(mask), words,
@@ -567,13 +579,15 @@ def attention(cache: Cache, seqs: Seqs, q, ws, scale: float = None, window: int 
 def kv_keep(cache: Cache, seqs: Seqs, keep, n_keep, kv_out=None, stream=None):
     """psd_kv_keep: new tokens keep[b][i] (int32 [B][width], strictly ascending), i < n_keep[b] (int32 [B]), move to the
     first new positions in every layer of the cache; returns the sequences' new lengths (int32 [B])."""
+    B = seqs.batch
     _ints(keep, "keep", 2)
     _ints(n_keep, "n_keep", 1)
-    _need(keep.shape[0] == seqs.batch and n_keep.shape[0] == seqs.batch, "keep [B][width], n_keep [B]")
+    if keep.shape[0] != B or n_keep.shape[0] != B:
+        _refuse("keep [B][width], n_keep [B]")
     if kv_out is None:
-        kv_out = torch.empty((seqs.batch,), dtype=torch.int32, device=keep.device)
-    _ints(kv_out, "kv_out", 1)
-    _need(kv_out.shape[0] >= seqs.batch, "kv_out: int32 [B]")
+        kv_out = torch.empty((B,), dtype=torch.int32, device=keep.device)
+    else:
+        _ints(kv_out, "kv_out", 1, B)
     _check(_lib.psd_kv_keep(ctypes.byref(cache), ctypes.byref(seqs), _ptr(keep), max(keep.stride(0), keep.shape[1]),
                             keep.shape[1], _ptr(n_keep), _ptr(kv_out), _stream(stream)))
     return kv_out
@@ -600,20 +614,27 @@ def verify_given(params: Params, ws, target_logits, draft_logits, draft_tokens, 
     "target_lse", "draft_lse"}."""
     B, gamma = int(draft_tokens.shape[0]), int(draft_tokens.shape[1])
     V, dev = params.vocab, draft_tokens.device
-    for t, shape, what in ((target_logits, (B, gamma + 1, V), "target_logits"), (draft_logits, (B, gamma, V), "draft_logits")):
-        _need(t.shape == shape and t.is_contiguous() and _dtype(t) == params.dtype, f"{what}: contiguous {shape} in params' dtype")
-    _need(draft_tokens.dtype == torch.int32 and draft_tokens.is_contiguous(), "draft_tokens: contiguous int32 [B][gamma]")
-    for t, shape, what in ((u, (B, gamma), "u"), (e, (B, V), "e")):
-        _need(t.shape == shape and t.is_contiguous() and t.dtype == torch.float32, f"{what}: contiguous float32 {shape}")
+    if (target_logits.shape != (B, gamma + 1, V) or draft_logits.shape != (B, gamma, V)
+            or _dtype(target_logits) != params.dtype or _dtype(draft_logits) != params.dtype
+            or not target_logits.is_contiguous() or not draft_logits.is_contiguous()):
+        _refuse(f"target_logits ({B}, {gamma + 1}, {V}) and draft_logits ({B}, {gamma}, {V}): contiguous, in params' dtype")
+    if draft_tokens.dtype != torch.int32 or not draft_tokens.is_contiguous():
+        _refuse("draft_tokens: contiguous int32 [B][gamma]")
+    if (u.shape != (B, gamma) or e.shape != (B, V) or u.dtype != torch.float32 or e.dtype != torch.float32
+            or not u.is_contiguous() or not e.is_contiguous()):
+        _refuse(f"u ({B}, {gamma}) and e ({B}, {V}): contiguous float32")
     if n_drafts is not None:
         _ints(n_drafts, "n_drafts", 1)
-        _need(n_drafts.shape[0] == B, "n_drafts: int32 [B]")
+        if n_drafts.shape[0] != B:
+            _refuse("n_drafts: int32 [B]")
     o = {} if out is None else dict(out)
-    o.setdefault("out_tokens", torch.empty((B, gamma + 1), dtype=torch.int32, device=dev))
-    o.setdefault("out_len", torch.empty((B,), dtype=torch.int32, device=dev))
-    if want_lse:
-        o.setdefault("target_lse", torch.empty((B, gamma + 1), dtype=torch.float32, device=dev))
-        o.setdefault("draft_lse", torch.empty((B, gamma), dtype=torch.float32, device=dev))
+    for name, shape, dt in (("out_tokens", (B, gamma + 1), torch.int32), ("out_len", (B,), torch.int32),
+                            ("target_lse", (B, gamma + 1), torch.float32), ("draft_lse", (B, gamma), torch.float32)):
+        if name not in o:
+            if dt is torch.int32 or want_lse:
+                o[name] = torch.empty(shape, dtype=dt, device=dev)
+        elif o[name].shape != shape or o[name].dtype != dt or not o[name].is_contiguous():
+            _refuse(f"{name}: contiguous {dt} {shape}")
     _check(_lib.psd_verify_given(ctypes.byref(params), B, gamma, _ptr(target_logits), _ptr(draft_logits), _ptr(draft_tokens),
                                  _ptr(n_drafts), _ptr(u), _ptr(e), _ptr(o["out_tokens"]), _ptr(o["out_len"]),
                                  _ptr(o.get("target_lse")), _ptr(o.get("draft_lse")), _ptr(ws), ws.numel(),
