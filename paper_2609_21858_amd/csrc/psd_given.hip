@@ -50,28 +50,58 @@ __device__ __forceinline__ float load_one(const void* base, int64_t element) {
         return ((const float*)base)[element];
 }
 
+// The last, incomplete 16 bytes of a row of floats or logits: n elements, `none` past them.
+template <bool BF16>
+__device__ __forceinline__ u32x4 load_tail(const void* base, int64_t element, int n, uint32_t none) {
+    u32x4 w;
+    if constexpr (BF16) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t lo = 2 * j < n ? ((const uint16_t*)base)[element + 2 * j] : none;
+            const uint32_t hi = 2 * j + 1 < n ? ((const uint16_t*)base)[element + 2 * j + 1] : none;
+            w[j] = lo | hi << 16;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = j < n ? ((const uint32_t*)base)[element + j] : none;
+    }
+    return w;
+}
+
+// Element j of 16 bytes.
+template <bool BF16>
+__device__ __forceinline__ float pick(const u32x4 w, int j) {
+    const int i = BF16 ? j >> 1 : j;
+    const uint32_t x = i < 2 ? (i == 0 ? w[0] : w[1]) : (i == 2 ? w[2] : w[3]);
+    if constexpr (BF16) return j & 1 ? word_hi(x) : word_lo(x);
+    return __uint_as_float(x);
+}
+
 struct Layout {
     size_t part, best, count, total;
     int rows, nseg, seg, rseg, rlen;  // stream segments per row and their length; race segments and theirs
+    int lanes;                        // log2 of the lanes that join a row's segments
 };
 
-// Segments: enough workgroups to fill the device several times over (2048), but at least
-// 2048 elements each, in multiples of a workgroup's 16-byte loads.
+// Segments: enough workgroups to fill the device (2048 for the rows, 1024 for the races, which
+// are resident together), but at least 16 bytes a thread.
 inline Layout layout(int B, int gamma, int V, bool bf16) {
     Layout L;
     const int grain = kThreads * (bf16 ? 8 : 4);
     L.rows = B * (2 * gamma + 1);
-    auto cut = [&](long rows, int* n, int* len) {
-        long want = std::min<long>(std::max<long>((2048 + rows - 1) / rows, 1), 64);
+    auto cut = [&](long rows, long fill, int* n, int* len) {
+        long want = std::min<long>(std::max<long>((fill + rows - 1) / rows, 1), 64);
         long l = ((V + want - 1) / want + grain - 1) / grain * grain;
         *len = (int)l;
         *n = (int)((V + l - 1) / l);
     };
-    cut(L.rows, &L.nseg, &L.seg);
-    cut(B, &L.rseg, &L.rlen);
+    cut(L.rows, 2048, &L.nseg, &L.seg);
+    cut(B, 1024, &L.rseg, &L.rlen);
+    L.lanes = 0;
+    while (1 << L.lanes < L.nseg) ++L.lanes;
     L.part = 0;
     L.best = align256((size_t)L.rows * L.nseg * 8);
-    L.count = align256(L.best + (size_t)B * 16);
+    L.count = align256(L.best + (size_t)B * 8);
     L.total = align256(L.count + (size_t)B * 4);
     return L;
 }
@@ -100,10 +130,10 @@ __global__ __launch_bounds__(kThreads) void given_stream_kernel(GivenArgs a, Lay
     const int lo = part * L.seg, hi = min(lo + L.seg, a.V);
     const int tid = threadIdx.x;
     char* ws = (char*)a.workspace;
-    if (part == 0 && tid < 2 && row < a.B) {
-        // the race's slots and counter of sequence `row`: written before its launch begins
-        ((unsigned long long*)(ws + L.best))[2 * row + tid] = kNone;
-        if (tid == 0) ((unsigned*)(ws + L.count))[row] = 0;
+    if (part == 0 && tid == 0 && row < a.B) {
+        // the race's slot and counter of sequence `row`: written before its launch begins
+        ((unsigned long long*)(ws + L.best))[row] = kNone;
+        ((unsigned*)(ws + L.count))[row] = 0;
     }
     float m = kNoLogit, s = 0.f;
     for (int v0 = lo + tid * VEC; v0 < hi; v0 += U * kThreads * VEC) {
@@ -153,13 +183,31 @@ __global__ __launch_bounds__(kThreads) void given_stream_kernel(GivenArgs a, Lay
 }
 
 constexpr int kMaxRows = 2 * 32 + 1;
+constexpr int kRaceUnroll = 2;  // 16-byte pieces of a row that a thread scores between two exchanges
+// Relative error assumed of a probability from the hardware's exponential: (l - max) / T up to
+// 100 in units of ln 2 errs by 100 2^-24 from the product, and a few 2^-24 from the rest.
+constexpr float kErr = 2e-5f;
+
+// Full-precision scores of tokens of the row that decides, as (score bits, token): scores
+// are positive, so their bits order them, and equal ones go to the lowest token.
+template <bool BF16>
+struct RaceRow {
+    const GivenArgs* a;
+    float top_p, sum_p, top_q, sum_q;
+    int64_t at_p, at_q, at_e;
+    __device__ float p(float l) const { return expf((l - top_p) / a->T_target) / sum_p; }
+    __device__ float q(float l) const { return sum_q > 0.f ? expf((l - top_q) / a->T_draft) / sum_q : 0.f; }
+    __device__ static unsigned long long key(float r, float e, int v) {
+        return r > 0.f ? (unsigned long long)__float_as_uint(e / r) << 32 | (unsigned)v : kNone;
+    }
+};
 
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void given_race_kernel(GivenArgs a, Layout L) {
+__global__ __launch_bounds__(kThreads, 4) void given_race_kernel(GivenArgs a, Layout L) {
     constexpr int VEC = Elem<BF16>::kVec;
     __shared__ float s_top[kMaxRows], s_sum[kMaxRows];
     __shared__ int s_taken;
-    __shared__ unsigned long long s_best[kWaves][2];
+    __shared__ unsigned long long s_best[kWaves];
     const int b = blockIdx.x / L.rseg, part = blockIdx.x - b * L.rseg;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int g = a.gamma;
@@ -167,46 +215,72 @@ __global__ __launch_bounds__(kThreads) void given_race_kernel(GivenArgs a, Layou
     char* ws = (char*)a.workspace;
     const float2* parts = (const float2*)(ws + L.part);
 
-    // every row of the sequence: rows [0, g] the target's, [g + 1, 2 g] the drafts'
-    for (int r = wave; r < 2 * g + 1; r += kWaves) {
+    // lane s of the first wave: draft s, its logits and its number, on their way while sums are joined
+    const int drafts = a.n_drafts ? min(max(a.n_drafts[b], 0), g) : g;
+    int x = -1;
+    float lt = 0.f, ld = 0.f, u = 0.f;
+    if (wave == 0 && lane < drafts) {
+        x = a.draft_tokens[(int64_t)b * g + lane];
+        u = a.u[(int64_t)b * g + lane];
+        if (x >= 0 && x < a.V) {
+            lt = load_one<BF16>(a.target, ((int64_t)b * (g + 1) + lane) * a.V + x);
+            ld = load_one<BF16>(a.draft, ((int64_t)b * g + lane) * a.V + x);
+        }
+    }
+
+    // the first pieces of e, which need nothing else
+    const int lo = part * L.rlen, hi = min(lo + L.rlen, a.V);
+    u32x4 we[kRaceUnroll][VEC / 4];
+    auto load_e = [&](int v0) {
+#pragma unroll
+        for (int k = 0; k < kRaceUnroll; ++k)
+#pragma unroll
+            for (int j = 0; j < VEC; j += 4) {
+                const int v = v0 + k * kThreads * VEC;
+                if (v + VEC <= hi)
+                    we[k][j / 4] = load_any<false>(a.e, (int64_t)b * a.V + v + j);
+                else
+                    we[k][j / 4] = load_tail<false>(a.e, (int64_t)b * a.V + v + j, hi - v - j, 0x3F800000u);
+            }
+    };
+    load_e(lo + tid * VEC);
+
+    // Every row of the sequence: rows [0, g] the target's, [g + 1, 2 g] the drafts'.  A row's segments
+    // lie on neighbouring lanes, 2^L.lanes of them.
+    const int row_lanes = 1 << L.lanes;
+    for (int r0 = 0; r0 < 2 * g + 1; r0 += kThreads >> L.lanes) {
+        const int r = r0 + (tid >> L.lanes), at = tid & (row_lanes - 1);
         const bool target = r <= g;
         const float T = target ? a.T_target : a.T_draft;
         const float c = kLog2e / T;
         const int64_t row = target ? (int64_t)b * (g + 1) + r : targets + (int64_t)b * g + (r - g - 1);
         float m = kNoLogit, s = 0.f;
-        if (lane < L.nseg) {
-            const float2 v = parts[row * L.nseg + lane];
+        if (r < 2 * g + 1 && at < L.nseg) {
+            const float2 v = parts[row * L.nseg + at];
             m = v.x;
             s = v.y;
         }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) merge(m, s, __shfl_xor(m, o), __shfl_xor(s, o), c);
-        if (lane == 0) {
+        for (int o = row_lanes / 2; o > 0; o >>= 1) merge(m, s, __shfl_xor(m, o), __shfl_xor(s, o), c);
+        if (at == 0 && r < 2 * g + 1) {
             s_top[r] = m == kNoLogit ? 0.f : m;
             s_sum[r] = m == kNoLogit ? 0.f : s;
             if (part == 0) {
                 float* out = target ? a.target_lse : a.draft_lse;
-                const int64_t at = target ? row : row - targets;
-                if (out) out[at] = m == kNoLogit ? kNoLogit : m / T + logf(s);
+                const int64_t to = target ? row : row - targets;
+                if (out) out[to] = m == kNoLogit ? kNoLogit : m / T + logf(s);
             }
         }
     }
     __syncthreads();
 
     // the first refusal
-    const int drafts = a.n_drafts ? min(max(a.n_drafts[b], 0), g) : g;
     if (wave == 0) {
         bool ok = false;
-        if (lane < drafts) {
-            const int x = a.draft_tokens[(int64_t)b * g + lane];
-            if (x >= 0 && x < a.V) {
-                const float lt = load_one<BF16>(a.target, ((int64_t)b * (g + 1) + lane) * a.V + x);
-                const float ld = load_one<BF16>(a.draft, ((int64_t)b * g + lane) * a.V + x);
-                const float sp = s_sum[lane], sq = s_sum[g + 1 + lane];
-                const float p = sp > 0.f ? expf((lt - s_top[lane]) / a.T_target) / sp : 0.f;
-                const float q = sq > 0.f ? expf((ld - s_top[g + 1 + lane]) / a.T_draft) / sq : 0.f;
-                ok = a.u[(int64_t)b * g + lane] * q < p;
-            }
+        if (x >= 0 && x < a.V) {
+            const float sp = s_sum[lane], sq = s_sum[g + 1 + lane];
+            const float p = sp > 0.f ? expf((lt - s_top[lane]) / a.T_target) / sp : 0.f;
+            const float q = sq > 0.f ? expf((ld - s_top[g + 1 + lane]) / a.T_draft) / sq : 0.f;
+            ok = u * q < p;
         }
         const unsigned long long refused = ~__ballot(ok);  // bit `drafts` is set: at most 32 drafts
         if (lane == 0) s_taken = __ffsll(refused) - 1;
@@ -215,82 +289,120 @@ __global__ __launch_bounds__(kThreads) void given_race_kernel(GivenArgs a, Layou
     const int taken = s_taken;
     const bool residual = taken < drafts;
 
-    // the race over row `taken`: the smallest e / max(p - q, 0), and the smallest e / p for a
-    // residual that is zero everywhere
-    const float top_p = s_top[taken], sum_p = s_sum[taken];
-    const float top_q = residual ? s_top[g + 1 + taken] : 0.f, sum_q = residual ? s_sum[g + 1 + taken] : 0.f;
-    const int64_t at_p = ((int64_t)b * (g + 1) + taken) * a.V;
-    const int64_t at_q = residual ? ((int64_t)b * g + taken) * a.V : 0;
-    const int64_t at_e = (int64_t)b * a.V;
-    const int lo = part * L.rlen, hi = min(lo + L.rlen, a.V);
-    unsigned long long best_r = kNone, best_p = kNone;
-    if (sum_p > 0.f) {
-        auto race = [&](int v, float lp, float lq, float e) {
-            const float p = expf((lp - top_p) / a.T_target) / sum_p;
-            const float q = sum_q > 0.f ? expf((lq - top_q) / a.T_draft) / sum_q : 0.f;
-            if (p > 0.f) best_p = min(best_p, (unsigned long long)__float_as_uint(e / p) << 32 | (unsigned)v);
-            const float r = p - q;
-            if (r > 0.f) best_r = min(best_r, (unsigned long long)__float_as_uint(e / r) << 32 | (unsigned)v);
+    // The race over one segment of row `taken`.  First every token's score from fast exponentials
+    // and reciprocals, as an interval: with both probabilities good to kErr of themselves,
+    // r is within kErr (p + q) of p - q.  Then only pieces with a lower bound that does not exceed
+    // the wave's smallest upper bound (one or two) are scored with full precision.
+    RaceRow<BF16> row;
+    row.a = &a;
+    row.top_p = s_top[taken];
+    row.sum_p = s_sum[taken];
+    row.top_q = residual ? s_top[g + 1 + taken] : 0.f;
+    row.sum_q = residual ? s_sum[g + 1 + taken] : 0.f;
+    row.at_p = ((int64_t)b * (g + 1) + taken) * a.V;
+    row.at_q = ((int64_t)b * g + min(taken, g - 1)) * a.V;
+    row.at_e = (int64_t)b * a.V;
+    unsigned long long best = kNone;
+    if (row.sum_p > 0.f) {
+        const bool use_q = row.sum_q > 0.f;
+        const float cp = kLog2e / a.T_target, cq = use_q ? kLog2e / a.T_draft : 0.f;
+        const float inv_p = 1.f / row.sum_p, inv_q = use_q ? 1.f / row.sum_q : 0.f;
+        // smallest lower and upper bounds so far; an upper bound needs r to be more than rounding
+        auto bounds = [&](float lp, float lq, float e, float& low, float& high) {
+            const float p = exp2_hw((lp - row.top_p) * cp) * inv_p;
+            const float q = use_q ? exp2_hw((lq - row.top_q) * cq) * inv_q : 0.f;
+            const float r = p - q, err = (p + q) * kErr;
+            const float down = e * __builtin_amdgcn_rcpf(r + err) * (1.f - kErr);
+            if (r + err > 0.f) low = fminf(low, down);
+            const float up = e * __builtin_amdgcn_rcpf(r - err) * (1.f + kErr);
+            if (r - err > 0.f) high = fminf(high, up);
         };
-        for (int v = lo + tid * VEC; v < hi; v += kThreads * VEC) {
-            float lp[VEC], lq[VEC], e[VEC];
-            if (v + VEC <= hi) {
-                const u32x4 wp = load_any<BF16>(a.target, at_p + v);
-                u32x4 wq = {0, 0, 0, 0};
-                if (residual) wq = load_any<BF16>(a.draft, at_q + v);
+        for (int v0 = lo + tid * VEC; v0 - tid * VEC < hi; v0 += kRaceUnroll * kThreads * VEC) {
+            float low[kRaceUnroll];  // of each piece: its smallest lower bound
+            float high = __builtin_inff();
+            u32x4 wp[kRaceUnroll], wq[kRaceUnroll];
 #pragma unroll
-                for (int j = 0; j < VEC; j += 4) {
-                    const u32x4 we = load_any<false>(a.e, at_e + v + j);
-                    Elem<false>::widen(we, e + j);
+            for (int k = 0; k < kRaceUnroll; ++k) {
+                const int v = v0 + k * kThreads * VEC;
+                wq[k] = u32x4{0, 0, 0, 0};
+                if (v + VEC <= hi) {
+                    wp[k] = load_any<BF16>(a.target, row.at_p + v);
+                    if (use_q) wq[k] = load_any<BF16>(a.draft, row.at_q + v);
+                } else {
+                    wp[k] = load_tail<BF16>(a.target, row.at_p + v, hi - v, BF16 ? 0xFF80u : 0xFF800000u);  // -inf
+                    if (use_q) wq[k] = load_tail<BF16>(a.draft, row.at_q + v, hi - v, 0);
                 }
-                Elem<BF16>::widen(wp, lp);
-                Elem<BF16>::widen(wq, lq);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) race(v + j, lp[j], lq[j], e[j]);
-            } else {
-                for (int j = 0; v + j < hi; ++j)
-                    race(v + j, load_one<BF16>(a.target, at_p + v + j),
-                         residual ? load_one<BF16>(a.draft, at_q + v + j) : 0.f, a.e[at_e + v + j]);
             }
+#pragma unroll
+            for (int k = 0; k < kRaceUnroll; ++k) {
+                float lp[VEC], lq[VEC], e[VEC];
+                Elem<BF16>::widen(wp[k], lp);
+                Elem<BF16>::widen(wq[k], lq);
+#pragma unroll
+                for (int j = 0; j < VEC; j += 4) Elem<false>::widen(we[k][j / 4], e + j);
+                low[k] = __builtin_inff();
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) bounds(lp[j], lq[j], e[j], low[k], high);
+                __builtin_amdgcn_sched_barrier(0);  // a piece's temporaries end here
+            }
+            // the wave's smallest upper bound: pieces whose tokens all lie above it have lost
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) high = fminf(high, __shfl_xor(high, o));
+            if (best != kNone) high = fminf(high, __uint_as_float((unsigned)(best >> 32)));
+#pragma unroll
+            for (int k = 0; k < kRaceUnroll; ++k)
+                if (low[k] <= high) {
+                    const int v = v0 + k * kThreads * VEC;
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        const float lp = pick<BF16>(wp[k], j), lq = pick<BF16>(wq[k], j);
+                        const float e = pick<false>(VEC == 8 && j >= 4 ? we[k][VEC / 4 - 1] : we[k][0], j & 3);
+                        float down = __builtin_inff(), up = high;
+                        bounds(lp, lq, e, down, up);
+                        if (down <= high && v + j < hi) best = min(best, row.key(row.p(lp) - row.q(lq), e, v + j));
+                    }
+                }
+            load_e(v0 + kRaceUnroll * kThreads * VEC);
         }
     }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        best_r = min(best_r, (unsigned long long)__shfl_xor((long long)best_r, o));
-        best_p = min(best_p, (unsigned long long)__shfl_xor((long long)best_p, o));
-    }
-    if (lane == 0) {
-        s_best[wave][0] = best_r;
-        s_best[wave][1] = best_p;
-    }
+    for (int o = 32; o > 0; o >>= 1) best = min(best, (unsigned long long)__shfl_xor((long long)best, o));
+    if (lane == 0) s_best[wave] = best;
     __syncthreads();
     __shared__ int s_last;
-    unsigned long long* slots = (unsigned long long*)(ws + L.best) + 2 * (int64_t)b;
+    unsigned long long* slot = (unsigned long long*)(ws + L.best) + b;
     if (tid == 0) {
-        for (int w = 1; w < kWaves; ++w) {
-            best_r = min(best_r, s_best[w][0]);
-            best_p = min(best_p, s_best[w][1]);
-        }
-        // minima do not depend on the order of the workgroups
-        __hip_atomic_fetch_min(&slots[0], best_r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_fetch_min(&slots[1], best_p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        const unsigned before = __hip_atomic_fetch_add((unsigned*)(ws + L.count) + b, 1u, __ATOMIC_ACQ_REL,
+        for (int w = 1; w < kWaves; ++w) best = min(best, s_best[w]);
+        // A minimum does not depend on the order of the workgroups.  Its returned value is waited for,
+        // so it has taken place when the count goes up: the workgroup that counts last reads
+        // the minimum of all.  Nothing else passes between them, and no fence is needed, which
+        // would empty the caches that the other workgroups stream through.
+        const unsigned long long was = __hip_atomic_fetch_min(slot, best, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("" ::"v"(was) : "memory");
+        const unsigned before = __hip_atomic_fetch_add((unsigned*)(ws + L.count) + b, 1u, __ATOMIC_RELAXED,
                                                        __HIP_MEMORY_SCOPE_AGENT);
         s_last = before == (unsigned)(L.rseg - 1);
     }
     __syncthreads();
-    if (!s_last || wave != 0) return;
-    if (lane <= g) {
-        const unsigned long long r = __hip_atomic_load(&slots[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        const unsigned long long p = __hip_atomic_load(&slots[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        const unsigned long long won = r != kNone ? r : p;
+    if (!s_last) return;
+    unsigned long long won = __hip_atomic_fetch_min(slot, kNone, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (won == kNone && residual && row.sum_p > 0.f) {
+        // a refusal with p <= q everywhere (rounding: two rows nearly the same): the race over p
+        for (int v = tid; v < a.V; v += kThreads) won = min(won, row.key(row.p(load_one<BF16>(a.target, row.at_p + v)), a.e[row.at_e + v], v));
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) won = min(won, (unsigned long long)__shfl_xor((long long)won, o));
+        if (lane == 0) s_best[wave] = won;
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) won = min(won, s_best[w]);
+    }
+    if (tid <= g) {
         int token = -1;
-        if (lane < taken)
-            token = a.draft_tokens[(int64_t)b * g + lane];
-        else if (lane == taken && won != kNone)
+        if (tid < taken)
+            token = a.draft_tokens[(int64_t)b * g + tid];
+        else if (tid == taken && won != kNone)
             token = (int)(unsigned)won;
-        a.out_tokens[(int64_t)b * (g + 1) + lane] = token;
-        if (lane == 0) a.out_len[b] = taken + 1;
+        a.out_tokens[(int64_t)b * (g + 1) + tid] = token;
+        if (tid == 0) a.out_len[b] = taken + 1;
     }
 }
 
