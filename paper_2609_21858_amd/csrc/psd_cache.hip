@@ -16,30 +16,64 @@ namespace psd {
 namespace {
 
 constexpr int kAppendThreads = 256;
+constexpr int kAppendRounds = 4;  // heads of a thread whose loads are in flight together
+
+// Where the pair partner of an element lies.
+enum Turn {
+    kNoTurn,       // R = 0
+    kInterleaved,  // in the same 16 bytes
+    kPieces,       // halves of whole 16-byte pieces: one other piece, read again (from the first-level cache)
+    kAnywhere,     // halves that cut a piece: through LDS
+};
+
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
 
 // One workgroup per packed row.  A head's 16-byte pieces lie on neighbouring lanes (GS of
-// them, a power of two at least D / VEC), and a thread takes the same piece of several heads,
-// so the row's cosines and sines are loaded once into registers.  The pair partner of an
-// element in the half-split order is in another lane: the normed head goes through LDS,
-// transposed so that neighbouring lanes hit neighbouring banks (any R, no alignment rule).
-template <bool BF16>
+// them, a power of two at least D / VEC, all of one wave), and a thread takes the same piece of
+// several heads, so the row's cosines and sines are loaded once into registers.  The row's
+// data sets out before its place is known, which takes three dependent loads.  q_out may be q:
+// a wave has read a head, partners included, before it writes it.
+template <bool BF16, Turn TURN>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, int GS) {
     using E = Elem<BF16>;
     constexpr int VEC = E::kVec;
-    __shared__ float s_x[VEC][kAppendThreads];
+    __shared__ float s_x[TURN == kAnywhere ? VEC : 1][kAppendThreads];
     const CacheArgs& c = a.c;
     const int t = blockIdx.x;
     const int tid = threadIdx.x;
+    const int half = a.R / 2;
+    const int lane = tid & (GS - 1), group = tid / GS, groups = kAppendThreads / GS;
+    const int d0 = lane * VEC;
+    const bool in_head = d0 < c.D;
+    const int dp = TURN == kPieces ? (d0 < half ? d0 + half : d0 - half) : 0;  // the partners' piece
+    const bool turns = TURN != kNoTurn && in_head && d0 < a.R;
+    const int slots = a.H + 2 * c.G;
+
+    u32x4 w[kAppendRounds], pw[kAppendRounds];
+    auto load = [&](int h0) {
+#pragma unroll
+        for (int k = 0; k < kAppendRounds; ++k) {
+            const int h = h0 + k * groups + group;
+            w[k] = pw[k] = u32x4{0, 0, 0, 0};
+            if (h < slots && in_head) {
+                const bool query = h < a.H, key = !query && h < a.H + c.G;
+                const RowsArgs& r = query ? a.q : key ? a.k : a.v;
+                const int head = query ? h : key ? h - a.H : h - a.H - c.G;
+                const char* src = (const char*)r.data + ((int64_t)t * r.stride_row + (int64_t)head * r.stride_head) * E::kBytes;
+                w[k] = *(const u32x4*)(src + d0 * E::kBytes);
+                if (TURN == kPieces && turns && (query || key)) pw[k] = *(const u32x4*)(src + dp * E::kBytes);
+            }
+        }
+    };
+    load(0);
+
     const int b = find_seq(c.new_start, c.B, t);
     if (b >= c.B) return;
     const Seq s = load_seq(c, b);
     const int i = t - s.row0;
     if (i < 0 || i >= s.n) return;
     const int pos = s.first + i;
-    const int half = a.R / 2;
-    const int lane = tid & (GS - 1), group = tid / GS, groups = kAppendThreads / GS;
-    const int d0 = lane * VEC;
-    const bool in_head = d0 < c.D;
 
     // the place in the cache, if the token has one
     int64_t at = -1;
@@ -52,93 +86,115 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, in
         }
     }
 
-    // cosine and signed sine of this thread's elements: y_d = x_d * cs + partner * sn
+    // cosine and signed sine of this thread's elements: y_d = x_d cs + partner sn
     float cs[VEC], sn[VEC];
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-        cs[j] = 1.f;
-        sn[j] = 0.f;
-    }
-    if (in_head && d0 < a.R) {
+    if (turns) {
         const int p = a.positions ? a.positions[t] : pos;
         const bool known = p >= 0 && p < a.positions_max;
         const int64_t base = (int64_t)(known ? p : 0) * half;
+        if constexpr (TURN == kPieces) {
+            const int r0 = d0 < half ? d0 : d0 - half;
+            const float sign = d0 < half ? -1.f : 1.f;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            const int d = d0 + j;
-            if (d < a.R) {
-                const int r = a.interleaved ? d / 2 : (d < half ? d : d - half);
-                const bool second = a.interleaved ? (d & 1) : d >= half;
-                const float cc = known ? a.cos[base + r] : __builtin_nanf("");
-                const float ss = known ? a.sin[base + r] : __builtin_nanf("");
-                cs[j] = cc;
-                sn[j] = second ? ss : -ss;
+            for (int j = 0; j < VEC; j += 4) {
+                const f32x4_any cc = *(const f32x4_any*)(a.cos + base + r0 + j), ss = *(const f32x4_any*)(a.sin + base + r0 + j);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    cs[j + e] = cc[e];
+                    sn[j + e] = ss[e] * sign;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const int d = d0 + j;
+                cs[j] = 1.f;
+                sn[j] = 0.f;
+                if (d < a.R) {
+                    const int r = TURN == kInterleaved ? d / 2 : d < half ? d : d - half;
+                    const bool second = TURN == kInterleaved ? (j & 1) : d >= half;
+                    cs[j] = a.cos[base + r];
+                    sn[j] = second ? a.sin[base + r] : -a.sin[base + r];
+                }
             }
         }
+        if (!known)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (d0 + j < a.R) cs[j] = __builtin_nanf("");
     }
 
-    const int slots = a.H + 2 * c.G;
-    // every group runs the same number of rounds: the shuffles and the LDS exchange stay
-    // within a group's lanes, all of one wave
-    for (int h0 = 0; h0 < slots; h0 += groups) {
-        const int h = h0 + group;
-        const bool on = h < slots && in_head;
-        const int kind = h < a.H ? 0 : h < a.H + c.G ? 1 : 2;  // query, key, value
-        const int head = kind == 0 ? h : kind == 1 ? h - a.H : h - a.H - c.G;
-        u32x4 w = {0, 0, 0, 0};
-        if (on) {
-            const RowsArgs& r = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
-            w = *(const u32x4*)((const char*)r.data + ((int64_t)t * r.stride_row + (int64_t)head * r.stride_head + d0) * E::kBytes);
-        }
-        float x[VEC];
-        E::widen(w, x);
-        const void* norm = kind == 0 ? a.q_norm : a.k_norm;
-        if (a.q_norm || a.k_norm) {
-            float sum = 0.f;
+    // every group runs the same rounds: exchanges stay within a group's lanes, all of one wave
+    for (int h0 = 0; h0 < slots; h0 += kAppendRounds * groups) {
+        if (h0 > 0) load(h0);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) sum += x[j] * x[j];
-            for (int o = GS / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-            if (on && kind != 2 && norm) {
-                const float scale = 1.f / sqrtf(sum / (float)c.D + a.eps);
-                float wt[VEC];
-                E::widen(*(const u32x4*)((const char*)norm + (int64_t)d0 * E::kBytes), wt);
+        for (int k = 0; k < kAppendRounds; ++k) {
+            if (h0 + k * groups >= slots) break;
+            const int h = h0 + k * groups + group;
+            const bool on = h < slots && in_head;
+            const bool query = h < a.H, key = !query && h < a.H + c.G;
+            const int head = query ? h : key ? h - a.H : h - a.H - c.G;
+            float x[VEC];
+            E::widen(w[k], x);
+            const void* norm = query ? a.q_norm : a.k_norm;
+            const bool normed = on && (query || key) && norm;
+            float scale = 1.f;
+            if (a.q_norm || a.k_norm) {
+                float sum = 0.f;
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) x[j] = x[j] * scale * wt[j];
+                for (int j = 0; j < VEC; ++j) sum += x[j] * x[j];
+                for (int o = GS / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+                if (normed) {
+                    scale = 1.f / sqrtf(sum / (float)c.D + a.eps);
+                    float wt[VEC];
+                    E::widen(*(const u32x4*)((const char*)norm + (int64_t)d0 * E::kBytes), wt);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) x[j] = x[j] * scale * wt[j];
+                }
             }
-        }
-        if (a.R > 0) {
-            float y[VEC];
-            if (a.interleaved) {
+            if constexpr (TURN == kInterleaved || TURN == kPieces) {
+                if (turns && (query || key)) {
+                    float y[VEC];
+                    if constexpr (TURN == kInterleaved) {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) y[j] = x[j ^ 1];
-            } else {
+                        for (int j = 0; j < VEC; ++j) y[j] = x[j ^ 1];
+                    } else {
+                        E::widen(pw[k], y);
+                        if (normed) {
+                            float wt[VEC];
+                            E::widen(*(const u32x4*)((const char*)norm + (int64_t)dp * E::kBytes), wt);
+#pragma unroll
+                            for (int j = 0; j < VEC; ++j) y[j] = y[j] * scale * wt[j];
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j)
+                        if (TURN == kPieces || d0 + j < a.R) x[j] = x[j] * cs[j] + y[j] * sn[j];
+                }
+            } else if constexpr (TURN == kAnywhere) {
+                // transposed, so that neighbouring lanes meet neighbouring banks
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) s_x[j][tid] = x[j];
-                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 __builtin_amdgcn_wave_barrier();
+                if (turns && (query || key)) {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const int d = d0 + j;
-                    const int p = d < half ? d + half : d - half;
-                    y[j] = d < a.R ? s_x[p % VEC][tid - lane + p / VEC] : 0.f;
+                    for (int j = 0; j < VEC; ++j) {
+                        const int d = d0 + j;
+                        const int p = d < half ? d + half : d - half;
+                        if (d < a.R) x[j] = x[j] * cs[j] + s_x[p % VEC][tid - lane + p / VEC] * sn[j];
+                    }
                 }
-                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 __builtin_amdgcn_wave_barrier();
             }
-            if (kind != 2 && d0 < a.R) {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j)
-                    if (d0 + j < a.R) x[j] = x[j] * cs[j] + y[j] * sn[j];
-            }
-        }
-        if (on) {
-            if (kind == 0) {
+            if (!on) continue;
+            if (query) {
                 *(u32x4*)((char*)a.q_out.data +
-                          ((int64_t)t * a.q_out.stride_row + (int64_t)head * a.q_out.stride_head + d0) * E::kBytes) =
-                    E::narrow(x);
+                          ((int64_t)t * a.q_out.stride_row + (int64_t)head * a.q_out.stride_head + d0) * E::kBytes) = E::narrow(x);
             } else if (at >= 0) {
-                char* pool = (char*)(kind == 1 ? c.k : c.v);
-                *(u32x4*)(pool + (at + (int64_t)head * c.stride_head + d0) * E::kBytes) = kind == 1 ? E::narrow(x) : w;
+                char* pool = (char*)(key ? c.k : c.v);
+                *(u32x4*)(pool + (at + (int64_t)head * c.stride_head + d0) * E::kBytes) = key ? E::narrow(x) : w[k];
             }
         }
     }
@@ -146,28 +202,29 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, in
 
 constexpr int kKeepThreads = 256;
 constexpr int kKeepBatch = 4;
+constexpr int kKeepPlaces = 64;
 
 // One thread moves one 16-byte column (keys or values, head, piece) of a sequence's kept
-// tokens in one layer.  Indices ascend strictly, so keep[i] >= i and the places still to be
-// read lie behind the places written so far: kKeepBatch tokens are read together, then written.
+// tokens in one layer.  The places of 64 tokens at a time are found by 64 threads together: the
+// chain of dependent loads is lengths and indices, page table, data.  Indices ascend strictly,
+// so keep[i] >= i and the places still to be read lie behind those written so far: kKeepBatch
+// tokens are read together, then written.
 __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KeepArgs a, int vec, int bytes) {
+    __shared__ int64_t s_from[kKeepPlaces], s_to[kKeepPlaces];
     const CacheArgs& c = a.c;
     const int pieces = c.D / vec;
     const int blocks = (2 * c.G * pieces + kKeepThreads - 1) / kKeepThreads;  // of one sequence and layer
     const int b = blockIdx.x / blocks, part = blockIdx.x - b * blocks;
     const int layer = blockIdx.y;
+    const int tid = threadIdx.x;
+    const int32_t* keep = a.keep + (int64_t)b * a.keep_stride;
+    int from = tid < min(kKeepPlaces, a.keep_width) ? keep[tid] : -1;
+    const int kept = a.n_keep[b];
     const Seq s = load_seq(c, b);
     const int total = max(c.new_start[b + 1] - max(c.new_start[b], 0), 0);
-    const int n = max(min(min(a.n_keep[b], a.keep_width), total), 0);
-    if (layer == 0 && part == 0 && threadIdx.x == 0 && a.kv_out) a.kv_out[b] = s.first + n;
-    const int col = part * kKeepThreads + threadIdx.x;
-    if (col >= 2 * c.G * pieces) return;
-    const bool value = col >= c.G * pieces;
-    const int rest = value ? col - c.G * pieces : col;
-    const int g = rest / pieces, d0 = (rest - g * pieces) * vec;
-    char* pool = (char*)(value ? c.v : c.k) + ((int64_t)layer * c.stride_layer + (int64_t)g * c.stride_head + d0) * bytes;
+    const int n = max(min(min(kept, a.keep_width), total), 0);
+    if (layer == 0 && part == 0 && tid == 0 && a.kv_out) a.kv_out[b] = s.first + n;
     const int32_t* table = c.table + (int64_t)b * c.table_stride;
-    const int32_t* keep = a.keep + (int64_t)b * a.keep_stride;
     auto place = [&](int i) -> int64_t {
         const int pos = s.first + i;
         if (i < 0 || i >= total || pos < 0 || pos >= c.max_kv) return -1;
@@ -177,21 +234,52 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KeepArgs a, int vec,
         if ((unsigned)page >= (unsigned)c.pages) return -1;
         return ((int64_t)page * c.stride_page + (int64_t)(pos - pi * c.P) * c.stride_token) * bytes;
     };
-    for (int i0 = 0; i0 < n; i0 += kKeepBatch) {
-        u32x4 w[kKeepBatch];
-        int64_t to[kKeepBatch];
-#pragma unroll
-        for (int j = 0; j < kKeepBatch; ++j) {
-            const int i = i0 + j;
-            const int from = i < n ? keep[i] : -1;
-            const int64_t src = from >= 0 && from != i ? place(from) : -1;
-            to[j] = src >= 0 ? place(i) : -1;
-            if (to[j] >= 0) w[j] = *(const u32x4*)(pool + src);
+    const int col = part * kKeepThreads + tid;
+    const bool on = col < 2 * c.G * pieces;
+    const bool value = col >= c.G * pieces;
+    const int rest = value ? col - c.G * pieces : col;
+    const int g = rest / pieces, d0 = (rest - g * pieces) * vec;
+    char* pool = (char*)(value ? c.v : c.k) + ((int64_t)layer * c.stride_layer + (int64_t)g * c.stride_head + d0) * bytes;
+    for (int i0 = 0; i0 < n; i0 += kKeepPlaces) {
+        if (i0 > 0) {
+            __syncthreads();
+            from = tid < min(kKeepPlaces, n - i0) ? keep[i0 + tid] : -1;
         }
+        if (tid < kKeepPlaces) {
+            const int i = i0 + tid;
+            const int64_t src = i < n && from != i ? place(from) : -1, dst = i < n ? place(i) : -1;
+            s_from[tid] = src;
+            s_to[tid] = src >= 0 ? dst : -1;
+        }
+        __syncthreads();
+        const int m = min(kKeepPlaces, n - i0);
+        if (!on) continue;
+        for (int j0 = 0; j0 < m; j0 += kKeepBatch) {
+            u32x4 w[kKeepBatch];
+            int64_t to[kKeepBatch];
 #pragma unroll
-        for (int j = 0; j < kKeepBatch; ++j)
-            if (to[j] >= 0) *(u32x4*)(pool + to[j]) = w[j];
+            for (int j = 0; j < kKeepBatch; ++j) {
+                to[j] = j0 + j < m ? s_to[j0 + j] : -1;
+                if (to[j] >= 0) w[j] = *(const u32x4*)(pool + s_from[j0 + j]);
+            }
+#pragma unroll
+            for (int j = 0; j < kKeepBatch; ++j)
+                if (to[j] >= 0) *(u32x4*)(pool + to[j]) = w[j];
+        }
     }
+}
+
+template <bool BF16>
+void append(const AppendArgs& a, int gs, hipStream_t stream) {
+    const dim3 grid(a.c.rows), block(kAppendThreads);
+    if (a.R == 0)
+        hipLaunchKernelGGL((append_kernel<BF16, kNoTurn>), grid, block, 0, stream, a, gs);
+    else if (a.interleaved)
+        hipLaunchKernelGGL((append_kernel<BF16, kInterleaved>), grid, block, 0, stream, a, gs);
+    else if (a.R / 2 % Elem<BF16>::kVec == 0)
+        hipLaunchKernelGGL((append_kernel<BF16, kPieces>), grid, block, 0, stream, a, gs);
+    else
+        hipLaunchKernelGGL((append_kernel<BF16, kAnywhere>), grid, block, 0, stream, a, gs);
 }
 
 }  // namespace
@@ -200,9 +288,9 @@ hipError_t launch_kv_append(const AppendArgs& a, bool bf16, hipStream_t stream) 
     int gs = 1;
     while (gs * (bf16 ? 8 : 4) < a.c.D) gs *= 2;
     if (bf16)
-        hipLaunchKernelGGL(append_kernel<true>, dim3(a.c.rows), dim3(kAppendThreads), 0, stream, a, gs);
+        append<true>(a, gs, stream);
     else
-        hipLaunchKernelGGL(append_kernel<false>, dim3(a.c.rows), dim3(kAppendThreads), 0, stream, a, gs);
+        append<false>(a, gs, stream);
     return hipGetLastError();
 }
 
