@@ -16,7 +16,6 @@ namespace psd {
 namespace {
 
 constexpr int kAppendThreads = 256;
-constexpr int kAppendRounds = 4;  // heads of a thread whose loads are in flight together
 
 // Where the pair partner of an element lies.
 enum Turn {
@@ -27,46 +26,53 @@ enum Turn {
 };
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
 
-// One workgroup per packed row.  A head's 16-byte pieces lie on neighbouring lanes (GS of
+// One piece of N heads at once.
+template <int N>
+struct Heads {
+    u32x4 own[N], other[N];  // this thread's piece, and its partners' (kPieces)
+};
+
+// A packed row per 64 or 256 threads.  A head's 16-byte pieces lie on neighbouring lanes (GS of
 // them, a power of two at least D / VEC, all of one wave), and a thread takes the same piece of
-// several heads, so the row's cosines and sines are loaded once into registers.  The row's
-// data sets out before its place is known, which takes three dependent loads.  q_out may be q:
-// a wave has read a head, partners included, before it writes it.
+// several heads.  What a row needs once per piece stays in registers: with A = weight cos and
+// B = partner's weight sin,
+//   y_d = (x_d A_d + x_partner B_d) / sqrt(mean(x^2) + eps).
+// The row's data sets out before its place is known, which takes three dependent loads.  q_out may
+// be q: a wave has read a head, partners included, before it writes it.
 template <bool BF16, Turn TURN>
-__global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, int GS) {
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, int GS, int row_threads) {
     using E = Elem<BF16>;
     constexpr int VEC = E::kVec;
+    constexpr int NQ = 4, NK = 2;  // heads of a thread whose loads are in flight together: queries; keys, values
     __shared__ float s_x[TURN == kAnywhere ? VEC : 1][kAppendThreads];
     const CacheArgs& c = a.c;
-    const int t = blockIdx.x;
     const int tid = threadIdx.x;
+    const int t = __builtin_amdgcn_readfirstlane(blockIdx.x * (kAppendThreads / row_threads) + tid / row_threads);
+    if (t >= c.rows) return;
     const int half = a.R / 2;
-    const int lane = tid & (GS - 1), group = tid / GS, groups = kAppendThreads / GS;
+    const int lane = tid & (GS - 1), group = (tid & (row_threads - 1)) / GS, groups = row_threads / GS;
     const int d0 = lane * VEC;
     const bool in_head = d0 < c.D;
-    const int dp = TURN == kPieces ? (d0 < half ? d0 + half : d0 - half) : 0;  // the partners' piece
     const bool turns = TURN != kNoTurn && in_head && d0 < a.R;
-    const int slots = a.H + 2 * c.G;
+    const int dp = TURN == kPieces && turns ? (d0 < half ? d0 + half : d0 - half) : d0;
 
-    u32x4 w[kAppendRounds], pw[kAppendRounds];
-    auto load = [&](int h0) {
+    // heads h0, h0 + groups, ...: clamped, so that loads are unconditional
+    auto load = [&](auto& w, const RowsArgs& r, int heads, int h0, bool pairs) {
+        const char* src = (const char*)r.data + (int64_t)t * r.stride_row * E::kBytes;
+        constexpr int N = sizeof(w.own) / sizeof(w.own[0]);
 #pragma unroll
-        for (int k = 0; k < kAppendRounds; ++k) {
-            const int h = h0 + k * groups + group;
-            w[k] = pw[k] = u32x4{0, 0, 0, 0};
-            if (h < slots && in_head) {
-                const bool query = h < a.H, key = !query && h < a.H + c.G;
-                const RowsArgs& r = query ? a.q : key ? a.k : a.v;
-                const int head = query ? h : key ? h - a.H : h - a.H - c.G;
-                const char* src = (const char*)r.data + ((int64_t)t * r.stride_row + (int64_t)head * r.stride_head) * E::kBytes;
-                w[k] = *(const u32x4*)(src + d0 * E::kBytes);
-                if (TURN == kPieces && turns && (query || key)) pw[k] = *(const u32x4*)(src + dp * E::kBytes);
-            }
+        for (int k = 0; k < N; ++k) {
+            const char* at = src + (int64_t)min(h0 + k * groups, heads - 1) * r.stride_head * E::kBytes;
+            w.own[k] = *(const u32x4*)(at + min(d0, c.D - VEC) * E::kBytes);
+            if (TURN == kPieces && pairs) w.other[k] = *(const u32x4*)(at + min(dp, c.D - VEC) * E::kBytes);
         }
     };
-    load(0);
+    Heads<NQ> wq;
+    Heads<NK> wk, wv;
+    if (a.H > 0) load(wq, a.q, a.H, group, true);
+    load(wk, a.k, c.G, group, true);
+    load(wv, a.v, c.G, group, false);
 
     const int b = find_seq(c.new_start, c.B, t);
     if (b >= c.B) return;
@@ -86,8 +92,13 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, in
         }
     }
 
-    // cosine and signed sine of this thread's elements: y_d = x_d cs + partner sn
+    // cosines and signed sines of this thread's elements
     float cs[VEC], sn[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        cs[j] = 1.f;
+        sn[j] = 0.f;
+    }
     if (turns) {
         const int p = a.positions ? a.positions[t] : pos;
         const bool known = p >= 0 && p < a.positions_max;
@@ -108,8 +119,6 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, in
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 const int d = d0 + j;
-                cs[j] = 1.f;
-                sn[j] = 0.f;
                 if (d < a.R) {
                     const int r = TURN == kInterleaved ? d / 2 : d < half ? d : d - half;
                     const bool second = TURN == kInterleaved ? (j & 1) : d >= half;
@@ -124,78 +133,101 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, in
                 if (d0 + j < a.R) cs[j] = __builtin_nanf("");
     }
 
-    // every group runs the same rounds: exchanges stay within a group's lanes, all of one wave
-    for (int h0 = 0; h0 < slots; h0 += kAppendRounds * groups) {
-        if (h0 > 0) load(h0);
+    const float inv_d = 1.f / (float)c.D;
+    // queries or keys: `pool` at `to` (no place: nothing is written)
+    auto turn = [&](auto& w, const RowsArgs& r, int heads, const void* norm, char* to, int64_t stride) {
+        constexpr int N = sizeof(w.own) / sizeof(w.own[0]);
+        float A[VEC], B[VEC];
 #pragma unroll
-        for (int k = 0; k < kAppendRounds; ++k) {
-            if (h0 + k * groups >= slots) break;
-            const int h = h0 + k * groups + group;
-            const bool on = h < slots && in_head;
-            const bool query = h < a.H, key = !query && h < a.H + c.G;
-            const int head = query ? h : key ? h - a.H : h - a.H - c.G;
-            float x[VEC];
-            E::widen(w[k], x);
-            const void* norm = query ? a.q_norm : a.k_norm;
-            const bool normed = on && (query || key) && norm;
-            float scale = 1.f;
-            if (a.q_norm || a.k_norm) {
-                float sum = 0.f;
+        for (int j = 0; j < VEC; ++j) {
+            A[j] = cs[j];
+            B[j] = sn[j];
+        }
+        if (norm && in_head) {
+            float wt[VEC];
+            E::widen(*(const u32x4*)((const char*)norm + (int64_t)d0 * E::kBytes), wt);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) sum += x[j] * x[j];
-                for (int o = GS / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-                if (normed) {
-                    scale = 1.f / sqrtf(sum / (float)c.D + a.eps);
-                    float wt[VEC];
-                    E::widen(*(const u32x4*)((const char*)norm + (int64_t)d0 * E::kBytes), wt);
+            for (int j = 0; j < VEC; ++j) A[j] *= wt[j];
+            if constexpr (TURN == kPieces) {
+                float wp[VEC];
+                E::widen(*(const u32x4*)((const char*)norm + (int64_t)dp * E::kBytes), wp);
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) x[j] = x[j] * scale * wt[j];
+                for (int j = 0; j < VEC; ++j) B[j] *= wp[j];
+            } else if constexpr (TURN == kInterleaved) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) B[j] *= wt[j ^ 1];
+            } else if constexpr (TURN == kAnywhere) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const int d = d0 + j;
+                    if (d < a.R) {
+                        const int p = d < half ? d + half : d - half;
+                        if constexpr (BF16)
+                            B[j] *= __uint_as_float((uint32_t)((const uint16_t*)norm)[p] << 16);
+                        else
+                            B[j] *= ((const float*)norm)[p];
+                    }
                 }
             }
-            if constexpr (TURN == kInterleaved || TURN == kPieces) {
-                if (turns && (query || key)) {
-                    float y[VEC];
-                    if constexpr (TURN == kInterleaved) {
+        }
+        // every group runs the same rounds: exchanges stay within a group's lanes, all of one wave
+        for (int h0 = 0; h0 < heads; h0 += N * groups) {
+            if (h0 > 0) load(w, r, heads, h0 + group, true);
 #pragma unroll
-                        for (int j = 0; j < VEC; ++j) y[j] = x[j ^ 1];
-                    } else {
-                        E::widen(pw[k], y);
-                        if (normed) {
-                            float wt[VEC];
-                            E::widen(*(const u32x4*)((const char*)norm + (int64_t)dp * E::kBytes), wt);
+            for (int k = 0; k < N; ++k) {
+                if (h0 + k * groups >= heads) break;
+                const int h = h0 + k * groups + group;
+                float x[VEC], y[VEC];
+                E::widen(w.own[k], x);
+                float scale = 1.f;
+                if (norm) {
+                    float sum = 0.f;
 #pragma unroll
-                            for (int j = 0; j < VEC; ++j) y[j] = y[j] * scale * wt[j];
-                        }
-                    }
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j)
-                        if (TURN == kPieces || d0 + j < a.R) x[j] = x[j] * cs[j] + y[j] * sn[j];
+                    for (int j = 0; j < VEC; ++j) sum += x[j] * x[j];
+                    if (!in_head) sum = 0.f;
+                    for (int o = GS / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+                    scale = rsqrtf(sum * inv_d + a.eps);
                 }
-            } else if constexpr (TURN == kAnywhere) {
-                // transposed, so that neighbouring lanes meet neighbouring banks
+                if constexpr (TURN == kPieces) {
+                    E::widen(w.other[k], y);
+                } else if constexpr (TURN == kInterleaved) {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) s_x[j][tid] = x[j];
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                if (turns && (query || key)) {
+                    for (int j = 0; j < VEC; ++j) y[j] = x[j ^ 1];
+                } else if constexpr (TURN == kAnywhere) {
+                    // transposed, so that neighbouring lanes meet neighbouring banks
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) s_x[j][tid] = x[j];
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) {
                         const int d = d0 + j;
                         const int p = d < half ? d + half : d - half;
-                        if (d < a.R) x[j] = x[j] * cs[j] + s_x[p % VEC][tid - lane + p / VEC] * sn[j];
+                        y[j] = d < a.R ? s_x[p % VEC][tid - lane + p / VEC] : 0.f;
                     }
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
                 }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    float v = x[j] * A[j];
+                    if (TURN != kNoTurn && turns && (TURN == kPieces || d0 + j < a.R)) v += y[j] * B[j];
+                    x[j] = norm ? v * scale : v;
+                }
+                if (in_head && h < heads && to) *(u32x4*)(to + ((int64_t)h * stride + d0) * E::kBytes) = E::narrow(x);
             }
-            if (!on) continue;
-            if (query) {
-                *(u32x4*)((char*)a.q_out.data +
-                          ((int64_t)t * a.q_out.stride_row + (int64_t)head * a.q_out.stride_head + d0) * E::kBytes) = E::narrow(x);
-            } else if (at >= 0) {
-                char* pool = (char*)(key ? c.k : c.v);
-                *(u32x4*)(pool + (at + (int64_t)head * c.stride_head + d0) * E::kBytes) = key ? E::narrow(x) : w[k];
-            }
+        }
+    };
+    if (a.H > 0)
+        turn(wq, a.q, a.H, a.q_norm, (char*)a.q_out.data + (int64_t)t * a.q_out.stride_row * E::kBytes, a.q_out.stride_head);
+    turn(wk, a.k, c.G, a.k_norm, at >= 0 ? (char*)c.k + at * E::kBytes : nullptr, c.stride_head);
+    if (at < 0) return;
+    for (int h0 = 0; h0 < c.G; h0 += NK * groups) {
+        if (h0 > 0) load(wv, a.v, c.G, h0 + group, false);
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+            const int h = h0 + k * groups + group;
+            if (in_head && h < c.G) *(u32x4*)((char*)c.v + (at + (int64_t)h * c.stride_head + d0) * E::kBytes) = wv.own[k];
         }
     }
 }
@@ -269,17 +301,23 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KeepArgs a, int vec,
     }
 }
 
+constexpr int kWaveRows = 2048;
+
 template <bool BF16>
 void append(const AppendArgs& a, int gs, hipStream_t stream) {
-    const dim3 grid(a.c.rows), block(kAppendThreads);
+    // A wave a row has the less to set up, a workgroup a row the shorter chain: from 2048 rows on (eight
+    // waves for each CU) the device is full of waves.
+    const int row_threads = a.c.rows >= kWaveRows ? 64 : kAppendThreads;
+    const int per = kAppendThreads / row_threads;
+    const dim3 grid((a.c.rows + per - 1) / per), block(kAppendThreads);
     if (a.R == 0)
-        hipLaunchKernelGGL((append_kernel<BF16, kNoTurn>), grid, block, 0, stream, a, gs);
+        hipLaunchKernelGGL((append_kernel<BF16, kNoTurn>), grid, block, 0, stream, a, gs, row_threads);
     else if (a.interleaved)
-        hipLaunchKernelGGL((append_kernel<BF16, kInterleaved>), grid, block, 0, stream, a, gs);
+        hipLaunchKernelGGL((append_kernel<BF16, kInterleaved>), grid, block, 0, stream, a, gs, row_threads);
     else if (a.R / 2 % Elem<BF16>::kVec == 0)
-        hipLaunchKernelGGL((append_kernel<BF16, kPieces>), grid, block, 0, stream, a, gs);
+        hipLaunchKernelGGL((append_kernel<BF16, kPieces>), grid, block, 0, stream, a, gs, row_threads);
     else
-        hipLaunchKernelGGL((append_kernel<BF16, kAnywhere>), grid, block, 0, stream, a, gs);
+        hipLaunchKernelGGL((append_kernel<BF16, kAnywhere>), grid, block, 0, stream, a, gs, row_threads);
 }
 
 }  // namespace
