@@ -477,8 +477,9 @@ psd_status psd_kv_append(const psd_cache *cache, const psd_seqs *seqs, const psd
  *   lse        device [T][H] float32, nullable
  *   mask       device [T][mask_words] uint32, nullable
  *   workspace  device, psd_attention_workspace_bytes() for this cache, seqs and H, 256-byte
- *              aligned; may be NULL when that is 0.  Nothing in it needs clearing, and
- *              nothing in it outlives the call.
+ *              aligned; may be NULL when that is 0.  Zero-filled before its first use
+ *              (psd_workspace_clear) and again after a launch that did not run to completion;
+ *              each call leaves it ready for the next, of any shape.  One call at a time.
  * Products of bfloat16 values are summed in float32, and softmax weights are rounded to
  * bfloat16 for the product with the values; float32 inputs are computed in float32. */
 psd_status psd_attention(const psd_cache *cache, const psd_seqs *seqs, const psd_rows *q, int32_t q_heads, float scale,

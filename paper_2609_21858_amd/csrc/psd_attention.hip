@@ -45,10 +45,16 @@ struct Plan {
     int h;          // rows per new token: H / G
     int tile_rows;  // rows of a workgroup
     int tiles;      // row tiles of the longest sequence
-    int parts;      // parts of the longest range of cached tokens
-    int chunk;      // cached tokens of a part
+    int wgs;        // few rows: workgroups of each key/value head
+    int parts;      // many rows: parts of the longest range of cached tokens
+    int chunk;      // many rows: cached tokens of a part
     int page_shift; // log2 of the page size, or -1
 };
+
+// The workspace: a counter for each workgroup of the few-row kernel (zero between calls), then
+// what workgroups leave for the join.
+constexpr int kCounters = 1024;
+constexpr int kCounterFloats = kCounters;
 
 struct Range {
     int lo, hi;  // cached positions that some row of a tile sees
@@ -130,15 +136,29 @@ struct Weights {
     }
 };
 
+// 16 bytes of the cache.  One workgroup reads a bfloat16 key or value for all its rows, once: it need
+// not stay in a cache (6.3 -> 7.0 TB/s of a plain read).  Float32 rows may be several tiles.
+template <bool BF16>
+__device__ __forceinline__ u32x4 stream_load(const char* at) {
+    if constexpr (BF16) return __builtin_nontemporal_load((const u32x4*)at);
+    return *(const u32x4*)at;
+}
+
 // ---------------------------------------------------------------- few rows
 
-// One workgroup: up to 16 RB rows of one (sequence, key/value head) over one part of its cache.
-// Its waves take blocks of TOK tokens in turn, each with a softmax of its own, joined at the
+// Up to 16 RB rows of one (sequence, key/value head) over a stretch of its cache.  The waves of
+// a workgroup take blocks of TOK tokens in turn, each with a softmax of its own, joined at the
 // end; no wave waits for another in between.  Keys go from memory straight into the A operand
 // (a lane's 16 bytes are consecutive dimensions of one token); values pass through the wave's own
 // LDS, where bfloat16 is transposed by ds_read_b64_tr_b16 (16 lanes read a 4-token by 16-dimension
 // tile and each gets one dimension's 4 tokens).  While a block is computed, the next one's
 // keys and values are on their way into registers.
+//
+// Lengths are known on the device alone, so the device divides the work: an item is a row tile of a
+// sequence, its length the 128-token units it sees, and each of a head's R workgroups (resident
+// together) takes an equal stretch of all items' W units in a row.  An item
+// inside one workgroup's stretch is finished by it; of an item that is cut, every workgroup leaves its
+// output, maximum and sum in the workspace, and the one that leaves last joins them.
 template <bool BF16, int DP>
 struct StreamShape {
     static constexpr int TOK = BF16 ? 32 : 16;
@@ -155,42 +175,141 @@ struct StreamShape {
     static constexpr int V_BYTES = TOK * PITCH * (BF16 ? 2 : 4);
 };
 
+// The waves' values; at an item's end, their outputs (rows of DP + 4 floats: the 16 rows of a store
+// fall on different banks).
 template <bool BF16, int DP, int RB>
 constexpr int stream_lds() {
     using S = StreamShape<BF16, DP>;
     constexpr int values = kWaves * S::V_BYTES;
-    constexpr int join = 2 * 16 * RB * DP * 4;
+    constexpr int join = kWaves * 16 * RB * (DP + 4) * 4;
     return values > join ? values : join;
 }
 
-template <bool BF16, int DP, int RB>
+constexpr int kUnit = 128;  // cached tokens: a block of each wave (two in float32)
+// Units that a workgroup has at least, if it has to join: leaving and joining the parts of an item
+// takes as long as about so many (float32 rows are bound by their products).
+template <bool BF16, int RB>
+constexpr int join_units() {
+    return BF16 ? 4 : RB == 1 ? 2 : 1;
+}
+
+// Values that are the same in all lanes, into scalar registers.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ Seq uniform(const Seq& s) {
+    return Seq{uniform(s.row0), uniform(s.n), uniform(s.first), uniform(s.kv)};
+}
+
+// A value anew, so that what rare code computes from it is not kept in registers through the common.
+__device__ __forceinline__ int again(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// Units of one item, row tile `tile` of a sequence; 0 without rows, and at least 1 with them.
+__device__ __forceinline__ int item_units(const AttentionArgs& a, const Plan& p, const Seq& s, int tile) {
+    const int row0 = tile * p.tile_rows;
+    const int rows = min(s.n * p.h - row0, p.tile_rows);
+    if (rows <= 0) return 0;
+    const Range range = tile_range(a, s, row0 / p.h, (row0 + rows - 1) / p.h);
+    return max((range.hi - range.lo + kUnit - 1) / kUnit, 1);
+}
+
+// What workgroups leave for each other: written through and read past the caches that are not
+// shared (relaxed accesses of agent scope), so that no fence has to empty those.
+__device__ __forceinline__ void leave2(float* at, float x, float y) {
+    const uint64_t w = (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x);
+    __hip_atomic_store((uint64_t*)at, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 fetch2(const float* at) {
+    const uint64_t w = __hip_atomic_load((const uint64_t*)at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
+}
+
+template <bool BF16, int DP, int RB, bool FULL>
 __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) void stream_kernel(AttentionArgs a, Plan p) {
     using S = StreamShape<BF16, DP>;
     using E = Elem<BF16>;
     constexpr int DB = DP / 16;
+    constexpr int ROWS = 16 * RB;
     __shared__ __align__(16) char s_mem[stream_lds<BF16, DP, RB>()];
     __shared__ int64_t s_off[kWaves][2][S::TOK];
-    __shared__ float s_m[kWaves][16 * RB], s_l[kWaves][16 * RB];
+    __shared__ float s_m[kWaves][ROWS], s_l[kWaves][ROWS], s_top[ROWS], s_sum[ROWS];
+    __shared__ int s_units[kThreads + 1], s_wave[kWaves], s_longest[kWaves];
+    __shared__ Seq s_seq[kThreads];  // of the items, while there are no more than threads
+    __shared__ int s_chunk, s_last;
 
     const CacheArgs& c = a.c;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int r = lane & 15, q = lane >> 4;
-    int x = blockIdx.x;
-    const int g = x % c.G;
-    x /= c.G;
-    const int tile = x % p.tiles;
-    x /= p.tiles;
-    const int b = x % c.B, part = x / c.B;
+    const int g = blockIdx.x % c.G, wg = blockIdx.x / c.G;
 
-    const Seq s = load_seq(c, b);
+    // units before each thread's items, by a scan over the workgroup
+    const int items = c.B * p.tiles;
+    const int each = (items + kThreads - 1) / kThreads;
+    auto seq_at = [&](int i) { return load_seq(c, i / p.tiles); };
+    auto units_at = [&](int i, const Seq& s) { return item_units(a, p, s, i % p.tiles); };
+    int mine = 0, longest = 0;
+    for (int i = tid * each; i < min((tid + 1) * each, items); ++i) {
+        const Seq s = seq_at(i);
+        const int n = units_at(i, s);
+        s_seq[tid] = s;
+        mine += n;
+        longest = max(longest, n);
+    }
+    int upto = mine;
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+        const int below = __shfl_up(upto, k);
+        if (lane >= k) upto += below;
+        longest = max(longest, __shfl_xor(longest, k));
+    }
+    if (lane == 63) {
+        s_wave[wave] = upto;
+        s_longest[wave] = longest;
+    }
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) upto += s_wave[w];
+        longest = max(longest, s_longest[w]);
+    }
+    s_units[tid + 1] = upto;
+    if (tid == 0) s_units[0] = 0;
+    __syncthreads();
+    const int units = uniform(s_units[kThreads]);
+    // R workgroups: the first W mod R have W / R + 1 units.  While no item is much longer than that,
+    // each workgroup takes one item whole and none is joined.
+    constexpr int kMinUnits = join_units<BF16, RB>();
+    const int wgs = min(p.wgs, max(units / kMinUnits, 1));
+    const int share = units / wgs, more = units - share * wgs;
+    const bool whole_items = each == 1 && items <= p.wgs && uniform(longest) <= units / p.wgs + 1 + kMinUnits;
+    auto start = [&](int w) { return whole_items ? s_units[min(w, items)] : w * share + min(w, more); };
+    auto owner = [&](int u) { return u < more * (share + 1) ? u / (share + 1) : more + (u - more * (share + 1)) / share; };
+    if (wg >= (whole_items ? items : wgs)) return;
+    const int u0 = uniform(start(wg)), u1 = uniform(start(wg + 1));  // this workgroup's
+    if (u0 == u1) return;
+    if (s_units[tid] <= u0 && u0 < s_units[tid + 1]) s_chunk = tid;
+    __syncthreads();
+    const int chunk = uniform(s_chunk);
+    int item = chunk * each, before = uniform(s_units[chunk]);
+    constexpr int kSlot = ROWS * DP + 2 * ROWS;  // floats of what a workgroup leaves of an item
+    auto slot_of = [&](int w, int second) {
+        return (float*)a.workspace + kCounterFloats + (((int64_t)w * c.G + g) * 2 + second) * kSlot;
+    };
+    const float sc = a.scale * kLog2e;
+    const int64_t head_at = (int64_t)g * c.stride_head;
+    char* s_v = s_mem + wave * S::V_BYTES;
+
+    for (int n_units; before < u1; before += n_units, ++item) {
+    const Seq s = uniform(each == 1 ? s_seq[item] : seq_at(item));
+    n_units = each == 1 ? uniform(s_units[item + 1]) - before : uniform(units_at(item, s));
+    if (before + n_units <= u0) continue;
+    const int b = item / p.tiles, tile = item - b * p.tiles;
     const int row0 = tile * p.tile_rows;
     const int rows = min(s.n * p.h - row0, p.tile_rows);
-    if (rows <= 0) return;
-    const int i_lo = row0 / p.h, i_hi = (row0 + rows - 1) / p.h;
+    const int i_lo = uniform(row0 / p.h), i_hi = uniform((row0 + rows - 1) / p.h);
     const Range range = tile_range(a, s, i_lo, i_hi);
-    const int n_parts = max((range.hi - range.lo + p.chunk - 1) / p.chunk, 1);
-    if (part >= n_parts) return;
-    const int c0 = range.lo + part * p.chunk, c1 = min(c0 + p.chunk, range.hi);
+    const int from = max(u0, before), to = min(u1, before + n_units);
+    const int c0 = range.lo + (from - before) * kUnit, c1 = min(range.lo + (to - before) * kUnit, range.hi);
     const int blocks = (c1 - c0 + S::TOK - 1) / S::TOK;
     const int32_t* table = c.table + (int64_t)b * c.table_stride;
 
@@ -221,19 +340,24 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
 #pragma unroll
         for (int db = 0; db < DB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const float sc = a.scale * kLog2e;
-    const int64_t head_at = (int64_t)g * c.stride_head;
-    char* s_v = s_mem + wave * S::V_BYTES;
-
-    // A block's tokens: lane t < TOK finds token t's place; -1: nothing there.
-    auto locate = [&](int blk) -> int64_t {
-        const int j = c0 + blk * S::TOK + lane;
-        if (lane >= S::TOK || blk >= blocks || j >= c1) return -1;
-        return token_offset(c, p, table, j);
+    // A block's tokens: lane t < TOK finds token t's place; -1: nothing there.  The page number is loaded
+    // a block before it is used, so that no load in between has to be waited for with it.
+    auto token_of = [&](int blk) { return c0 + blk * S::TOK + lane; };
+    auto page_of = [&](int blk) {
+        const int j = token_of(blk);
+        const int at = lane < S::TOK && j < c1 ? j : 0;
+        return table[p.page_shift >= 0 ? at >> p.page_shift : at / c.P];
+    };
+    auto place = [&](int blk, int page) -> int64_t {
+        const int j = token_of(blk);
+        const int pi = p.page_shift >= 0 ? j >> p.page_shift : j / c.P;
+        if (lane >= S::TOK || j >= c1 || (unsigned)page >= (unsigned)c.pages) return -1;
+        return (int64_t)page * c.stride_page + (int64_t)(j - pi * c.P) * c.stride_token;
     };
     // Loads are unconditional: a token that is not there reads the pool's first one instead, whose
     // scores are masked and whose values are zeroed, and a piece past the head's end reads its
     // last piece, which counts as zero in a key and goes to no output in a value.
+    auto clamp = [&](int d) { return FULL ? d : min(d, c.D - S::VEC); };
     u32x4 kf[S::TT][S::KK], vf[S::NV];
     auto load_keys = [&](int slot) {
 #pragma unroll
@@ -241,44 +365,45 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
             const char* src = (const char*)c.k + (s_off[wave][slot][16 * t + r] + head_at) * E::kBytes;
 #pragma unroll
             for (int kk = 0; kk < S::KK; ++kk)
-                kf[t][kk] = *(const u32x4*)(src + min(kk * S::KSTEP + q * S::VEC, c.D - S::VEC) * E::kBytes);
+                kf[t][kk] = stream_load<BF16>(src + clamp(kk * S::KSTEP + q * S::VEC) * E::kBytes);
         }
     };
     auto load_values = [&](int slot) {
-        const int d = min((lane % S::LPR) * S::VEC, c.D - S::VEC);
+        const int d = clamp((lane % S::LPR) * S::VEC);
         const char* src = (const char*)c.v + (head_at + d) * E::kBytes;
 #pragma unroll
         for (int k = 0; k < S::NV; ++k)
-            vf[k] = *(const u32x4*)(src + s_off[wave][slot][k * S::TPI + lane / S::LPR] * E::kBytes);
+            vf[k] = stream_load<BF16>(src + s_off[wave][slot][k * S::TPI + lane / S::LPR] * E::kBytes);
     };
     auto wave_sync = [&]() {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     };
 
-    int64_t off = locate(wave), off_next = locate(wave + kWaves);
+    int64_t off = place(wave, page_of(wave));
+    int page_next = page_of(wave + kWaves);
     if (lane < S::TOK) s_off[wave][0][lane] = max(off, (int64_t)0);
     wave_sync();
-    if (wave < blocks) {
-        load_keys(0);
-        load_values(0);
-    }
+    load_keys(0);
+    __builtin_amdgcn_sched_barrier(0);  // keys before values, as in the loop: their wait counts on it
+    load_values(0);
     int slot = 0;
     for (int blk = wave; blk < blocks; blk += kWaves, slot ^= 1) {
         const int j0 = c0 + blk * S::TOK;
         const uint32_t there = (uint32_t)__ballot(lane < S::TOK && off >= 0);
-        const bool more = blk + kWaves < blocks;
         // every row sees the whole block, or bits say which tokens
         const uint32_t every = S::TOK == 32 ? ~0u : (1u << S::TOK) - 1u;
         const bool whole = there == every &&
                            (a.mask ? j0 + S::TOK <= s.first
                                    : j0 + S::TOK - 1 <= s.first + i_lo && (a.window == 0 || j0 > s.first + i_hi - a.window));
-        if (c.D < DP) {
 #pragma unroll
-            for (int kk = 0; kk < S::KK; ++kk)
-                if (kk * S::KSTEP + q * S::VEC >= c.D)
+        for (int kk = 0; kk < S::KK; ++kk) {
+            if (FULL || ((kk + 1) * S::KSTEP <= DP / 2 && DP > 64)) continue;  // D > DP / 2 there
+            const bool past = kk * S::KSTEP + q * S::VEC >= c.D;
 #pragma unroll
-                    for (int t = 0; t < S::TT; ++t) kf[t][kk] = u32x4{0, 0, 0, 0};
+            for (int t = 0; t < S::TT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) kf[t][kk][e] = past ? 0u : kf[t][kk][e];
         }
         Weights<BF16> w[RB];
 #pragma unroll
@@ -292,11 +417,11 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
             }
             if (rb == RB - 1) {
                 // the next block's keys set out
-                off = off_next;
+                off = place(blk + kWaves, page_next);
                 if (lane < S::TOK) s_off[wave][slot ^ 1][lane] = max(off, (int64_t)0);
                 wave_sync();
-                if (more) load_keys(slot ^ 1);
-                off_next = locate(blk + 2 * kWaves);
+                load_keys(slot ^ 1);
+                page_next = page_of(blk + 2 * kWaves);
             }
             float top = kNoScore;
 #pragma unroll
@@ -335,79 +460,78 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
             w[rb].take(sv);
         }
 
-        // Values.  A row's weight 0 times an infinite or NaN value that the row does not see
-        // would be NaN: where rows differ in what they see, such elements are taken out, and a second
+        // Values.  A row's weight 0 times an infinite or NaN value that the row does not see would be
+        // NaN: where rows differ in what they see, such elements are taken out, and a second
         // product of the largest finite numbers puts infinity where a row does see one.
         bool odd = false;
         if (!whole) {
-            bool mine = false;
+            bool any = false;
 #pragma unroll
             for (int k = 0; k < S::NV; ++k) {
                 const bool gone = !((there >> (k * S::TPI + lane / S::LPR)) & 1u);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if (gone) vf[k][e] = 0;
-                    mine |= odd_lo<BF16>(vf[k][e]) || odd_hi(vf[k][e]);
+                    any |= odd_lo<BF16>(vf[k][e]) || odd_hi(vf[k][e]);
                 }
             }
-            odd = __any(mine);
-        }
-        auto put = [&]() {
+            odd = __any(any);
+            if (odd) {
 #pragma unroll
-            for (int k = 0; k < S::NV; ++k)
-                *(u32x4*)(s_v + ((k * S::TPI + lane / S::LPR) * S::PITCH + (lane % S::LPR) * S::VEC) * E::kBytes) = vf[k];
-            wave_sync();
+                for (int k = 0; k < S::NV; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (odd_lo<BF16>(vf[k][e])) vf[k][e] &= 0xFFFF0000u;
+                        if (odd_hi(vf[k][e])) vf[k][e] &= BF16 ? 0xFFFFu : 0u;
+                    }
+            }
+        }
+        auto piece_at = [&](int k) {
+            return (u32x4*)(s_v + ((k * S::TPI + lane / S::LPR) * S::PITCH + (lane % S::LPR) * S::VEC) * E::kBytes);
         };
-        // V^T of 16 dimensions as an A operand: this lane's dimension of the tokens of its weights
-        auto get = [&](int db) -> u32x4 {
-            if constexpr (BF16) {
-                char* at = s_v + ((4 * q + r / 4) * S::PITCH + db * 16 + (r % 4) * 4) * 2;
-                union {
-                    s16x4 half[2];
-                    u32x4 all;
-                } v;
-                v.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at));
-                v.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4*)(at + 16 * S::PITCH * 2));
-                return v.all;
-            } else {
+        // o += V^T of 16 dimensions (this lane's dimension of the tokens of its weights) times the weights
+        auto add_values = [&]() {
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
                 u32x4 v;
+                if constexpr (BF16) {
+                    char* at = s_v + ((4 * q + r / 4) * S::PITCH + db * 16 + (r % 4) * 4) * 2;
+                    union {
+                        s16x4 half[2];
+                        u32x4 all;
+                    } both;
+                    both.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at));
+                    both.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (__attribute__((address_space(3))) s16x4*)(at + 16 * S::PITCH * 2));
+                    v = both.all;
+                } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = *(const uint32_t*)(s_v + ((4 * q + e) * S::PITCH + db * 16 + r) * 4);
-                return v;
+                    for (int e = 0; e < 4; ++e) v[e] = *(const uint32_t*)(s_v + ((4 * q + e) * S::PITCH + db * 16 + r) * 4);
+                }
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) o[rb][db] = multiply<BF16>(v, w[rb].all, o[rb][db]);
             }
         };
-        if (odd) {
 #pragma unroll
-            for (int k = 0; k < S::NV; ++k)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (odd_lo<BF16>(vf[k][e])) vf[k][e] &= 0xFFFF0000u;
-                    if (odd_hi(vf[k][e])) vf[k][e] &= BF16 ? 0xFFFFu : 0u;
-                }
-        }
-        put();
-        if (more && !odd) load_values(slot ^ 1);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-            const u32x4 v = get(db);
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) o[rb][db] = multiply<BF16>(v, w[rb].all, o[rb][db]);
-        }
+        for (int k = 0; k < S::NV; ++k) *piece_at(k) = vf[k];
+        wave_sync();
+        load_values(slot ^ 1);
+        add_values();
         wave_sync();
         if (odd) {
-            load_values(slot);
             constexpr uint32_t kLo = BF16 ? 0x7F7Fu : 0u, kHi = BF16 ? 0x7F7F0000u : 0x7F7FFFFFu;  // largest finite
-#pragma unroll
+            const int ol = again(lane);
+            const int d = clamp((ol % S::LPR) * S::VEC);
+#pragma unroll 1
             for (int k = 0; k < S::NV; ++k) {
-                const bool gone = !((there >> (k * S::TPI + lane / S::LPR)) & 1u);
+                const int t = k * S::TPI + ol / S::LPR;
+                u32x4 v = *(const u32x4*)((const char*)c.v + (head_at + d + s_off[wave][slot][t]) * E::kBytes);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t w = vf[k][e];
-                    vf[k][e] = gone ? 0u : (odd_lo<BF16>(w) ? kLo : 0u) | (odd_hi(w) ? kHi : 0u);
-                }
+                for (int e = 0; e < 4; ++e)
+                    v[e] = there >> t & 1u ? (odd_lo<BF16>(v[e]) ? kLo : 0u) | (odd_hi(v[e]) ? kHi : 0u) : 0u;
+                *piece_at(k) = v;
             }
-            put();
+            wave_sync();
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 const uint32_t bits = (there & row_bits(a, s, row_i[rb], s.row0 + row_i[rb], j0)) >> (4 * q);
@@ -418,94 +542,147 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
                     for (int e = 0; e < 4; ++e) one[t][e] = bits & (1u << (16 * t + e)) ? kHuge : 0.f;
                 w[rb].take(one);
             }
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                const u32x4 v = get(db);
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) o[rb][db] = multiply<BF16>(v, w[rb].all, o[rb][db]);
-            }
+            add_values();
             wave_sync();
-            if (more) load_values(slot ^ 1);
         }
     }
 
-    // join the waves: a common maximum, then the outputs added pairwise through LDS
+    // Join the waves: a common maximum, then the outputs through LDS, summed by all threads, each for NP
+    // pairs of neighbouring dimensions.
+    constexpr int NP = ROWS * DP / 2 / kThreads;
+    constexpr int OP = DP + 4;
+    const int el = again(lane), et = again(tid), er = el & 15, eq = el >> 4;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         l[rb] += __shfl_xor(l[rb], 16);
         l[rb] += __shfl_xor(l[rb], 32);
-        if (q == 0) {
-            s_m[wave][rb * 16 + r] = m[rb];
-            s_l[wave][rb * 16 + r] = l[rb];
+        if (eq == 0) {
+            s_m[wave][rb * 16 + er] = m[rb];
+            s_l[wave][rb * 16 + er] = l[rb];
         }
     }
     __syncthreads();
-    float top[RB], total[RB];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        top[rb] = kNoScore;
-        total[rb] = 0.f;
-        for (int w = 0; w < kWaves; ++w) top[rb] = fmaxf(top[rb], s_m[w][rb * 16 + r]);
-        if (top[rb] != kNoScore)
-            for (int w = 0; w < kWaves; ++w) total[rb] += s_l[w][rb * 16 + r] * exp2_hw(s_m[w][rb * 16 + r] - top[rb]);
-        const float by = m[rb] == kNoScore ? 0.f : exp2_hw(m[rb] - top[rb]);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) o[rb][db] *= by;
-    }
     float* s_o = (float*)s_mem;
 #pragma unroll
-    for (int step = kWaves / 2; step > 0; step /= 2) {
-        if (wave >= step && wave < 2 * step) {
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-                for (int db = 0; db < DB; ++db)
-                    *(f32x4*)(s_o + ((((wave - step) * RB + rb) * DB + db) * 64 + lane) * 4) = o[rb][db];
-        }
-        __syncthreads();
-        if (wave < step) {
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-                for (int db = 0; db < DB; ++db)
-                    o[rb][db] += *(const f32x4*)(s_o + (((wave * RB + rb) * DB + db) * 64 + lane) * 4);
-        }
-        __syncthreads();
-    }
-    if (wave != 0) return;
-#pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        if (rb * 16 + r >= rows) continue;
-        const int rr = row0 + rb * 16 + r;
-        const int head = g * p.h + rr - row_i[rb] * p.h;
-        const int64_t t = s.row0 + row_i[rb];
-        if (n_parts == 1) {
-            const float by = top[rb] == kNoScore ? 0.f : 1.f / total[rb];
-            char* dst = (char*)a.out.data + (t * a.out.stride_row + (int64_t)head * a.out.stride_head) * E::kBytes;
+        const int row = rb * 16 + er;
+        float top = kNoScore;
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][row]);
+        const float by = m[rb] == kNoScore ? 0.f : exp2_hw(m[rb] - top);
 #pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                const int d = db * 16 + 4 * q;
-                if (d >= c.D) continue;
-                const f32x4 y = top[rb] == kNoScore ? f32x4{0.f, 0.f, 0.f, 0.f} : o[rb][db] * by;
-                if constexpr (BF16)
-                    *(uint2*)(dst + d * 2) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-                else
-                    *(f32x4*)(dst + d * 4) = y;
-            }
-            if (q == 0 && a.lse) a.lse[t * a.H + head] = top[rb] == kNoScore ? kNoScore : (top[rb] + log2f(total[rb])) * kLn2;
-        } else {
-            const int64_t at = ((int64_t)part * c.rows + t) * a.H + head;
-            float* dst = (float*)a.workspace + at * c.D;
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                const int d = db * 16 + 4 * q;
-                if (d < c.D) *(f32x4*)(dst + d) = o[rb][db];
-            }
-            if (q == 0) {
-                float2* ml = (float2*)((float*)a.workspace + (int64_t)p.parts * c.rows * a.H * c.D);
-                ml[at] = make_float2(top[rb], total[rb]);
-            }
+        for (int db = 0; db < DB; ++db) *(f32x4*)(s_o + (wave * ROWS + row) * OP + db * 16 + 4 * eq) = o[rb][db] * by;
+        if (wave == 0 && eq == 0) {
+            float sum = 0.f;
+            if (top != kNoScore)
+                for (int w = 0; w < kWaves; ++w) sum += s_l[w][row] * exp2_hw(s_m[w][row] - top);
+            s_top[row] = top;
+            s_sum[row] = sum;
         }
+    }
+    __syncthreads();
+    float2 y[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int e = (i * kThreads + et) * 2;
+        y[i] = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float2 x = *(const float2*)(s_o + (w * ROWS + e / DP) * OP + e % DP);
+            y[i].x += x.x;
+            y[i].y += x.y;
+        }
+    }
+    if (from != before || to != before + n_units) {
+        // A part of an item.  What a workgroup leaves of an item that its stretch begins with goes to
+        // its first slot, of one that begins later to its second.
+        const int w_first = owner(before), n_parts = owner(before + n_units - 1) - w_first + 1;
+        float* dst = slot_of(wg, from == u0 ? 0 : 1);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) leave2(dst + (i * kThreads + et) * 2, y[i].x, y[i].y);
+        if (et < ROWS) leave2(dst + ROWS * DP + 2 * et, s_top[et], s_sum[et]);
+        // all of it is written when the counter goes up: the workgroup that counts last finds every part
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (et == 0) {
+            unsigned* counter = (unsigned*)a.workspace + w_first * c.G + g;
+            const unsigned was = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            s_last = was == (unsigned)(n_parts - 1);
+            if (s_last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (!s_last) continue;  // s_last is written again two barriers later at the earliest
+        // the parts' common maximum and sum of each row, then their outputs, kBatch parts at a time
+        constexpr int kSubs = kThreads / ROWS, kBatch = 2048 / ROWS;
+        float* s_red = (float*)s_mem;         // [kSubs][ROWS][2]
+        float* s_fac = s_red + 2 * kThreads;  // [kBatch][ROWS]: the parts' factors
+        const int first_slot = before == start(w_first) ? 0 : 1;
+        auto part_slot = [&](int k) { return slot_of(w_first + k, k == 0 ? first_slot : 0); };
+        const int row = et % ROWS;
+        float mm = kNoScore, ll = 0.f;
+        for (int k = et / ROWS; k < n_parts; k += kSubs) {
+            const float2 x = fetch2(part_slot(k) + ROWS * DP + 2 * row);
+            const float up = fmaxf(mm, x.x);
+            if (up != kNoScore) ll = ll * exp2_hw(mm - up) + x.y * exp2_hw(x.x - up);
+            mm = up;
+        }
+        s_red[2 * et] = mm;
+        s_red[2 * et + 1] = ll;
+        __syncthreads();
+        if (et < ROWS) {
+            for (int k = 1; k < kSubs; ++k) {
+                const float xm = s_red[2 * (k * ROWS + et)], xl = s_red[2 * (k * ROWS + et) + 1];
+                const float up = fmaxf(mm, xm);
+                if (up != kNoScore) ll = ll * exp2_hw(mm - up) + xl * exp2_hw(xm - up);
+                mm = up;
+            }
+            s_top[et] = mm;
+            s_sum[et] = ll;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NP; ++i) y[i] = make_float2(0.f, 0.f);
+        for (int k0 = 0; k0 < n_parts; k0 += kBatch) {
+            const int nk = min(kBatch, n_parts - k0);
+            for (int i = et; i < nk * ROWS; i += kThreads) {
+                const float pm = fetch2(part_slot(k0 + i / ROWS) + ROWS * DP + 2 * (i % ROWS)).x;
+                s_fac[i] = pm == kNoScore ? 0.f : exp2_hw(pm - s_top[i % ROWS]);
+            }
+            __syncthreads();
+            for (int k = 0; k < nk; ++k) {
+                const float* src = part_slot(k0 + k);
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    const int e = (i * kThreads + et) * 2;
+                    const float2 x = fetch2(src + e);
+                    const float f = s_fac[k * ROWS + e / DP];
+                    if (f != 0.f) {
+                        y[i].x += x.x * f;
+                        y[i].y += x.y * f;
+                    }
+                }
+            }
+            __syncthreads();
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int e = (i * kThreads + et) * 2;
+        const int row = e / DP, d = e % DP;
+        if (row >= rows || d >= c.D) continue;
+        const int rr = row0 + row, ri = rr / p.h;
+        const int head = g * p.h + rr - ri * p.h;
+        const int64_t t = s.row0 + ri;
+        const bool none = s_top[row] == kNoScore;
+        const float by = none ? 0.f : 1.f / s_sum[row];
+        const float y0 = none ? 0.f : y[i].x * by, y1 = none ? 0.f : y[i].y * by;
+        char* dst = (char*)a.out.data + (t * a.out.stride_row + (int64_t)head * a.out.stride_head + d) * E::kBytes;
+        if constexpr (BF16)
+            *(uint32_t*)dst = pack_bf16(y0, y1);
+        else
+            *(float2*)dst = make_float2(y0, y1);
+        if (d == 0 && a.lse) a.lse[t * a.H + head] = none ? kNoScore : (s_top[row] + log2f(s_sum[row])) * kLn2;
+    }
+    __syncthreads();
     }
 }
 
@@ -522,7 +699,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 template <int DP>
 struct TileShape {
     static constexpr int TOK = 64;
-    static constexpr int ROWS = 128;
+    static constexpr int ROWS = 128;  // of kTileRows
     static constexpr int LPR = DP / 8;              // 16-byte pieces of a token
     static constexpr int TPP = kThreads / LPR;      // tokens of one load of the workgroup
     static constexpr int N = TOK / TPP;             // loads a block
@@ -820,7 +997,7 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
         if (hi == 0 && a.lse) a.lse[t_row * a.H + head] = m == kNoScore ? kNoScore : (m + log2f(l)) * kLn2;
     } else {
         const int64_t at = ((int64_t)part * c.rows + t_row) * a.H + head;
-        float* dst = (float*)a.workspace + at * c.D;
+        float* dst = (float*)a.workspace + kCounterFloats + at * c.D;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -829,7 +1006,7 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
                 if (d < c.D) *(f32x4*)(dst + d) = f32x4{o[db][e], o[db][e + 1], o[db][e + 2], o[db][e + 3]};
             }
         if (hi == 0) {
-            float2* ml = (float2*)((float*)a.workspace + (int64_t)p.parts * c.rows * a.H * c.D);
+            float2* ml = (float2*)((float*)a.workspace + kCounterFloats + (int64_t)p.parts * c.rows * a.H * c.D);
             ml[at] = make_float2(m, l);
         }
     }
@@ -855,7 +1032,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a, Plan p)
     const Range range = tile_range(a, s, row0 / p.h, (row0 + rows - 1) / p.h);
     const int n_parts = max((range.hi - range.lo + p.chunk - 1) / p.chunk, 1);
     if (n_parts == 1) return;
-    const float2* ml = (const float2*)((const float*)a.workspace + (int64_t)p.parts * c.rows * a.H * c.D);
+    const float2* ml = (const float2*)((const float*)a.workspace + kCounterFloats + (int64_t)p.parts * c.rows * a.H * c.D);
     const int64_t step = (int64_t)c.rows * a.H;
     float2 mine = make_float2(kNoScore, 0.f);
     if (lane < n_parts) mine = ml[lane * step + item];
@@ -871,7 +1048,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a, Plan p)
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     for (int k = 0; k < n_parts; ++k) {
         const float w = __shfl(by, k);
-        if (d < c.D && w != 0.f) o += *(const f32x4*)((const float*)a.workspace + (k * step + item) * c.D + d) * w;
+        if (d < c.D && w != 0.f) o += *(const f32x4*)((const float*)a.workspace + kCounterFloats + (k * step + item) * c.D + d) * w;
     }
     if (d < c.D) {
         const f32x4 y = top == kNoScore ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.f / total);
@@ -884,48 +1061,69 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a, Plan p)
     if (lane == 0 && a.lse) a.lse[item] = top == kNoScore ? kNoScore : (top + log2f(total)) * kLn2;
 }
 
-constexpr int kMaxParts = 64;   // join_kernel holds a part's weight in a lane
-constexpr int kMinChunk = 128;  // cached tokens of a part at least: a block per wave
-constexpr long kFill = 1024;    // workgroups that fill the device: 4 for each of 256 CUs
+constexpr int kMaxParts = 64;     // join_kernel holds a part's weight in a lane
+constexpr int kMinChunk = 128;    // cached tokens of a part at least
+constexpr int kTileRows = 128;    // rows of a tile_kernel workgroup
+constexpr long kFill = 1024;      // tile_kernel workgroups that fill the device: two rounds
+constexpr int kCus = 256;
+
+int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
 Plan make_plan(const CacheArgs& c, int H, bool bf16, int span) {
     Plan p;
     p.h = H / c.G;
     const long most = (long)c.max_new * p.h;
     const int limit = c.D > 128 ? 32 : 64;
-    p.tile_rows = most <= 16 ? 16 : most <= 32 ? 32 : bf16 && most > 64 ? 128 : limit;
+    p.tile_rows = most <= 16 ? 16 : most <= 32 ? 32 : bf16 && most > 64 ? kTileRows : limit;
     p.tiles = (int)((most + p.tile_rows - 1) / p.tile_rows);
-    const long groups = (long)c.B * c.G * p.tiles;
-    const long want = std::min<long>(std::min<long>((kFill + groups - 1) / groups, (span + kMinChunk - 1) / kMinChunk), kMaxParts);
-    p.parts = (int)std::max<long>(want, 1);
-    p.chunk = ((span + p.parts - 1) / p.parts + kMinChunk - 1) / kMinChunk * kMinChunk;
-    p.parts = (span + p.chunk - 1) / p.chunk;
+    p.wgs = p.parts = p.chunk = 0;
+    if (p.tile_rows != kTileRows) {
+        // resident workgroups: two a CU, or one where the rows' outputs take the registers of two
+        const int resident = kCus * (p.tile_rows / 16 * padded(c.D) >= 512 || c.D > 128 ? 1 : 2);
+        p.wgs = std::max(resident / c.G, 1);
+    } else {
+        const long groups = (long)c.B * c.G * p.tiles;
+        const long want = std::min<long>(std::min<long>((kFill + groups - 1) / groups, (span + kMinChunk - 1) / kMinChunk), kMaxParts);
+        p.parts = (int)std::max<long>(want, 1);
+        p.chunk = ((span + p.parts - 1) / p.parts + kMinChunk - 1) / kMinChunk * kMinChunk;
+        p.parts = (span + p.chunk - 1) / p.chunk;
+    }
     p.page_shift = -1;
     for (int k = 0; k <= 16; ++k)
         if (c.P == 1 << k) p.page_shift = k;
     return p;
 }
 
-template <bool BF16, int DP>
+template <bool BF16, int DP, bool FULL>
 void launch_stream(const AttentionArgs& a, const Plan& p, dim3 grid, hipStream_t stream) {
     if (p.tile_rows == 16)
-        hipLaunchKernelGGL((stream_kernel<BF16, DP, 1>), grid, dim3(kThreads), 0, stream, a, p);
+        hipLaunchKernelGGL((stream_kernel<BF16, DP, 1, FULL>), grid, dim3(kThreads), 0, stream, a, p);
     else if (p.tile_rows == 32)
-        hipLaunchKernelGGL((stream_kernel<BF16, DP, 2>), grid, dim3(kThreads), 0, stream, a, p);
+        hipLaunchKernelGGL((stream_kernel<BF16, DP, 2, FULL>), grid, dim3(kThreads), 0, stream, a, p);
     else if constexpr (DP <= 128)
-        hipLaunchKernelGGL((stream_kernel<BF16, DP, 4>), grid, dim3(kThreads), 0, stream, a, p);
+        hipLaunchKernelGGL((stream_kernel<BF16, DP, 4, FULL>), grid, dim3(kThreads), 0, stream, a, p);
+}
+
+template <bool BF16, int DP>
+void launch_stream(const AttentionArgs& a, const Plan& p, dim3 grid, hipStream_t stream) {
+    if (a.c.D == DP)
+        launch_stream<BF16, DP, true>(a, p, grid, stream);
+    else
+        launch_stream<BF16, DP, false>(a, p, grid, stream);
 }
 
 }  // namespace
 
 size_t attention_workspace(const CacheArgs& c, int H, bool bf16) {
     const Plan p = make_plan(c, H, bf16, c.max_kv);
-    if (p.parts == 1) return 0;
-    return align256((size_t)p.parts * c.rows * H * (c.D + 2) * 4);
+    if (p.tile_rows != kTileRows)
+        return align256(kCounterFloats * 4 + (size_t)p.wgs * c.G * 2 * p.tile_rows * (padded(c.D) + 2) * 4);
+    return p.parts == 1 ? 0 : align256(kCounterFloats * 4 + (size_t)p.parts * c.rows * H * (c.D + 2) * 4);
 }
 
 bool attention_fits(const CacheArgs& c, int H, bool bf16) {
     const Plan p = make_plan(c, H, bf16, c.max_kv);
+    if (p.tile_rows != kTileRows) return (long)c.B * p.tiles * (c.max_kv / kUnit + 2) < 1L << 30;  // units
     return (long)c.B * c.G * p.tiles * p.parts < 1L << 23;
 }
 
@@ -934,8 +1132,8 @@ hipError_t launch_attention(const AttentionArgs& a, bool bf16, hipStream_t strea
     // a windowed row sees at most `window` positions, a tile's rows together max_new - 1 more
     const int span = a.window > 0 ? (int)std::min<long>(c.max_kv, (long)a.window + c.max_new - 1) : c.max_kv;
     const Plan p = make_plan(c, a.H, bf16, span);
-    const dim3 grid((unsigned)((long)c.B * c.G * p.tiles * p.parts));
-    if (p.tile_rows == 128) {
+    const dim3 grid((unsigned)(p.tile_rows == kTileRows ? (long)c.B * c.G * p.tiles * p.parts : (long)p.wgs * c.G));
+    if (p.tile_rows == kTileRows) {
         if (c.D <= 64)
             hipLaunchKernelGGL(tile_kernel<64>, grid, dim3(kThreads), 0, stream, a, p);
         else if (c.D <= 128)
@@ -958,7 +1156,7 @@ hipError_t launch_attention(const AttentionArgs& a, bool bf16, hipStream_t strea
             launch_stream<false, 256>(a, p, grid, stream);
     }
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.parts == 1) return e;
+    if (e != hipSuccess || p.parts <= 1) return e;
     const dim3 joins((unsigned)(((long)c.rows * a.H + kWaves - 1) / kWaves));
     if (bf16)
         hipLaunchKernelGGL(join_kernel<true>, joins, dim3(kThreads), 0, stream, a, p);

@@ -541,8 +541,8 @@ def attention_workspace_bytes(cache: Cache, seqs: Seqs, q_heads: int) -> int:
 
 
 def new_attention_workspace(cache: Cache, seqs: Seqs, q_heads: int, device="cuda") -> torch.Tensor:
-    """Device workspace of psd_attention for these bounds (uninitialised; may be empty)."""
-    return torch.empty(attention_workspace_bytes(cache, seqs, q_heads), dtype=torch.uint8, device=device)
+    """Zero-filled device workspace of psd_attention for these bounds (may be empty)."""
+    return torch.zeros(attention_workspace_bytes(cache, seqs, q_heads), dtype=torch.uint8, device=device)
 
 
 def attention(cache: Cache, seqs: Seqs, q, ws, scale: float = None, window: int = 0, mask=None, out=None,
