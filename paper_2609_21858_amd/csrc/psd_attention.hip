@@ -136,8 +136,9 @@ struct Weights {
     }
 };
 
-// 16 bytes of the cache.  One workgroup reads a bfloat16 key or value for all its rows, once: it need
-// not stay in a cache (6.3 -> 7.0 TB/s of a plain read).  Float32 rows may be several tiles.
+// 16 bytes of a bfloat16 value, which one workgroup reads for all its rows, once: a whole row at a time,
+// it need not stay in a cache.  (A key's 128-byte line is read by two instructions, so keys stay.
+// 32 x up to 16384 tokens: 236 us; neither 256, both 250.)  Float32 rows may be several tiles.
 template <bool BF16>
 __device__ __forceinline__ u32x4 stream_load(const char* at) {
     if constexpr (BF16) return __builtin_nontemporal_load((const u32x4*)at);
@@ -155,8 +156,8 @@ __device__ __forceinline__ u32x4 stream_load(const char* at) {
 // keys and values are on their way into registers.
 //
 // Lengths are known on the device alone, so the device divides the work: an item is a row tile of a
-// sequence, its length the 128-token units it sees, and each of a head's R workgroups (resident
-// together) takes an equal stretch of all items' W units in a row.  An item
+// sequence, its length the 128-token units it sees, and each of a head's R workgroups (one a CU)
+// takes an equal stretch of all items' W units in a row.  An item
 // inside one workgroup's stretch is finished by it; of an item that is cut, every workgroup leaves its
 // output, maximum and sum in the workspace, and the one that leaves last joins them.
 template <bool BF16, int DP>
@@ -175,13 +176,16 @@ struct StreamShape {
     static constexpr int V_BYTES = TOK * PITCH * (BF16 ? 2 : 4);
 };
 
+// One workgroup a CU: two waves a SIMD, or one where the rows' outputs take the registers of two.
+constexpr int stream_waves(int DP, int RB) { return RB * DP >= 512 || DP == 256 ? 4 : 8; }
+
 // The waves' values; at an item's end, their outputs (rows of DP + 4 floats: the 16 rows of a store
 // fall on different banks).
 template <bool BF16, int DP, int RB>
 constexpr int stream_lds() {
     using S = StreamShape<BF16, DP>;
-    constexpr int values = kWaves * S::V_BYTES;
-    constexpr int join = kWaves * 16 * RB * (DP + 4) * 4;
+    constexpr int values = stream_waves(DP, RB) * S::V_BYTES;
+    constexpr int join = stream_waves(DP, RB) * 16 * RB * (DP + 4) * 4;
     return values > join ? values : join;
 }
 
@@ -226,16 +230,17 @@ __device__ __forceinline__ float2 fetch2(const float* at) {
 }
 
 template <bool BF16, int DP, int RB, bool FULL>
-__global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) void stream_kernel(AttentionArgs a, Plan p) {
+__global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(AttentionArgs a, Plan p) {
     using S = StreamShape<BF16, DP>;
     using E = Elem<BF16>;
     constexpr int DB = DP / 16;
+    constexpr int NW = stream_waves(DP, RB), NT = 64 * NW;
     constexpr int ROWS = 16 * RB;
     __shared__ __align__(16) char s_mem[stream_lds<BF16, DP, RB>()];
-    __shared__ int64_t s_off[kWaves][2][S::TOK];
-    __shared__ float s_m[kWaves][ROWS], s_l[kWaves][ROWS], s_top[ROWS], s_sum[ROWS];
-    __shared__ int s_units[kThreads + 1], s_wave[kWaves], s_longest[kWaves];
-    __shared__ Seq s_seq[kThreads];  // of the items, while there are no more than threads
+    __shared__ int64_t s_off[NW][2][S::TOK];
+    __shared__ float s_m[NW][ROWS], s_l[NW][ROWS], s_top[ROWS], s_sum[ROWS];
+    __shared__ int s_units[NT + 1], s_wave[NW], s_longest[NW];
+    __shared__ Seq s_seq[NT];  // of the items, while there are no more than threads
     __shared__ int s_chunk, s_last;
 
     const CacheArgs& c = a.c;
@@ -245,7 +250,7 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
 
     // units before each thread's items, by a scan over the workgroup
     const int items = c.B * p.tiles;
-    const int each = (items + kThreads - 1) / kThreads;
+    const int each = (items + NT - 1) / NT;
     auto seq_at = [&](int i) { return load_seq(c, i / p.tiles); };
     auto units_at = [&](int i, const Seq& s) { return item_units(a, p, s, i % p.tiles); };
     int mine = 0, longest = 0;
@@ -268,14 +273,14 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
         s_longest[wave] = longest;
     }
     __syncthreads();
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < NW; ++w) {
         if (w < wave) upto += s_wave[w];
         longest = max(longest, s_longest[w]);
     }
     s_units[tid + 1] = upto;
     if (tid == 0) s_units[0] = 0;
     __syncthreads();
-    const int units = uniform(s_units[kThreads]);
+    const int units = uniform(s_units[NT]);
     // R workgroups: the first W mod R have W / R + 1 units.  While no item is much longer than that,
     // each workgroup takes one item whole and none is joined.
     constexpr int kMinUnits = join_units<BF16, RB>();
@@ -365,7 +370,7 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
             const char* src = (const char*)c.k + (s_off[wave][slot][16 * t + r] + head_at) * E::kBytes;
 #pragma unroll
             for (int kk = 0; kk < S::KK; ++kk)
-                kf[t][kk] = stream_load<BF16>(src + clamp(kk * S::KSTEP + q * S::VEC) * E::kBytes);
+                kf[t][kk] = *(const u32x4*)(src + clamp(kk * S::KSTEP + q * S::VEC) * E::kBytes);
         }
     };
     auto load_values = [&](int slot) {
@@ -381,14 +386,19 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
     };
 
     int64_t off = place(wave, page_of(wave));
-    int page_next = page_of(wave + kWaves);
+    int page_next = page_of(wave + NW);
     if (lane < S::TOK) s_off[wave][0][lane] = max(off, (int64_t)0);
     wave_sync();
     load_keys(0);
     __builtin_amdgcn_sched_barrier(0);  // keys before values, as in the loop: their wait counts on it
     load_values(0);
     int slot = 0;
-    for (int blk = wave; blk < blocks; blk += kWaves, slot ^= 1) {
+    for (int round = 0; round < blocks; round += NW, slot ^= 1) {
+        // The CU serves its older waves first; left alone, they would be done in half the time, and the
+        // others could not keep memory busy.  The next blocks' loads are in flight meanwhile.
+        __builtin_amdgcn_s_barrier();
+        const int blk = round + wave;
+        if (blk >= blocks) continue;
         const int j0 = c0 + blk * S::TOK;
         const uint32_t there = (uint32_t)__ballot(lane < S::TOK && off >= 0);
         // every row sees the whole block, or bits say which tokens
@@ -417,11 +427,11 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
             }
             if (rb == RB - 1) {
                 // the next block's keys set out
-                off = place(blk + kWaves, page_next);
+                off = place(blk + NW, page_next);
                 if (lane < S::TOK) s_off[wave][slot ^ 1][lane] = max(off, (int64_t)0);
                 wave_sync();
                 load_keys(slot ^ 1);
-                page_next = page_of(blk + 2 * kWaves);
+                page_next = page_of(blk + 2 * NW);
             }
             float top = kNoScore;
 #pragma unroll
@@ -549,7 +559,7 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
 
     // Join the waves: a common maximum, then the outputs through LDS, summed by all threads, each for NP
     // pairs of neighbouring dimensions.
-    constexpr int NP = ROWS * DP / 2 / kThreads;
+    constexpr int NP = ROWS * DP / 2 / NT;
     constexpr int OP = DP + 4;
     const int el = again(lane), et = again(tid), er = el & 15, eq = el >> 4;
 #pragma unroll
@@ -567,14 +577,14 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
     for (int rb = 0; rb < RB; ++rb) {
         const int row = rb * 16 + er;
         float top = kNoScore;
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][row]);
+        for (int w = 0; w < NW; ++w) top = fmaxf(top, s_m[w][row]);
         const float by = m[rb] == kNoScore ? 0.f : exp2_hw(m[rb] - top);
 #pragma unroll
         for (int db = 0; db < DB; ++db) *(f32x4*)(s_o + (wave * ROWS + row) * OP + db * 16 + 4 * eq) = o[rb][db] * by;
         if (wave == 0 && eq == 0) {
             float sum = 0.f;
             if (top != kNoScore)
-                for (int w = 0; w < kWaves; ++w) sum += s_l[w][row] * exp2_hw(s_m[w][row] - top);
+                for (int w = 0; w < NW; ++w) sum += s_l[w][row] * exp2_hw(s_m[w][row] - top);
             s_top[row] = top;
             s_sum[row] = sum;
         }
@@ -583,10 +593,10 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
     float2 y[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-        const int e = (i * kThreads + et) * 2;
+        const int e = (i * NT + et) * 2;
         y[i] = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < NW; ++w) {
             const float2 x = *(const float2*)(s_o + (w * ROWS + e / DP) * OP + e % DP);
             y[i].x += x.x;
             y[i].y += x.y;
@@ -598,7 +608,7 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
         const int w_first = owner(before), n_parts = owner(before + n_units - 1) - w_first + 1;
         float* dst = slot_of(wg, from == u0 ? 0 : 1);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) leave2(dst + (i * kThreads + et) * 2, y[i].x, y[i].y);
+        for (int i = 0; i < NP; ++i) leave2(dst + (i * NT + et) * 2, y[i].x, y[i].y);
         if (et < ROWS) leave2(dst + ROWS * DP + 2 * et, s_top[et], s_sum[et]);
         // all of it is written when the counter goes up: the workgroup that counts last finds every part
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -612,9 +622,9 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
         __syncthreads();
         if (!s_last) continue;  // s_last is written again two barriers later at the earliest
         // the parts' common maximum and sum of each row, then their outputs, kBatch parts at a time
-        constexpr int kSubs = kThreads / ROWS, kBatch = 2048 / ROWS;
+        constexpr int kSubs = NT / ROWS, kBatch = 2048 / ROWS;
         float* s_red = (float*)s_mem;         // [kSubs][ROWS][2]
-        float* s_fac = s_red + 2 * kThreads;  // [kBatch][ROWS]: the parts' factors
+        float* s_fac = s_red + 2 * NT;  // [kBatch][ROWS]: the parts' factors
         const int first_slot = before == start(w_first) ? 0 : 1;
         auto part_slot = [&](int k) { return slot_of(w_first + k, k == 0 ? first_slot : 0); };
         const int row = et % ROWS;
@@ -643,7 +653,7 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
         for (int i = 0; i < NP; ++i) y[i] = make_float2(0.f, 0.f);
         for (int k0 = 0; k0 < n_parts; k0 += kBatch) {
             const int nk = min(kBatch, n_parts - k0);
-            for (int i = et; i < nk * ROWS; i += kThreads) {
+            for (int i = et; i < nk * ROWS; i += NT) {
                 const float pm = fetch2(part_slot(k0 + i / ROWS) + ROWS * DP + 2 * (i % ROWS)).x;
                 s_fac[i] = pm == kNoScore ? 0.f : exp2_hw(pm - s_top[i % ROWS]);
             }
@@ -652,7 +662,7 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
                 const float* src = part_slot(k0 + k);
 #pragma unroll
                 for (int i = 0; i < NP; ++i) {
-                    const int e = (i * kThreads + et) * 2;
+                    const int e = (i * NT + et) * 2;
                     const float2 x = fetch2(src + e);
                     const float f = s_fac[k * ROWS + e / DP];
                     if (f != 0.f) {
@@ -666,7 +676,7 @@ __global__ __launch_bounds__(kThreads, (RB * DP >= 512 || DP == 256 ? 1 : 2)) vo
     }
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-        const int e = (i * kThreads + et) * 2;
+        const int e = (i * NT + et) * 2;
         const int row = e / DP, d = e % DP;
         if (row >= rows || d >= c.D) continue;
         const int rr = row0 + row, ri = rr / p.h;
@@ -1078,9 +1088,7 @@ Plan make_plan(const CacheArgs& c, int H, bool bf16, int span) {
     p.tiles = (int)((most + p.tile_rows - 1) / p.tile_rows);
     p.wgs = p.parts = p.chunk = 0;
     if (p.tile_rows != kTileRows) {
-        // resident workgroups: two a CU, or one where the rows' outputs take the registers of two
-        const int resident = kCus * (p.tile_rows / 16 * padded(c.D) >= 512 || c.D > 128 ? 1 : 2);
-        p.wgs = std::max(resident / c.G, 1);
+        p.wgs = std::max(kCus / c.G, 1);  // one a CU
     } else {
         const long groups = (long)c.B * c.G * p.tiles;
         const long want = std::min<long>(std::min<long>((kFill + groups - 1) / groups, (span + kMinChunk - 1) / kMinChunk), kMaxParts);
@@ -1097,11 +1105,11 @@ Plan make_plan(const CacheArgs& c, int H, bool bf16, int span) {
 template <bool BF16, int DP, bool FULL>
 void launch_stream(const AttentionArgs& a, const Plan& p, dim3 grid, hipStream_t stream) {
     if (p.tile_rows == 16)
-        hipLaunchKernelGGL((stream_kernel<BF16, DP, 1, FULL>), grid, dim3(kThreads), 0, stream, a, p);
+        hipLaunchKernelGGL((stream_kernel<BF16, DP, 1, FULL>), grid, dim3(64 * stream_waves(DP, 1)), 0, stream, a, p);
     else if (p.tile_rows == 32)
-        hipLaunchKernelGGL((stream_kernel<BF16, DP, 2, FULL>), grid, dim3(kThreads), 0, stream, a, p);
+        hipLaunchKernelGGL((stream_kernel<BF16, DP, 2, FULL>), grid, dim3(64 * stream_waves(DP, 2)), 0, stream, a, p);
     else if constexpr (DP <= 128)
-        hipLaunchKernelGGL((stream_kernel<BF16, DP, 4, FULL>), grid, dim3(kThreads), 0, stream, a, p);
+        hipLaunchKernelGGL((stream_kernel<BF16, DP, 4, FULL>), grid, dim3(64 * stream_waves(DP, 4)), 0, stream, a, p);
 }
 
 template <bool BF16, int DP>
