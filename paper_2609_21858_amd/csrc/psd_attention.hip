@@ -658,17 +658,22 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
                 s_fac[i] = pm == kNoScore ? 0.f : exp2_hw(pm - s_top[i % ROWS]);
             }
             __syncthreads();
+            // all of a part's loads set out before one is waited for, and the next part's before this one is added
+            float2 x[NP], x_next[NP];
+            auto fetch = [&](int k, float2 (&into)[NP]) {
+                const float* src = part_slot(k0 + k) + 2 * et;
+#pragma unroll
+                for (int i = 0; i < NP; ++i) into[i] = fetch2(src + 2 * i * NT);
+            };
+            fetch(0, x);
             for (int k = 0; k < nk; ++k) {
-                const float* src = part_slot(k0 + k);
+                fetch(min(k + 1, nk - 1), x_next);
 #pragma unroll
                 for (int i = 0; i < NP; ++i) {
-                    const int e = (i * NT + et) * 2;
-                    const float2 x = fetch2(src + e);
-                    const float f = s_fac[k * ROWS + e / DP];
-                    if (f != 0.f) {
-                        y[i].x += x.x * f;
-                        y[i].y += x.y * f;
-                    }
+                    const float f = s_fac[k * ROWS + (i * NT + et) * 2 / DP];
+                    y[i].x += x[i].x * f;
+                    y[i].y += x[i].y * f;
+                    x[i] = x_next[i];
                 }
             }
             __syncthreads();
