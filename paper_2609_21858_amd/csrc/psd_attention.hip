@@ -363,6 +363,8 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
     // scores are masked and whose values are zeroed, and a piece past the head's end reads its
     // last piece, which counts as zero in a key and goes to no output in a value.
     auto clamp = [&](int d) { return FULL ? d : min(d, c.D - S::VEC); };
+    // float32 products bound their kernel, so those past the head's end are left out
+    auto in_head = [&](int d) { return FULL || BF16 || d < c.D; };
     u32x4 kf[S::TT][S::KK], vf[S::NV];
     auto load_keys = [&](int slot) {
 #pragma unroll
@@ -423,7 +425,8 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
             for (int t = 0; t < S::TT; ++t) {
                 sv[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int kk = 0; kk < S::KK; ++kk) sv[t] = multiply<BF16>(kf[t][kk], qf[rb][kk], sv[t]);
+                for (int kk = 0; kk < S::KK; ++kk)
+                    if (in_head(kk * S::KSTEP)) sv[t] = multiply<BF16>(kf[t][kk], qf[rb][kk], sv[t]);
             }
             if (rb == RB - 1) {
                 // the next block's keys set out
@@ -503,6 +506,7 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
         auto add_values = [&]() {
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
+                if (!in_head(16 * db)) break;
                 u32x4 v;
                 if constexpr (BF16) {
                     char* at = s_v + ((4 * q + r / 4) * S::PITCH + db * 16 + (r % 4) * 4) * 2;
