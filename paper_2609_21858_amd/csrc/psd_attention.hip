@@ -318,6 +318,7 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
     const int blocks = (c1 - c0 + S::TOK - 1) / S::TOK;
     const int32_t* table = c.table + (int64_t)b * c.table_stride;
 
+    auto clamp = [&](int d) { return FULL ? d : min(d, c.D - S::VEC); };
     // this lane's rows, and their queries as B operands
     int row_i[RB];
     u32x4 qf[RB][S::KK];
@@ -332,9 +333,18 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
 #pragma unroll
         for (int kk = 0; kk < S::KK; ++kk) {
             const int d = kk * S::KSTEP + q * S::VEC;
-            qf[rb][kk] = on && d < c.D ? *(const u32x4*)(src + d * E::kBytes) : u32x4{0, 0, 0, 0};
+            qf[rb][kk] = *(const u32x4*)(src + clamp(d) * E::kBytes);
         }
     }
+    // (unconditional loads; rows and dimensions that are not there count as zero)
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int kk = 0; kk < S::KK; ++kk) {
+            const bool none = rb * 16 + r >= rows || kk * S::KSTEP + q * S::VEC >= c.D;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) qf[rb][kk][e] = none ? 0u : qf[rb][kk][e];
+        }
 
     f32x4 o[RB][DB];
     float m[RB], l[RB];
@@ -362,7 +372,6 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
     // Loads are unconditional: a token that is not there reads the pool's first one instead, whose
     // scores are masked and whose values are zeroed, and a piece past the head's end reads its
     // last piece, which counts as zero in a key and goes to no output in a value.
-    auto clamp = [&](int d) { return FULL ? d : min(d, c.D - S::VEC); };
     // float32 products bound their kernel, so those past the head's end are left out
     auto in_head = [&](int d) { return FULL || BF16 || d < c.D; };
     u32x4 kf[S::TT][S::KK], vf[S::NV];
@@ -738,7 +747,7 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
     __shared__ int s_odd[2];
 
     const CacheArgs& c = a.c;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int r = lane & 31, hi = lane >> 5;
     int x = blockIdx.x;
     const int g = x % c.G;
@@ -747,11 +756,11 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
     x /= p.tiles;
     const int b = x % c.B, part = x / c.B;
 
-    const Seq s = load_seq(c, b);
+    const Seq s = uniform(load_seq(c, b));
     const int row0 = tile * S::ROWS;
     const int rows = min(s.n * p.h - row0, S::ROWS);
     if (rows <= 0) return;
-    const int i_lo = row0 / p.h, i_hi = (row0 + rows - 1) / p.h;
+    const int i_lo = uniform(row0 / p.h), i_hi = uniform((row0 + rows - 1) / p.h);
     const Range range = tile_range(a, s, i_lo, i_hi);
     const int n_parts = max((range.hi - range.lo + p.chunk - 1) / p.chunk, 1);
     if (part >= n_parts) return;
@@ -761,7 +770,7 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
 
     // this wave's rows: new tokens [w_lo, w_hi]; a wave without rows keeps company with zeros
     const int mine = min(max(rows - wave * 32, 0), 32);
-    const int w_lo = (row0 + min(wave * 32, rows - 1)) / p.h, w_hi = (row0 + min(wave * 32 + 31, rows - 1)) / p.h;
+    const int w_lo = uniform((row0 + min(wave * 32, rows - 1)) / p.h), w_hi = uniform((row0 + min(wave * 32 + 31, rows - 1)) / p.h);
     const bool on = r < mine;
     const int rr = row0 + wave * 32 + r;
     const int row_i = on ? rr / p.h : w_lo;
@@ -774,15 +783,14 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
     u32x4 qf[KK];
     {
         const char* src = (const char*)a.q.data + (t_row * a.q.stride_row + (int64_t)head * a.q.stride_head) * 2;
+        // unconditional loads; rows and dimensions that are not there count as zero
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) qf[kk] = *(const u32x4*)(src + min(kk * 16 + hi * 8, c.D - 8) * 2);
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
-            const int d = kk * 16 + hi * 8;
-            qf[kk] = u32x4{0, 0, 0, 0};
-            if (on && d < c.D) {
-                qf[kk] = *(const u32x4*)(src + d * 2);
+            const bool none = !on || kk * 16 + hi * 8 >= c.D;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) qf[kk][e] ^= sign;
-            }
+            for (int e = 0; e < 4; ++e) qf[kk][e] = none ? 0u : qf[kk][e] ^ sign;
         }
     }
     f32x16 o[DB];
@@ -799,15 +807,27 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
     const char* k_src = (const char*)c.k + (head_at + d_piece) * 2;
     const char* v_src = (const char*)c.v + (head_at + d_piece) * 2;
 
-    auto locate = [&](int blk) -> int64_t {  // threads of wave 0
-        const int j = c0 + blk * S::TOK + tid;
-        if (blk >= blocks || j >= c1) return -1;
-        return token_offset(c, p, table, j);
+    // Wave 0 finds the tokens' places; a page number is loaded a block before it is used.
+    auto page_of = [&](int blk) {
+        const int j = c0 + blk * S::TOK + lane;
+        const int at = j < c1 ? j : 0;
+        return table[p.page_shift >= 0 ? at >> p.page_shift : at / c.P];
     };
-    auto publish = [&](int blk, int64_t off) {
-        s_off[blk & 3][tid] = max(off, (int64_t)0);
+    auto place = [&](int blk, int page) -> int64_t {
+        const int j = c0 + blk * S::TOK + lane;
+        const int pi = p.page_shift >= 0 ? j >> p.page_shift : j / c.P;
+        if (j >= c1 || (unsigned)page >= (unsigned)c.pages) return -1;
+        return (int64_t)page * c.stride_page + (int64_t)(j - pi * c.P) * c.stride_token;
+    };
+    auto publish = [&](int blk, int page) {
+        const int64_t off = place(blk, page);
+        s_off[blk & 3][lane] = max(off, (int64_t)0);
         const uint64_t bits = __ballot(off >= 0);
-        if (tid == 0) s_there[blk & 3] = bits;
+        if (lane == 0) s_there[blk & 3] = bits;
+    };
+    auto there_of = [&](int blk) {
+        const uint64_t bits = s_there[blk & 3];
+        return (uint64_t)(uint32_t)uniform((int)(uint32_t)bits) | (uint64_t)(uint32_t)uniform((int)(bits >> 32)) << 32;
     };
     u32x4 kf[S::N], vf[S::N];
     auto load = [&](int blk) {
@@ -821,7 +841,7 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
     // Does every row of new tokens [lo, hi] see the whole block?
     auto whole = [&](int blk, int lo, int top) {
         const int j0 = c0 + blk * S::TOK;
-        if (s_there[blk & 3] != ~0ull) return false;
+        if (there_of(blk) != ~0ull) return false;
         if (a.mask) return j0 + S::TOK <= s.first;
         return j0 + S::TOK - 1 <= s.first + lo && (a.window == 0 || j0 > s.first + top - a.window);
     };
@@ -834,7 +854,7 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
 #pragma unroll
             for (int k = 0; k < S::N; ++k) kf[k] = u32x4{0, 0, 0, 0};
         if (!whole(blk, i_lo, i_hi)) {
-            const uint64_t there = s_there[blk & 3];
+            const uint64_t there = there_of(blk);
             bool odd = false;
 #pragma unroll
             for (int k = 0; k < S::N; ++k) {
@@ -872,26 +892,21 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
         return v.all;
     };
 
-    int64_t off = -1;
-    if (wave == 0) {
-        publish(0, locate(0));
-        off = locate(1);
-    }
+    if (wave == 0) publish(0, page_of(0));
+    int page = page_of(1);
     if (tid < 2) s_odd[tid] = 0;
     __syncthreads();
-    if (blocks > 0) load(0);
-    if (wave == 0) {
-        publish(1, off);
-        off = locate(2);
-    }
+    load(0);
+    if (wave == 0) publish(1, page);
+    page = page_of(2);
     if (blocks > 0) store(0);
     for (int blk = 0; blk < blocks; ++blk) {
         __syncthreads();
         const int j0 = c0 + blk * S::TOK;
         const bool more = blk + 1 < blocks;
-        if (more) load(blk + 1);
+        load(blk + 1);  // (past the end: the pool's first tokens, which nothing uses)
         const bool seen_by_all = whole(blk, w_lo, w_hi);
-        const uint64_t there = s_there[blk & 3];
+        const uint64_t there = there_of(blk);
         // nothing of the block lies before this wave's last row's end (or behind its window)
         const bool idle = mine == 0 || (!a.mask && (j0 > s.first + w_hi ||
                                                     (a.window > 0 && j0 + S::TOK - 1 <= s.first + w_lo - a.window)));
@@ -919,6 +934,7 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
 #pragma unroll
                     for (int e = 0; e < 16; ++e) sv[t][e] = bits[t] & (1u << (8 * (e / 4) + e % 4)) ? sv[t][e] : kNoScore;
                 }
+                if (a.mask) __builtin_amdgcn_s_waitcnt(0x0F70);  // no load of this branch is pending behind it
             }
             float top = sv[0][0];
 #pragma unroll
@@ -954,7 +970,7 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
                     o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(values, db, ks), __builtin_bit_cast(bf16x8, w[ks]), o[db],
                                                                     0, 0, 0);
         }
-        if (s_odd[blk & 1] == blk + 1) {
+        if (uniform(s_odd[blk & 1]) == blk + 1) {
             // infinite or NaN values were taken out of this block: a product of the largest finite
             // numbers puts infinity where a row sees one
             u32x4 again[S::N];
@@ -991,10 +1007,8 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
             }
         }
         if (more) store(blk + 1);
-        if (wave == 0) {
-            publish(blk + 2, off);
-            off = locate(blk + 3);
-        }
+        if (wave == 0) publish(blk + 2, page);
+        page = page_of(blk + 3);
     }
 
     l += __shfl_xor(l, 32);
@@ -1081,9 +1095,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a, Plan p)
 }
 
 constexpr int kMaxParts = 64;     // join_kernel holds a part's weight in a lane
-constexpr int kMinChunk = 128;    // cached tokens of a part at least
+constexpr int kMinChunk = 256;    // tile_kernel: cached tokens of a part at least
 constexpr int kTileRows = 128;    // rows of a tile_kernel workgroup
-constexpr long kFill = 1024;      // tile_kernel workgroups that fill the device: two rounds
 constexpr int kCus = 256;
 
 int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
@@ -1099,10 +1112,20 @@ Plan make_plan(const CacheArgs& c, int H, bool bf16, int span) {
     if (p.tile_rows != kTileRows) {
         p.wgs = std::max(kCus / c.G, 1);  // one a CU
     } else {
+        // Parts of the longest range, by the time they take in 64-token blocks: every round of resident
+        // workgroups takes a part and about 3 blocks to start and end; the join of 2 parts of 512 groups
+        // took as long as 13 blocks.
         const long groups = (long)c.B * c.G * p.tiles;
-        const long want = std::min<long>(std::min<long>((kFill + groups - 1) / groups, (span + kMinChunk - 1) / kMinChunk), kMaxParts);
-        p.parts = (int)std::max<long>(want, 1);
-        p.chunk = ((span + p.parts - 1) / p.parts + kMinChunk - 1) / kMinChunk * kMinChunk;
+        const long resident = kCus * (c.D > 128 ? 1 : 2);
+        double best = 0;
+        for (int parts = 1; parts <= kMaxParts && (parts - 1) * kMinChunk < span; ++parts) {
+            const int chunk = ((span + parts - 1) / parts + kMinChunk - 1) / kMinChunk * kMinChunk;
+            const double rounds = (double)((groups * parts + resident - 1) / resident);
+            const double cost = rounds * (chunk / 64.0 + 3) + (parts > 1 ? 1.5 + groups * parts * (13.0 / 1024) : 0);
+            if (parts > 1 && cost >= best) continue;
+            best = cost;
+            p.chunk = chunk;
+        }
         p.parts = (span + p.chunk - 1) / p.chunk;
     }
     p.page_shift = -1;
