@@ -1,0 +1,139 @@
+"""Attention whose work is divided over workgroups: many sequences, very unlike ones, long caches in parts,
+and that the division changes nothing from call to call (GPU).  Bounds as in test_gpu_serving.py."""
+import math
+import os
+import sys
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+sys.path.insert(0, ROOT)
+sys.path.insert(0, os.path.join(ROOT, "tests"))
+
+import serving_ref as ref  # noqa: E402
+from test_gpu_serving import check_attention, path_mask  # noqa: E402
+
+BF16, F32 = torch.bfloat16, torch.float32
+TYPES = pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+
+
+@pytest.fixture(scope="module")
+def psd():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_21858_amd import psd as m
+    return m
+
+
+@TYPES
+def test_more_sequences_than_threads(psd, dtype):
+    """700 sequences, some without new tokens or without any, and one that is far longer than the others."""
+    g = torch.Generator().manual_seed(9)
+    lens = []
+    for b in range(700):
+        n = int(torch.randint(0, 4, (1,), generator=g))
+        lens.append((n, n + int(torch.randint(0, 40, (1,), generator=g))))
+    lens[600] = (3, 2000)
+    check_attention(psd, lens, 4, 2, 64, 16, dtype, print_name="700")
+
+
+@TYPES
+def test_a_head_of_its_own_for_each_query(psd, dtype):
+    check_attention(psd, [(1, 20 * b + 1) for b in range(40)], 16, 16, 64, 16, dtype)
+
+
+@TYPES
+@pytest.mark.parametrize("n,H,G,D,kv", [(1, 4, 1, 128, 5000), (5, 4, 1, 128, 3001), (1, 16, 8, 128, 4097), (11, 4, 1, 64, 2500),
+                                        (40, 4, 1, 128, 2700), (130, 2, 2, 64, 2300), (1, 8, 2, 256, 2999), (35, 4, 2, 200, 1400)])
+def test_one_long_sequence_in_parts(psd, n, H, G, D, kv, dtype):
+    check_attention(psd, [(n, kv)], H, G, D, 24, dtype)
+
+
+@TYPES
+def test_unlike_sequences(psd, dtype):
+    """Cuts inside sequences, whole short ones between them, rows of several sizes."""
+    check_attention(psd, [(1, 3000), (2, 5), (1, 700), (0, 900), (2, 2), (1, 2500), (1, 1)], 8, 2, 128, 16, dtype)
+    check_attention(psd, [(40, 1500), (3, 1200), (40, 40), (1, 1)], 4, 1, 128, 64, dtype)
+
+
+@TYPES
+def test_windows_and_paths_in_parts(psd, dtype):
+    check_attention(psd, [(4, 3000), (2, 2900)], 8, 2, 64, 16, dtype, window=1500)
+    check_attention(psd, [(60, 2600)], 4, 1, 128, 16, dtype, window=1100)
+    check_attention(psd, [(17, 2000), (17, 17)], 8, 2, 128, 32, dtype, mask=path_mask(4, 4) * 2)
+    check_attention(psd, [(33, 1800)], 8, 2, 64, 32, dtype, mask=path_mask(4, 8))
+
+
+@TYPES
+@pytest.mark.parametrize("n", [2, 70])
+def test_unseen_values_in_parts(psd, n, dtype):
+    """NaN in the last token's key and value, and behind the window, in a cache that is cut."""
+    s = ref.Sequences([(n, 3000)], 1, 64, 16, dtype, seed=3)
+    q = torch.randn((n, 4, 64), generator=s.gen).to(dtype)
+    want, *_ = ref.attention(s, q, 0.125, 2500)
+    for pos, value in ((2999, math.nan), (3000 - n - 2500 - 3, math.inf)):
+        page, place = s.place(0, pos)
+        s.k[page, place] = value
+        s.v[page, place] = value
+    cache, seqs, dk, dv = s.handles(psd)
+    got = psd.attention(cache, seqs, q.cuda(), psd.new_attention_workspace(cache, seqs, 4), window=2500)["out"].cpu().double()
+    assert bool(torch.isfinite(got[:-1]).all()) and not bool(torch.isfinite(got[-1]).any())
+    assert float((got[:-1] - want[:-1]).abs().max()) < (0.01 if dtype == BF16 else 1e-4)
+
+
+@TYPES
+def test_same_bits_every_time(psd, dtype):
+    """Who finishes a part first does not change its sum, and one workspace serves calls of other shapes."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    ws = None
+    runs = []
+    for lens, H in (([(1, 6000), (1, 300), (2, 4000)], 8), ([(40, 3000)], 8), ([(1, 6000), (1, 300), (2, 4000)], 8)):
+        s = ref.Sequences(lens, 2, 128, 64, dtype, seed=7)
+        q = torch.randn((s.rows, H, 128), generator=s.gen).to(dtype).cuda()
+        cache, seqs, dk, dv = s.handles(psd)
+        need = psd.attention_workspace_bytes(cache, seqs, H)
+        if ws is None:
+            ws = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
+        assert need <= ws.numel()
+        first = psd.attention(cache, seqs, q, ws, want_lse=True)
+        for _ in range(6):
+            torch.randn((1 << 20,), device="cuda", generator=g)
+            again = psd.attention(cache, seqs, q, ws, want_lse=True)
+            assert torch.equal(first["out"], again["out"]) and torch.equal(first["lse"], again["lse"])
+        runs.append(first)
+    assert torch.equal(runs[0]["out"], runs[2]["out"])
+
+
+@TYPES
+@pytest.mark.parametrize("interleaved,R", [(False, 64), (True, 64), (False, 20), (False, 0)])
+def test_append_of_many_rows(psd, interleaved, R, dtype):
+    """A wave a row from some number of rows on: the same bits as the rows in smaller calls."""
+    n, H, G, D, P = 2500, 4, 2, 64, 16
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn((n, H + 2 * G, D), device="cuda", generator=g).to(dtype)
+    w = torch.randn((2, D), device="cuda", generator=g).to(dtype)
+    angle = torch.rand((n, max(R // 2, 1)), device="cuda", generator=g) * 6
+    cos, sin = (angle.cos(), angle.sin()) if R else (None, None)
+    width = -(-n // P)
+    table = torch.randperm(width, device="cuda", generator=g).to(torch.int32)[None].contiguous()
+    pools, queries = [], []
+    for cut in (n, 1000):
+        k = torch.zeros((width, P, G, D), dtype=dtype, device="cuda")
+        v = torch.zeros_like(k)
+        out = torch.empty((n, H, D), dtype=dtype, device="cuda")
+        for at in range(0, n, cut):
+            rows = min(cut, n - at)
+            seqs = psd.make_seqs(torch.tensor([0, rows], dtype=torch.int32).cuda(),
+                                 torch.tensor([at + rows], dtype=torch.int32).cuda(), table, rows, rows, n)
+            part = x[at:at + rows]
+            psd.kv_append(psd.make_cache(k, v), seqs, part[:, H:H + G], part[:, H + G:], q=part[:, :H], q_out=out[at:at + rows],
+                          cos=cos, sin=sin, interleaved=interleaved, q_norm=w[0], k_norm=w[1])
+        pools += [k, v]
+        queries.append(out)
+    torch.cuda.synchronize()
+    assert torch.equal(pools[0], pools[2]) and torch.equal(pools[1], pools[3]) and torch.equal(queries[0], queries[1])
+    seq = table[0].long()
+    assert torch.equal(pools[1][seq].reshape(-1, G, D)[:n], x[:, H + G:])
