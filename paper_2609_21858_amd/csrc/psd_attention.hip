@@ -880,9 +880,10 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
         }
     };
     // this lane's dimension of 32 db + .., tokens 16 ks + {4 hi .., 8 + 4 hi ..}, as an A operand
-    auto value = [&](const char* values, int db, int ks) -> bf16x8 {
-        const int i = lane & 15;
-        const char* at = values + ((16 * ks + 4 * hi + i / 4) * S::VP + db * 32 + ((lane >> 4) & 1) * 16 + (i % 4) * 4) * 2;
+    const int v_lane = ((4 * hi + (lane & 15) / 4) * S::VP + ((lane >> 4) & 1) * 16 + (lane & 3) * 4) * 2;
+    typedef __attribute__((address_space(3))) char lds_char;
+    auto value = [&](lds_char* mine, int db, int ks) -> bf16x8 {  // mine: the block's values + v_lane
+        lds_char* at = mine + (16 * ks * S::VP + db * 32) * 2;
         union {
             s16x4 half[2];
             bf16x8 all;
@@ -913,17 +914,31 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
         uint32_t bits[2] = {~0u, ~0u};
         if (!idle) {
             const char* keys = key_at(blk);
-            const char* values = value_at(blk);
+            lds_char* values = (lds_char*)value_at(blk) + v_lane;
+            // Scores: four keys' pieces are read from LDS while the last four are multiplied.
             f32x16 sv[2];
+            u32x4 kb[2][4];
+            constexpr int CH = KK / 4;  // groups of four pieces of 32 keys
+            auto read_keys = [&](int n, u32x4 (&into)[4]) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+                for (int i = 0; i < 4; ++i)
+                    into[i] = *(const u32x4*)(keys + ((32 * (n / CH) + r) * S::KP + (n % CH * 4 + i) * 16 + hi * 8) * 2);
+            };
+            read_keys(0, kb[0]);
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sv[t][e] = 0.f;
+            for (int n = 0; n < 2 * CH; ++n) {
+                if (n + 1 < 2 * CH) read_keys(n + 1, kb[(n + 1) & 1]);
 #pragma unroll
-                for (int kk = 0; kk < KK; ++kk) {
-                    const u32x4 kv = *(const u32x4*)(keys + ((32 * t + r) * S::KP + kk * 16 + hi * 8) * 2);
-                    sv[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kv),
-                                                                    __builtin_bit_cast(bf16x8, qf[kk]), sv[t], 0, 0, 0);
+                for (int i = 0; i < 4; ++i) {
+                    if (n % CH == 0 && i == 0)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) sv[n / CH][e] = 0.f;
+                    sv[n / CH] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kb[n & 1][i]),
+                                                                        __builtin_bit_cast(bf16x8, qf[n % CH * 4 + i]), sv[n / CH], 0,
+                                                                        0, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);                         // one product,
+                    if (n + 1 < 2 * CH) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // one read
                 }
             }
             if (!seen_by_all) {
@@ -952,23 +967,45 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
                 for (int db = 0; db < DB; ++db) o[db] *= by;
             }
             const float from = m == kNoScore ? 0.f : m;
-            u32x4 w[4];
+            // Weights of 16 tokens at a time, and their product with the values, whose pieces are read 16 tokens ahead:
+            // exponentials and reads go between the products.
+            auto weights = [&](int ks) {
+                u32x4 w;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    const float w0 = exp2_hw(__builtin_fmaf(sv[t][e], sc, -from));
-                    const float w1 = exp2_hw(__builtin_fmaf(sv[t][e + 1], sc, -from));
+                for (int e = 0; e < 8; e += 2) {
+                    const float w0 = exp2_hw(__builtin_fmaf(sv[ks / 2][8 * (ks % 2) + e], sc, -from));
+                    const float w1 = exp2_hw(__builtin_fmaf(sv[ks / 2][8 * (ks % 2) + e + 1], sc, -from));
                     l += w0;
                     l += w1;
-                    w[2 * t + e / 8][(e % 8) / 2] = pack_bf16(w0, w1);
+                    w[e / 2] = pack_bf16(w0, w1);
+                }
+                return w;
+            };
+            bf16x8 vb[2][DB];
+            auto read_values = [&](int ks, bf16x8 (&into)[DB]) {
+#pragma unroll
+                for (int db = 0; db < DB; ++db) into[db] = value(values, db, ks);
+            };
+            read_values(0, vb[0]);
+            u32x4 w = weights(0);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+                u32x4 w_next = w;
+                if (ks < 3) {
+                    read_values(ks + 1, vb[(ks + 1) & 1]);
+                    w_next = weights(ks + 1);
                 }
 #pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(values, db, ks), __builtin_bit_cast(bf16x8, w[ks]), o[db],
-                                                                    0, 0, 0);
+                for (int db = 0; db < DB; ++db) {
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[ks & 1][db], __builtin_bit_cast(bf16x8, w), o[db], 0, 0, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                    if (ks < 3) {
+                        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x402, 36 / DB, 0);
+                    }
+                }
+                w = w_next;
+            }
         }
         if (uniform(s_odd[blk & 1]) == blk + 1) {
             // infinite or NaN values were taken out of this block: a product of the largest finite
@@ -990,6 +1027,7 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
             }
             __syncthreads();
             if (!idle) {
+                lds_char* ones = (lds_char*)value_at(blk) + v_lane;
                 u32x4 w[4];
 #pragma unroll
                 for (int ks = 0; ks < 4; ++ks)
@@ -1002,7 +1040,7 @@ __global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(Att
                 for (int db = 0; db < DB; ++db)
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks)
-                        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(values, db, ks), __builtin_bit_cast(bf16x8, w[ks]),
+                        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(ones, db, ks), __builtin_bit_cast(bf16x8, w[ks]),
                                                                         o[db], 0, 0, 0);
             }
         }
