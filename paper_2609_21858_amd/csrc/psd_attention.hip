@@ -46,8 +46,9 @@ struct Plan {
     int tile_rows;  // rows of a workgroup
     int tiles;      // row tiles of the longest sequence
     int wgs;        // few rows: workgroups of each key/value head
-    int parts;      // many rows: parts of the longest range of cached tokens
-    int chunk;      // many rows: cached tokens of a part
+    bool many;      // many rows: tile_kernel, with
+    int parts;      // parts of the longest range of cached tokens and
+    int chunk;      // cached tokens of a part
     int page_shift; // log2 of the page size, or -1
 };
 
@@ -716,20 +717,21 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
 
 // ---------------------------------------------------------------- many rows
 
-// One workgroup: 128 rows of one (sequence, key/value head), 32 a wave, over one part of its cache.
-// Blocks of 64 tokens go through LDS, which all four waves read: 32x32x16 products, 64 x 32
+// One workgroup: 32 NW rows of one (sequence, key/value head), 32 a wave, over one part of its cache.
+// Blocks of 64 tokens go through LDS, which all waves read: 32x32x16 products, 64 x 32
 // scores a wave in 32 registers, the outputs in D/2 more.  Two buffers, one barrier a block: while
 // block n is computed, block n + 1 is on its way into registers, and is stored behind the
-// arithmetic.  Two workgroups a CU (two waves a SIMD), so one wave's exponentials overlap
-// the other's products.
+// arithmetic.  Two waves a SIMD, so one wave's exponentials overlap the other's products: one
+// workgroup of 8 waves a CU, which loads and stores half as much a row, or two of 4 for fewer rows.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-template <int DP>
+template <int DP, int NW>
 struct TileShape {
     static constexpr int TOK = 64;
-    static constexpr int ROWS = 128;  // of kTileRows
+    static constexpr int NT = 64 * NW;
+    static constexpr int ROWS = 32 * NW;
     static constexpr int LPR = DP / 8;              // 16-byte pieces of a token
-    static constexpr int TPP = kThreads / LPR;      // tokens of one load of the workgroup
+    static constexpr int TPP = NT / LPR;      // tokens of one load of the workgroup
     static constexpr int N = TOK / TPP;             // loads a block
     // Row pitches (elements): 8 lanes reading 16 bytes of 8 consecutive keys, and the 4-token by
     // 64-byte tiles of the transposing reads, fall on different banks.
@@ -737,9 +739,9 @@ struct TileShape {
     static constexpr int BYTES = TOK * (KP + VP) * 2;
 };
 
-template <int DP>
-__global__ __launch_bounds__(kThreads, (DP == 256 ? 1 : 2)) void tile_kernel(AttentionArgs a, Plan p) {
-    using S = TileShape<DP>;
+template <int DP, int NW>
+__global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_kernel(AttentionArgs a, Plan p) {
+    using S = TileShape<DP, NW>;
     constexpr int KK = DP / 16, DB = DP / 32;
     __shared__ __align__(16) char s_mem[2 * S::BYTES];  // two buffers of keys and values
     __shared__ int64_t s_off[4][S::TOK];                // written two blocks ahead, read in two
@@ -1134,7 +1136,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a, Plan p)
 
 constexpr int kMaxParts = 64;     // join_kernel holds a part's weight in a lane
 constexpr int kMinChunk = 256;    // tile_kernel: cached tokens of a part at least
-constexpr int kTileRows = 128;    // rows of a tile_kernel workgroup
+constexpr double kWide = 0.9;    // a block's time in 8 waves of one workgroup to that in 4 of each of two
 constexpr int kCus = 256;
 
 int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
@@ -1143,26 +1145,32 @@ Plan make_plan(const CacheArgs& c, int H, bool bf16, int span) {
     Plan p;
     p.h = H / c.G;
     const long most = (long)c.max_new * p.h;
-    const int limit = c.D > 128 ? 32 : 64;
-    p.tile_rows = most <= 16 ? 16 : most <= 32 ? 32 : bf16 && most > 64 ? kTileRows : limit;
-    p.tiles = (int)((most + p.tile_rows - 1) / p.tile_rows);
+    p.many = bf16 && most > 64;
     p.wgs = p.parts = p.chunk = 0;
-    if (p.tile_rows != kTileRows) {
+    if (!p.many) {
+        const int limit = c.D > 128 ? 32 : 64;
+        p.tile_rows = most <= 16 ? 16 : most <= 32 ? 32 : limit;
+        p.tiles = (int)((most + p.tile_rows - 1) / p.tile_rows);
         p.wgs = std::max(kCus / c.G, 1);  // one a CU
     } else {
-        // Parts of the longest range, by the time they take in 64-token blocks: every round of resident
-        // workgroups takes a part and about 3 blocks to start and end; the join of 2 parts of 512 groups
-        // took as long as 13 blocks.
-        const long groups = (long)c.B * c.G * p.tiles;
-        const long resident = kCus * (c.D > 128 ? 1 : 2);
-        double best = 0;
-        for (int parts = 1; parts <= kMaxParts && (parts - 1) * kMinChunk < span; ++parts) {
-            const int chunk = ((span + parts - 1) / parts + kMinChunk - 1) / kMinChunk * kMinChunk;
-            const double rounds = (double)((groups * parts + resident - 1) / resident);
-            const double cost = rounds * (chunk / 64.0 + 3) + (parts > 1 ? 1.5 + groups * parts * (13.0 / 1024) : 0);
-            if (parts > 1 && cost >= best) continue;
-            best = cost;
-            p.chunk = chunk;
+        // Rows of a workgroup and parts of the longest range, by the time they take in 64-token blocks:
+        // every round of resident workgroups takes a part and about 3 blocks to start and end; the join of
+        // 2 parts of 512 groups of 128 rows took as long as 13 blocks.
+        double best = -1;
+        for (int rows = 128; rows <= (c.D > 128 ? 128 : 256); rows *= 2) {
+            const long tiles = (most + rows - 1) / rows, groups = (long)c.B * c.G * tiles;
+            const long resident = kCus * (c.D > 128 || rows == 256 ? 1 : 2);
+            for (int parts = 1; parts <= kMaxParts && (parts - 1) * kMinChunk < span; ++parts) {
+                const int chunk = ((span + parts - 1) / parts + kMinChunk - 1) / kMinChunk * kMinChunk;
+                const double rounds = (double)((groups * parts + resident - 1) / resident);
+                const double join = parts > 1 ? 1.5 + groups * parts * (rows / 128) * (13.0 / 1024) : 0;
+                const double cost = rounds * (chunk / 64.0 + 3) * (rows == 256 ? kWide : 1.0) + join;
+                if (best >= 0 && cost >= best) continue;
+                best = cost;
+                p.tile_rows = rows;
+                p.tiles = (int)tiles;
+                p.chunk = chunk;
+            }
         }
         p.parts = (span + p.chunk - 1) / p.chunk;
     }
@@ -1190,18 +1198,26 @@ void launch_stream(const AttentionArgs& a, const Plan& p, dim3 grid, hipStream_t
         launch_stream<BF16, DP, false>(a, p, grid, stream);
 }
 
+template <int DP>
+void launch_tiles(const AttentionArgs& a, const Plan& p, dim3 grid, hipStream_t stream) {
+    if (p.tile_rows == 256)
+        hipLaunchKernelGGL((tile_kernel<DP, 8>), grid, dim3(512), 0, stream, a, p);
+    else
+        hipLaunchKernelGGL((tile_kernel<DP, 4>), grid, dim3(256), 0, stream, a, p);
+}
+
 }  // namespace
 
 size_t attention_workspace(const CacheArgs& c, int H, bool bf16) {
     const Plan p = make_plan(c, H, bf16, c.max_kv);
-    if (p.tile_rows != kTileRows)
+    if (!p.many)
         return align256(kCounterFloats * 4 + (size_t)p.wgs * c.G * 2 * p.tile_rows * (padded(c.D) + 2) * 4);
     return p.parts == 1 ? 0 : align256(kCounterFloats * 4 + (size_t)p.parts * c.rows * H * (c.D + 2) * 4);
 }
 
 bool attention_fits(const CacheArgs& c, int H, bool bf16) {
     const Plan p = make_plan(c, H, bf16, c.max_kv);
-    if (p.tile_rows != kTileRows) return (long)c.B * p.tiles * (c.max_kv / kUnit + 2) < 1L << 30;  // units
+    if (!p.many) return (long)c.B * p.tiles * (c.max_kv / kUnit + 2) < 1L << 30;  // units
     return (long)c.B * c.G * p.tiles * p.parts < 1L << 23;
 }
 
@@ -1210,14 +1226,14 @@ hipError_t launch_attention(const AttentionArgs& a, bool bf16, hipStream_t strea
     // a windowed row sees at most `window` positions, a tile's rows together max_new - 1 more
     const int span = a.window > 0 ? (int)std::min<long>(c.max_kv, (long)a.window + c.max_new - 1) : c.max_kv;
     const Plan p = make_plan(c, a.H, bf16, span);
-    const dim3 grid((unsigned)(p.tile_rows == kTileRows ? (long)c.B * c.G * p.tiles * p.parts : (long)p.wgs * c.G));
-    if (p.tile_rows == kTileRows) {
+    const dim3 grid((unsigned)(p.many ? (long)c.B * c.G * p.tiles * p.parts : (long)p.wgs * c.G));
+    if (p.many) {
         if (c.D <= 64)
-            hipLaunchKernelGGL(tile_kernel<64>, grid, dim3(kThreads), 0, stream, a, p);
+            launch_tiles<64>(a, p, grid, stream);
         else if (c.D <= 128)
-            hipLaunchKernelGGL(tile_kernel<128>, grid, dim3(kThreads), 0, stream, a, p);
+            launch_tiles<128>(a, p, grid, stream);
         else
-            hipLaunchKernelGGL(tile_kernel<256>, grid, dim3(kThreads), 0, stream, a, p);
+            hipLaunchKernelGGL((tile_kernel<256, 4>), grid, dim3(256), 0, stream, a, p);
     } else if (bf16) {
         if (c.D <= 64)
             launch_stream<true, 64>(a, p, grid, stream);
