@@ -831,13 +831,15 @@ __global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_
         const uint64_t bits = s_there[blk & 3];
         return (uint64_t)(uint32_t)uniform((int)(uint32_t)bits) | (uint64_t)(uint32_t)uniform((int)(bits >> 32)) << 32;
     };
-    u32x4 kf[S::N], vf[S::N];
-    auto load = [&](int blk) {
+    struct Stage {
+        u32x4 k[S::N], v[S::N];
+    };
+    auto load = [&](int blk, Stage& x) {
 #pragma unroll
         for (int k = 0; k < S::N; ++k) {
             const int64_t at = s_off[blk & 3][k * S::TPP + token] * 2;
-            kf[k] = *(const u32x4*)(k_src + at);
-            vf[k] = *(const u32x4*)(v_src + at);
+            x.k[k] = *(const u32x4*)(k_src + at);
+            x.v[k] = *(const u32x4*)(v_src + at);
         }
     };
     // Does every row of new tokens [lo, hi] see the whole block?
@@ -851,10 +853,10 @@ __global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_
     auto value_at = [&](int blk) { return s_mem + (blk & 1) * S::BYTES + S::TOK * S::KP * 2; };
     // Into LDS.  Where rows differ in what they see, values of tokens that are not there are zeroed
     // and infinite or NaN values taken out (a weight 0 times them is NaN for rows that do not see them).
-    auto store = [&](int blk) {
+    auto store = [&](int blk, Stage& x) {
         if (past)
 #pragma unroll
-            for (int k = 0; k < S::N; ++k) kf[k] = u32x4{0, 0, 0, 0};
+            for (int k = 0; k < S::N; ++k) x.k[k] = u32x4{0, 0, 0, 0};
         if (!whole(blk, i_lo, i_hi)) {
             const uint64_t there = there_of(blk);
             bool odd = false;
@@ -863,12 +865,12 @@ __global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_
                 const bool gone = !((there >> (k * S::TPP + token)) & 1u);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    uint32_t w = gone ? 0u : vf[k][e];
+                    uint32_t w = gone ? 0u : x.v[k][e];
                     const bool lo_odd = odd_lo<true>(w), hi_odd = odd_hi(w);
                     odd |= lo_odd || hi_odd;
                     if (lo_odd) w &= 0xFFFF0000u;
                     if (hi_odd) w &= 0xFFFFu;
-                    vf[k][e] = w;
+                    x.v[k][e] = w;
                 }
             }
             if (odd) s_odd[blk & 1] = blk + 1;
@@ -877,8 +879,8 @@ __global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_
         char* values = value_at(blk);
 #pragma unroll
         for (int k = 0; k < S::N; ++k) {
-            *(u32x4*)(keys + ((k * S::TPP + token) * S::KP + piece * 8) * 2) = kf[k];
-            *(u32x4*)(values + ((k * S::TPP + token) * S::VP + piece * 8) * 2) = vf[k];
+            *(u32x4*)(keys + ((k * S::TPP + token) * S::KP + piece * 8) * 2) = x.k[k];
+            *(u32x4*)(values + ((k * S::TPP + token) * S::VP + piece * 8) * 2) = x.v[k];
         }
     };
     // this lane's dimension of 32 db + .., tokens 16 ks + {4 hi .., 8 + 4 hi ..}, as an A operand
@@ -895,19 +897,28 @@ __global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_
         return v.all;
     };
 
-    if (wave == 0) publish(0, page_of(0));
-    int page = page_of(1);
+    // Blocks on their way into registers: one, or two where a workgroup of 8 waves has the registers (a block
+    // takes it about as long as memory takes to answer).
+    constexpr int AHEAD = NW == 8 ? 2 : 1;
     if (tid < 2) s_odd[tid] = 0;
+    int page = 0;
+#pragma unroll
+    for (int n = 0; n <= AHEAD; ++n) {
+        page = page_of(n);
+        if (wave == 0) publish(n, page);
+    }
+    page = page_of(AHEAD + 1);
     __syncthreads();
-    load(0);
-    if (wave == 0) publish(1, page);
-    page = page_of(2);
-    if (blocks > 0) store(0);
-    for (int blk = 0; blk < blocks; ++blk) {
+    Stage first, second;
+    load(0, first);
+    if (blocks > 0) store(0, first);
+    if (AHEAD == 2) load(1, first);
+    // Block `blk`, which is in LDS, while `into` is loaded; then block blk + 1 goes from `from` into LDS.
+    auto step = [&](int blk, Stage& from_stage, Stage& into) {
         __syncthreads();
         const int j0 = c0 + blk * S::TOK;
         const bool more = blk + 1 < blocks;
-        load(blk + 1);  // (past the end: the pool's first tokens, which nothing uses)
+        load(blk + AHEAD, into);  // (past the end: the pool's first tokens, which nothing uses)
         const bool seen_by_all = whole(blk, w_lo, w_hi);
         const uint64_t there = there_of(blk);
         // nothing of the block lies before this wave's last row's end (or behind its window)
@@ -1001,10 +1012,6 @@ __global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_
                 for (int db = 0; db < DB; ++db) {
                     o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[ks & 1][db], __builtin_bit_cast(bf16x8, w), o[db], 0, 0, 0);
                     __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                    if (ks < 3) {
-                        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-                        __builtin_amdgcn_sched_group_barrier(0x402, 36 / DB, 0);
-                    }
                 }
                 w = w_next;
             }
@@ -1046,9 +1053,13 @@ __global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_
                                                                         o[db], 0, 0, 0);
             }
         }
-        if (more) store(blk + 1);
-        if (wave == 0) publish(blk + 2, page);
-        page = page_of(blk + 3);
+        if (more) store(blk + 1, from_stage);
+        if (wave == 0) publish(blk + 1 + AHEAD, page);
+        page = page_of(blk + 2 + AHEAD);
+    };
+    for (int blk = 0; blk < blocks; blk += AHEAD) {
+        step(blk, first, AHEAD == 2 ? second : first);
+        if (AHEAD == 2 && blk + 1 < blocks) step(blk + 1, second, first);
     }
 
     l += __shfl_xor(l, 32);
