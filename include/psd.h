@@ -523,7 +523,7 @@ psd_status psd_kv_keep(const psd_cache *cache, const psd_seqs *seqs, const int32
  *   target_lse     device [B][gamma+1] float32, nullable;  draft_lse [B][gamma], nullable
  *   workspace      device, psd_verify_given_workspace_bytes(), 256-byte aligned; needs no
  *                  clearing; one call at a time
- * batch * (2 gamma + 1) is at most 2^23.  Two launches. */
+ * batch * (2 gamma + 1) is at most 2^23.  One launch for few short rows, else two. */
 psd_status psd_verify_given(const psd_params *params, int32_t batch, int32_t gamma, const void *target_logits,
                             const void *draft_logits, const int32_t *draft_tokens, const int32_t *n_drafts,
                             const float *u, const float *e, int32_t *out_tokens, int32_t *out_len, float *target_lse,

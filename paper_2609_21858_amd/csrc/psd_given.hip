@@ -5,7 +5,7 @@
 // r = max(p_n - q_n, 0) at a refusal and r = p_n after all drafts.  The residual's total is
 // not needed: the race is invariant to scale.
 //
-// Two launches.  given_stream_kernel reads every row once (memory bounds it: (2 gamma + 1) V
+// Two launches (one for few short rows, see kWhole).  given_stream_kernel reads every row once (memory bounds it: (2 gamma + 1) V
 // elements a sequence) and leaves each segment's maximum and sum of exponentials.
 // given_race_kernel merges them (every workgroup again: a few hundred values), finds the
 // first refusal and races one segment of the one row that decides, whose logits the
@@ -116,38 +116,27 @@ __device__ __forceinline__ void merge(float& m, float& s, float m2, float s2, fl
     m = top;
 }
 
-// Rows [0, B (gamma + 1)) are the target's, the others the drafts'.
+// Maximum and sum of 2^((l - maximum) c) over [lo, hi) of the row at `at`, by `threads` threads of which
+// this is number `me`: this thread's share.
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void given_stream_kernel(GivenArgs a, Layout L) {
+__device__ __forceinline__ void row_share(const void* base, int64_t at, int lo, int hi, int me, int threads, float c, float& m,
+                                          float& s) {
     constexpr int VEC = Elem<BF16>::kVec;
     constexpr int U = 4;  // loads in flight before the first is used
-    const int row = blockIdx.x / L.nseg, part = blockIdx.x - row * L.nseg;
-    const int targets = a.B * (a.gamma + 1);
-    const bool target = row < targets;
-    const void* base = target ? a.target : a.draft;
-    const int64_t at = (int64_t)(target ? row : row - targets) * a.V;
-    const float c = kLog2e / (target ? a.T_target : a.T_draft);
-    const int lo = part * L.seg, hi = min(lo + L.seg, a.V);
-    const int tid = threadIdx.x;
-    char* ws = (char*)a.workspace;
-    if (part == 0 && tid == 0 && row < a.B) {
-        // the race's slot and counter of sequence `row`: written before its launch begins
-        ((unsigned long long*)(ws + L.best))[row] = kNone;
-        ((unsigned*)(ws + L.count))[row] = 0;
-    }
-    float m = kNoLogit, s = 0.f;
-    for (int v0 = lo + tid * VEC; v0 < hi; v0 += U * kThreads * VEC) {
+    m = kNoLogit;
+    s = 0.f;
+    for (int v0 = lo + me * VEC; v0 < hi; v0 += U * threads * VEC) {
         u32x4 w[U];
         float x[U][VEC];
         float top = kNoLogit;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            const int v = v0 + k * kThreads * VEC;
+            const int v = v0 + k * threads * VEC;
             if (v + VEC <= hi) w[k] = load_any<BF16>(base, at + v);
         }
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            const int v = v0 + k * kThreads * VEC;
+            const int v = v0 + k * threads * VEC;
             if (v + VEC <= hi) {
                 Elem<BF16>::widen(w[k], x[k]);
             } else {
@@ -168,6 +157,25 @@ __global__ __launch_bounds__(kThreads) void given_stream_kernel(GivenArgs a, Lay
                 for (int j = 0; j < VEC; ++j) s += exp2_hw((x[k][j] - m) * c);
         }
     }
+}
+
+// Rows [0, B (gamma + 1)) are the target's, the others the drafts'.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void given_stream_kernel(GivenArgs a, Layout L) {
+    const int row = blockIdx.x / L.nseg, part = blockIdx.x - row * L.nseg;
+    const int targets = a.B * (a.gamma + 1);
+    const bool target = row < targets;
+    const float c = kLog2e / (target ? a.T_target : a.T_draft);
+    const int lo = part * L.seg, hi = min(lo + L.seg, a.V);
+    const int tid = threadIdx.x;
+    char* ws = (char*)a.workspace;
+    if (part == 0 && tid == 0 && row < a.B) {
+        // the race's slot and counter of sequence `row`: written before its launch begins
+        ((unsigned long long*)(ws + L.best))[row] = kNone;
+        ((unsigned*)(ws + L.count))[row] = 0;
+    }
+    float m, s;
+    row_share<BF16>(target ? a.target : a.draft, (int64_t)(target ? row : row - targets) * a.V, lo, hi, tid, kThreads, c, m, s);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) merge(m, s, __shfl_xor(m, o), __shfl_xor(s, o), c);
     __shared__ float s_m[kWaves], s_s[kWaves];
@@ -184,9 +192,15 @@ __global__ __launch_bounds__(kThreads) void given_stream_kernel(GivenArgs a, Lay
 
 constexpr int kMaxRows = 2 * 32 + 1;
 constexpr int kRaceUnroll = 2;  // 16-byte pieces of a row that a thread scores between two exchanges
-// Relative error assumed of a probability from the hardware's exponential: (l - max) / T up to
-// 100 in units of ln 2 errs by 100 2^-24 from the product, and a few 2^-24 from the rest.
-constexpr float kErr = 2e-5f;
+// Relative error assumed of a probability from the hardware's exponential: (l - max) / T is at most 149 in
+// units of ln 2 (a float's range) and errs by 3 2^-24 of itself, 2e-5 in the probability at most.
+constexpr float kErr = 4e-5f;
+// Elements of a sequence's rows up to which one workgroup does all of it in one launch, while there is a CU
+// for each sequence (V=1024, gamma=4, from Python: 15.5 us and 18.0 us in two launches up to 64 sequences,
+// 27.0 and 20.9 us with 512).
+constexpr long kWhole = 32768;
+constexpr int kWholeBatch = 256;
+constexpr int kWholeThreads = 1024;
 
 // Full-precision scores of tokens of the row that decides, as (score bits, token): scores
 // are positive, so their bits order them, and equal ones go to the lowest token.
@@ -202,12 +216,14 @@ struct RaceRow {
     }
 };
 
-template <bool BF16>
-__global__ __launch_bounds__(kThreads, 4) void given_race_kernel(GivenArgs a, Layout L) {
+// WHOLE: a workgroup a sequence, which also reads its rows.  Otherwise a workgroup a segment of the race.
+template <bool BF16, bool WHOLE>
+__global__ __launch_bounds__(WHOLE ? kWholeThreads : kThreads, WHOLE ? 1 : 4) void given_race_kernel(GivenArgs a, Layout L) {
     constexpr int VEC = Elem<BF16>::kVec;
+    constexpr int NT = WHOLE ? kWholeThreads : kThreads, NW = NT / 64;
     __shared__ float s_top[kMaxRows], s_sum[kMaxRows];
     __shared__ int s_taken;
-    __shared__ unsigned long long s_best[kWaves];
+    __shared__ unsigned long long s_best[NW];
     const int b = blockIdx.x / L.rseg, part = blockIdx.x - b * L.rseg;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int g = a.gamma;
@@ -236,7 +252,7 @@ __global__ __launch_bounds__(kThreads, 4) void given_race_kernel(GivenArgs a, La
         for (int k = 0; k < kRaceUnroll; ++k)
 #pragma unroll
             for (int j = 0; j < VEC; j += 4) {
-                const int v = v0 + k * kThreads * VEC;
+                const int v = v0 + k * NT * VEC;
                 if (v + VEC <= hi)
                     we[k][j / 4] = load_any<false>(a.e, (int64_t)b * a.V + v + j);
                 else
@@ -246,19 +262,24 @@ __global__ __launch_bounds__(kThreads, 4) void given_race_kernel(GivenArgs a, La
     load_e(lo + tid * VEC);
 
     // Every row of the sequence: rows [0, g] the target's, [g + 1, 2 g] the drafts'.  A row's segments
-    // lie on neighbouring lanes, 2^L.lanes of them.
-    const int row_lanes = 1 << L.lanes;
-    for (int r0 = 0; r0 < 2 * g + 1; r0 += kThreads >> L.lanes) {
-        const int r = r0 + (tid >> L.lanes), at = tid & (row_lanes - 1);
+    // lie on neighbouring lanes, 2^L.lanes of them; a whole row on all of a wave's.
+    const int row_lanes = WHOLE ? 64 : 1 << L.lanes;
+    for (int r0 = 0; r0 < 2 * g + 1; r0 += NT / row_lanes) {
+        const int r = r0 + tid / row_lanes, at = tid & (row_lanes - 1);
         const bool target = r <= g;
         const float T = target ? a.T_target : a.T_draft;
         const float c = kLog2e / T;
         const int64_t row = target ? (int64_t)b * (g + 1) + r : targets + (int64_t)b * g + (r - g - 1);
+        const int64_t to = target ? row : row - targets;  // among the target's or the drafts' rows
         float m = kNoLogit, s = 0.f;
-        if (r < 2 * g + 1 && at < L.nseg) {
-            const float2 v = parts[row * L.nseg + at];
-            m = v.x;
-            s = v.y;
+        if (r < 2 * g + 1) {
+            if constexpr (WHOLE) {
+                row_share<BF16>(target ? a.target : a.draft, to * a.V, 0, a.V, lane, 64, c, m, s);
+            } else if (at < L.nseg) {
+                const float2 v = parts[row * L.nseg + at];
+                m = v.x;
+                s = v.y;
+            }
         }
         for (int o = row_lanes / 2; o > 0; o >>= 1) merge(m, s, __shfl_xor(m, o), __shfl_xor(s, o), c);
         if (at == 0 && r < 2 * g + 1) {
@@ -266,7 +287,6 @@ __global__ __launch_bounds__(kThreads, 4) void given_race_kernel(GivenArgs a, La
             s_sum[r] = m == kNoLogit ? 0.f : s;
             if (part == 0) {
                 float* out = target ? a.target_lse : a.draft_lse;
-                const int64_t to = target ? row : row - targets;
                 if (out) out[to] = m == kNoLogit ? kNoLogit : m / T + logf(s);
             }
         }
@@ -317,13 +337,13 @@ __global__ __launch_bounds__(kThreads, 4) void given_race_kernel(GivenArgs a, La
             const float up = e * __builtin_amdgcn_rcpf(r - err) * (1.f + kErr);
             if (r - err > 0.f) high = fminf(high, up);
         };
-        for (int v0 = lo + tid * VEC; v0 - tid * VEC < hi; v0 += kRaceUnroll * kThreads * VEC) {
+        for (int v0 = lo + tid * VEC; v0 - tid * VEC < hi; v0 += kRaceUnroll * NT * VEC) {
             float low[kRaceUnroll];  // of each piece: its smallest lower bound
             float high = __builtin_inff();
             u32x4 wp[kRaceUnroll], wq[kRaceUnroll];
 #pragma unroll
             for (int k = 0; k < kRaceUnroll; ++k) {
-                const int v = v0 + k * kThreads * VEC;
+                const int v = v0 + k * NT * VEC;
                 wq[k] = u32x4{0, 0, 0, 0};
                 if (v + VEC <= hi) {
                     wp[k] = load_any<BF16>(a.target, row.at_p + v);
@@ -352,7 +372,7 @@ __global__ __launch_bounds__(kThreads, 4) void given_race_kernel(GivenArgs a, La
 #pragma unroll
             for (int k = 0; k < kRaceUnroll; ++k)
                 if (low[k] <= high) {
-                    const int v = v0 + k * kThreads * VEC;
+                    const int v = v0 + k * NT * VEC;
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) {
                         const float lp = pick<BF16>(wp[k], j), lq = pick<BF16>(wq[k], j);
@@ -362,38 +382,45 @@ __global__ __launch_bounds__(kThreads, 4) void given_race_kernel(GivenArgs a, La
                         if (down <= high && v + j < hi) best = min(best, row.key(row.p(lp) - row.q(lq), e, v + j));
                     }
                 }
-            load_e(v0 + kRaceUnroll * kThreads * VEC);
+            load_e(v0 + kRaceUnroll * NT * VEC);
         }
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) best = min(best, (unsigned long long)__shfl_xor((long long)best, o));
     if (lane == 0) s_best[wave] = best;
     __syncthreads();
-    __shared__ int s_last;
-    unsigned long long* slot = (unsigned long long*)(ws + L.best) + b;
-    if (tid == 0) {
-        for (int w = 1; w < kWaves; ++w) best = min(best, s_best[w]);
-        // A minimum does not depend on the order of the workgroups.  Its returned value is waited for,
-        // so it has taken place when the count goes up: the workgroup that counts last reads
-        // the minimum of all.  Nothing else passes between them, and no fence is needed, which
-        // would empty the caches that the other workgroups stream through.
-        const unsigned long long was = __hip_atomic_fetch_min(slot, best, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        asm volatile("" ::"v"(was) : "memory");
-        const unsigned before = __hip_atomic_fetch_add((unsigned*)(ws + L.count) + b, 1u, __ATOMIC_RELAXED,
-                                                       __HIP_MEMORY_SCOPE_AGENT);
-        s_last = before == (unsigned)(L.rseg - 1);
+    unsigned long long won;
+    if constexpr (WHOLE) {
+        won = s_best[0];
+        for (int w = 1; w < NW; ++w) won = min(won, s_best[w]);
+    } else {
+        __shared__ int s_last;
+        unsigned long long* slot = (unsigned long long*)(ws + L.best) + b;
+        if (tid == 0) {
+            for (int w = 1; w < NW; ++w) best = min(best, s_best[w]);
+            // A minimum does not depend on the order of the workgroups.  Its returned value is waited for,
+            // so it has taken place when the count goes up: the workgroup that counts last reads
+            // the minimum of all.  Nothing else passes between them, and no fence is needed, which
+            // would empty the caches that the other workgroups stream through.
+            const unsigned long long was = __hip_atomic_fetch_min(slot, best, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            asm volatile("" ::"v"(was) : "memory");
+            const unsigned before = __hip_atomic_fetch_add((unsigned*)(ws + L.count) + b, 1u, __ATOMIC_RELAXED,
+                                                           __HIP_MEMORY_SCOPE_AGENT);
+            s_last = before == (unsigned)(L.rseg - 1);
+        }
+        __syncthreads();
+        if (!s_last) return;
+        won = __hip_atomic_fetch_min(slot, kNone, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    __syncthreads();
-    if (!s_last) return;
-    unsigned long long won = __hip_atomic_fetch_min(slot, kNone, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (won == kNone && residual && row.sum_p > 0.f) {
         // a refusal with p <= q everywhere (rounding: two rows nearly the same): the race over p
-        for (int v = tid; v < a.V; v += kThreads) won = min(won, row.key(row.p(load_one<BF16>(a.target, row.at_p + v)), a.e[row.at_e + v], v));
+        for (int v = tid; v < a.V; v += NT) won = min(won, row.key(row.p(load_one<BF16>(a.target, row.at_p + v)), a.e[row.at_e + v], v));
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) won = min(won, (unsigned long long)__shfl_xor((long long)won, o));
+        __syncthreads();
         if (lane == 0) s_best[wave] = won;
         __syncthreads();
-        for (int w = 0; w < kWaves; ++w) won = min(won, s_best[w]);
+        for (int w = 0; w < NW; ++w) won = min(won, s_best[w]);
     }
     if (tid <= g) {
         int token = -1;
@@ -406,19 +433,29 @@ __global__ __launch_bounds__(kThreads, 4) void given_race_kernel(GivenArgs a, La
     }
 }
 
+bool given_whole(int B, int gamma, int V) { return B <= kWholeBatch && (2L * gamma + 1) * V <= kWhole; }
+
 }  // namespace
 
 size_t given_workspace(int B, int gamma, int V, bool bf16) { return layout(B, gamma, V, bf16).total; }
 
 hipError_t launch_given(const GivenArgs& a, bool bf16, hipStream_t stream) {
-    const Layout L = layout(a.B, a.gamma, a.V, bf16);
+    Layout L = layout(a.B, a.gamma, a.V, bf16);
+    if (given_whole(a.B, a.gamma, a.V)) L.rseg = 1, L.rlen = a.V;
+    if (given_whole(a.B, a.gamma, a.V)) {
+        if (bf16)
+            hipLaunchKernelGGL((given_race_kernel<true, true>), dim3(a.B), dim3(kWholeThreads), 0, stream, a, L);
+        else
+            hipLaunchKernelGGL((given_race_kernel<false, true>), dim3(a.B), dim3(kWholeThreads), 0, stream, a, L);
+        return hipGetLastError();
+    }
     const dim3 stream_grid((unsigned)L.rows * L.nseg), race_grid((unsigned)a.B * L.rseg);
     if (bf16) {
         hipLaunchKernelGGL(given_stream_kernel<true>, stream_grid, dim3(kThreads), 0, stream, a, L);
-        hipLaunchKernelGGL(given_race_kernel<true>, race_grid, dim3(kThreads), 0, stream, a, L);
+        hipLaunchKernelGGL((given_race_kernel<true, false>), race_grid, dim3(kThreads), 0, stream, a, L);
     } else {
         hipLaunchKernelGGL(given_stream_kernel<false>, stream_grid, dim3(kThreads), 0, stream, a, L);
-        hipLaunchKernelGGL(given_race_kernel<false>, race_grid, dim3(kThreads), 0, stream, a, L);
+        hipLaunchKernelGGL((given_race_kernel<false, false>), race_grid, dim3(kThreads), 0, stream, a, L);
     }
     return hipGetLastError();
 }
