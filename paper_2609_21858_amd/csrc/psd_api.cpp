@@ -1202,8 +1202,8 @@ psd_status psd_attention(const psd_cache* cache, const psd_seqs* seqs, const psd
     if (!psd::attention_fits(a.c, q_heads, bf16) || (long)seqs->rows * q_heads / 4 >= kMaxGrid)
         return fail(PSD_E_ARG, "call too large: batch %d, rows %d, max_new %d", seqs->batch, seqs->rows, seqs->max_new);
     const size_t need = psd::attention_workspace(a.c, q_heads, bf16);
-    if (need > 0) {
-        if (!workspace) return fail(PSD_E_WORKSPACE, "workspace is NULL");
+    if (need > 0 && !workspace) return fail(PSD_E_WORKSPACE, "workspace is NULL");
+    if (workspace) {
         if (((uintptr_t)workspace & 255u) != 0) return fail(PSD_E_WORKSPACE, "workspace must be 256-byte aligned");
         if (workspace_bytes < need) return fail(PSD_E_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
     }
@@ -1211,11 +1211,12 @@ psd_status psd_attention(const psd_cache* cache, const psd_seqs* seqs, const psd
     a.out = rows_args(out);
     a.H = q_heads;
     a.scale = scale;
-    a.window = window;
+    a.window = std::min<int32_t>(window, PSD_MAX_KV);  // wider ones see no more
     a.mask = mask;
     a.mask_words = mask ? mask_words : 0;
     a.lse = lse;
     a.workspace = workspace;
+    a.workspace_bytes = workspace ? workspace_bytes : 0;
     const hipError_t e = psd::launch_attention(a, bf16, stream);
     if (e != hipSuccess) return hip_fail(e, "attention kernel launch");
     return PSD_OK;

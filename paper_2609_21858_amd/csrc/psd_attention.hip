@@ -201,7 +201,7 @@ constexpr int join_units() {
 // Values that are the same in all lanes, into scalar registers.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ Seq uniform(const Seq& s) {
-    return Seq{uniform(s.row0), uniform(s.n), uniform(s.first), uniform(s.kv)};
+    return Seq{uniform(s.row0), uniform(s.n), uniform(s.first), uniform(s.kv), uniform(s.total)};
 }
 
 // A value anew, so that what rare code computes from it is not kept in registers through the common.
@@ -1219,12 +1219,17 @@ void launch_tiles(const AttentionArgs& a, const Plan& p, dim3 grid, hipStream_t 
 
 }  // namespace
 
-size_t attention_workspace(const CacheArgs& c, int H, bool bf16) {
-    const Plan p = make_plan(c, H, bf16, c.max_kv);
+namespace {
+
+size_t plan_bytes(const Plan& p, const CacheArgs& c, int H) {
     if (!p.many)
         return align256(kCounterFloats * 4 + (size_t)p.wgs * c.G * 2 * p.tile_rows * (padded(c.D) + 2) * 4);
     return p.parts == 1 ? 0 : align256(kCounterFloats * 4 + (size_t)p.parts * c.rows * H * (c.D + 2) * 4);
 }
+
+}  // namespace
+
+size_t attention_workspace(const CacheArgs& c, int H, bool bf16) { return plan_bytes(make_plan(c, H, bf16, c.max_kv), c, H); }
 
 bool attention_fits(const CacheArgs& c, int H, bool bf16) {
     const Plan p = make_plan(c, H, bf16, c.max_kv);
@@ -1236,7 +1241,9 @@ hipError_t launch_attention(const AttentionArgs& a, bool bf16, hipStream_t strea
     const CacheArgs& c = a.c;
     // a windowed row sees at most `window` positions, a tile's rows together max_new - 1 more
     const int span = a.window > 0 ? (int)std::min<long>(c.max_kv, (long)a.window + c.max_new - 1) : c.max_kv;
-    const Plan p = make_plan(c, a.H, bf16, span);
+    Plan p = make_plan(c, a.H, bf16, span);
+    // the caller's workspace is sized for max_kv: a window's parts may want more of it than there is
+    if (plan_bytes(p, c, a.H) > a.workspace_bytes) p = make_plan(c, a.H, bf16, c.max_kv);
     const dim3 grid((unsigned)(p.many ? (long)c.B * c.G * p.tiles * p.parts : (long)p.wgs * c.G));
     if (p.many) {
         if (c.D <= 64)

@@ -253,7 +253,7 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KeepArgs a, int vec,
     int from = tid < min(kKeepPlaces, a.keep_width) ? keep[tid] : -1;
     const int kept = a.n_keep[b];
     const Seq s = load_seq(c, b);
-    const int total = max(c.new_start[b + 1] - max(c.new_start[b], 0), 0);
+    const int total = s.total;
     const int n = max(min(min(kept, a.keep_width), total), 0);
     if (layer == 0 && part == 0 && tid == 0 && a.kv_out) a.kv_out[b] = s.first + n;
     const int32_t* table = c.table + (int64_t)b * c.table_stride;

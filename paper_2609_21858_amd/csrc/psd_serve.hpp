@@ -62,6 +62,7 @@ struct AttentionArgs {
     int mask_words;
     float* lse;
     void* workspace;
+    size_t workspace_bytes;
 };
 size_t attention_workspace(const CacheArgs& c, int H, bool bf16);
 bool attention_fits(const CacheArgs& c, int H, bool bf16);  // the launch stays inside a grid's limits

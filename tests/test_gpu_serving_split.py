@@ -137,3 +137,61 @@ def test_append_of_many_rows(psd, interleaved, R, dtype):
     assert torch.equal(pools[0], pools[2]) and torch.equal(pools[1], pools[3]) and torch.equal(queries[0], queries[1])
     seq = table[0].long()
     assert torch.equal(pools[1][seq].reshape(-1, G, D)[:n], x[:, H + G:])
+
+
+@pytest.mark.parametrize("rows,kv", [(40, 2000), (70, 4000), (600, 5000), (2048, 6000)])
+def test_workspace_of_windowed_calls(psd, rows, kv):
+    """A window's parts stay inside the workspace that the bounds without it ask for."""
+    H, G, D, P = 8, 2, 128, 64
+    g = torch.Generator(device="cuda").manual_seed(3)
+    width = -(-kv // P)
+    k = torch.randn((width, P, G, D), device="cuda", generator=g).to(BF16)
+    cache = psd.make_cache(k, k.clone())
+    table = torch.arange(width, device="cuda", dtype=torch.int32)[None].contiguous()
+    seqs = psd.make_seqs(torch.tensor([0, rows], dtype=torch.int32).cuda(), torch.tensor([kv], dtype=torch.int32).cuda(), table,
+                         rows, rows, kv)
+    q = torch.randn((rows, H, D), device="cuda", generator=g).to(BF16)
+    need = psd.attention_workspace_bytes(cache, seqs, H)
+    whole = torch.zeros(need + (1 << 20), dtype=torch.uint8, device="cuda")
+    whole[need:] = 0x5A
+    roomy = torch.zeros(256 << 20, dtype=torch.uint8, device="cuda")
+    for window in (1, 64, 300, 1000, 1900, 3000, 1 << 30, (1 << 31) - 1):
+        a = psd.attention(cache, seqs, q, whole[:need] if need else None, window=window)["out"]
+        b = psd.attention(cache, seqs, q, roomy, window=window)["out"]
+        assert bool((whole[need:] == 0x5A).all()), window
+        assert float((a.float() - b.float()).abs().max()) < 0.05 and bool(torch.isfinite(a.float()).all()), window
+    # a window wider than the cache is none
+    assert float((psd.attention(cache, seqs, q, roomy)["out"].float() - b.float()).abs().max()) < 0.05
+
+
+@TYPES
+@pytest.mark.parametrize("rows", [2, 90])
+def test_lengths_that_no_call_can_have(psd, rows, dtype):
+    """Lengths outside every bound are cut: such a sequence's rows see nothing or the bounded cache, the others are
+    what they are."""
+    s = ref.Sequences([(rows, 100), (rows, 150), (rows, 120)], 2, 64, 16, dtype)
+    q = torch.randn((3 * rows, 4, 64), generator=s.gen).to(dtype)
+    want, *_ = ref.attention(s, q, 0.125)
+    cache, seqs, dk, dv = s.handles(psd)
+    ws = psd.new_attention_workspace(cache, seqs, 4)
+    starts, kv_len, table = seqs.tensors
+    for bad in (-1, -(1 << 31), (1 << 31) - 1, 0):
+        kv = kv_len.clone()
+        kv[1] = bad
+        odd = psd.make_seqs(starts, kv, table, 3 * rows, rows, 150)
+        for window, mask in ((0, None), (40, None), ((1 << 31) - 1, None), (0, torch.zeros((3 * rows, 1), dtype=torch.int32, device="cuda"))):
+            got = psd.attention(cache, odd, q.cuda(), ws, scale=0.125, window=window, mask=mask)["out"].cpu().double()
+            if bad <= 0:
+                assert bool((got[rows:2 * rows] == 0).all())
+            if window != 40 and mask is None:
+                tol = 0.03 if dtype == BF16 else 1e-4
+                assert float((got[:rows] - want[:rows]).abs().max()) < tol
+                assert float((got[2 * rows:] - want[2 * rows:]).abs().max()) < tol
+    # starts past the rows and out of order: the rows that are there are those of sequences that hold them
+    odd = psd.make_seqs(torch.tensor([0, rows, 1 << 30, (1 << 31) - 1], dtype=torch.int32).cuda(), kv_len, table, 3 * rows, rows, 150)
+    got = psd.attention(cache, odd, q.cuda(), ws, scale=0.125)["out"].cpu().double()
+    assert float((got[:rows] - want[:rows]).abs().max()) < (0.03 if dtype == BF16 else 1e-4)
+    k = torch.zeros((3 * rows, 2, 64), dtype=dtype, device="cuda")
+    psd.kv_append(cache, odd, k, k)
+    psd.kv_keep(cache, odd, torch.zeros((3, 1), dtype=torch.int32, device="cuda"), torch.ones(3, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
