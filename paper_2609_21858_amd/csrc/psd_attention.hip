@@ -901,13 +901,13 @@ __global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_
     // takes it about as long as memory takes to answer).
     constexpr int AHEAD = NW == 8 ? 2 : 1;
     if (tid < 2) s_odd[tid] = 0;
-    int page = 0;
+    int pages[AHEAD + 2];
 #pragma unroll
-    for (int n = 0; n <= AHEAD; ++n) {
-        page = page_of(n);
-        if (wave == 0) publish(n, page);
-    }
-    page = page_of(AHEAD + 1);
+    for (int n = 0; n < AHEAD + 2; ++n) pages[n] = page_of(n);
+    if (wave == 0)
+#pragma unroll
+        for (int n = 0; n <= AHEAD; ++n) publish(n, pages[n]);
+    int page = pages[AHEAD + 1];
     __syncthreads();
     Stage first, second;
     load(0, first);
@@ -1128,13 +1128,27 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a, Plan p)
 #pragma unroll
     for (int k = 32; k > 0; k >>= 1) total += __shfl_xor(total, k);
     if (mine.y != mine.y) total = mine.y;
-    const int d = lane * 4;
+    // 4 dimensions a lane, and the parts in turn over what groups of lanes that leaves, four loads in flight each
+    const int span = c.D <= 64 ? 16 : c.D <= 128 ? 32 : 64, groups = 64 / span;
+    const int d = lane % span * 4, group = lane / span;
+    const float* src = (const float*)a.workspace + kCounterFloats + item * c.D + min(d, c.D - 4);
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < n_parts; ++k) {
-        const float w = __shfl(by, k);
-        if (d < c.D && w != 0.f) o += *(const f32x4*)((const float*)a.workspace + kCounterFloats + (k * step + item) * c.D + d) * w;
+    for (int k0 = 0; k0 < n_parts; k0 += 4 * groups) {
+        f32x4 x[4];
+        float w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int k = k0 + i * groups + group;
+            x[i] = *(const f32x4*)(src + min(k, n_parts - 1) * step * c.D);
+            w[i] = __shfl(by, min(k, 63));  // 0 past the parts
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o += x[i] * w[i];
     }
-    if (d < c.D) {
+    for (int k = span; k < 64; k <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], k);
+    if (group == 0 && d < c.D) {
         const f32x4 y = top == kNoScore ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.f / total);
         char* dst = (char*)a.out.data + ((int64_t)t * a.out.stride_row + (int64_t)head * a.out.stride_head + d) * E::kBytes;
         if constexpr (BF16)
@@ -1159,7 +1173,9 @@ Plan make_plan(const CacheArgs& c, int H, bool bf16, int span) {
     p.many = bf16 && most > 64;
     p.wgs = p.parts = p.chunk = 0;
     if (!p.many) {
-        const int limit = c.D > 128 ? 32 : 64;
+        // float32 rows in tiles of 32 while tiles of 64 would leave CUs without one
+        const bool few = !bf16 && c.D > 64 && (long)c.B * c.G * ((most + 63) / 64) < kCus;
+        const int limit = c.D > 128 || few ? 32 : 64;
         p.tile_rows = most <= 16 ? 16 : most <= 32 ? 32 : limit;
         p.tiles = (int)((most + p.tile_rows - 1) / p.tile_rows);
         p.wgs = std::max(kCus / c.G, 1);  // one a CU
