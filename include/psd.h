@@ -472,7 +472,8 @@ psd_status psd_kv_append(const psd_cache *cache, const psd_seqs *seqs, const psd
  *               behind one root share the cache and one call (target_rows = K).
  * A row that sees nothing gives zeros and lse -inf.  Positions no row sees are not read,
  * and a masked or unseen token's key and value change nothing, NaN and infinities
- * included.  A score of +inf or NaN that a row does see gives that row NaN.
+ * included.  A score of +inf or NaN that a row does see gives that row NaN, an infinite or
+ * NaN value gives no finite number in that element (which of them is not defined).
  *   q, out     [T][H][D] (dtype); out may be q itself
  *   lse        device [T][H] float32, nullable
  *   mask       device [T][mask_words] uint32, nullable

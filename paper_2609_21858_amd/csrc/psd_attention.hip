@@ -94,13 +94,6 @@ __device__ __forceinline__ uint32_t row_bits(const AttentionArgs& a, const Seq& 
     return bits;
 }
 
-__device__ __forceinline__ int64_t token_offset(const CacheArgs& c, const Plan& p, const int32_t* table, int j) {
-    const int pi = p.page_shift >= 0 ? j >> p.page_shift : j / c.P;
-    const int page = table[pi];
-    if ((unsigned)page >= (unsigned)c.pages) return -1;
-    return (int64_t)page * c.stride_page + (int64_t)(j - pi * c.P) * c.stride_token;
-}
-
 // Infinite or NaN: the upper (float32: the) element of a word, and the lower one of two bfloat16.
 __device__ __forceinline__ bool odd_hi(uint32_t w) { return (w & 0x7F800000u) == 0x7F800000u; }
 template <bool BF16>
@@ -109,6 +102,12 @@ __device__ __forceinline__ bool odd_lo(uint32_t w) {
 }
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Sums of weights with maxima m and m2 as one with maximum `top` of both.  Maxima pass over NaN, sums do
+// not: a row that sees nothing but NaN scores has no maximum and a NaN sum, one that sees nothing sum 0.
+__device__ __forceinline__ float add_sums(float l, float m, float l2, float m2, float top) {
+    return top == kNoScore ? l + l2 : l * exp2_hw(m - top) + l2 * exp2_hw(m2 - top);
+}
 
 // acc += A B of 16 x 16 results: 16 bytes of A's row and of B's column from each lane (32 products
 // a result in bfloat16, 16 in float32, where element e of all lanes makes one instruction).
@@ -306,412 +305,411 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
     char* s_v = s_mem + wave * S::V_BYTES;
 
     for (int n_units; before < u1; before += n_units, ++item) {
-    const Seq s = uniform(each == 1 ? s_seq[item] : seq_at(item));
-    n_units = each == 1 ? uniform(s_units[item + 1]) - before : uniform(units_at(item, s));
-    if (before + n_units <= u0) continue;
-    const int b = item / p.tiles, tile = item - b * p.tiles;
-    const int row0 = tile * p.tile_rows;
-    const int rows = min(s.n * p.h - row0, p.tile_rows);
-    const int i_lo = uniform(row0 / p.h), i_hi = uniform((row0 + rows - 1) / p.h);
-    const Range range = tile_range(a, s, i_lo, i_hi);
-    const int from = max(u0, before), to = min(u1, before + n_units);
-    const int c0 = range.lo + (from - before) * kUnit, c1 = min(range.lo + (to - before) * kUnit, range.hi);
-    const int blocks = (c1 - c0 + S::TOK - 1) / S::TOK;
-    const int32_t* table = c.table + (int64_t)b * c.table_stride;
+        const Seq s = uniform(each == 1 ? s_seq[item] : seq_at(item));
+        n_units = each == 1 ? uniform(s_units[item + 1]) - before : uniform(units_at(item, s));
+        if (before + n_units <= u0) continue;
+        const int b = item / p.tiles, tile = item - b * p.tiles;
+        const int row0 = tile * p.tile_rows;
+        const int rows = min(s.n * p.h - row0, p.tile_rows);
+        const int i_lo = uniform(row0 / p.h), i_hi = uniform((row0 + rows - 1) / p.h);
+        const Range range = tile_range(a, s, i_lo, i_hi);
+        const int from = max(u0, before), to = min(u1, before + n_units);
+        const int c0 = range.lo + (from - before) * kUnit, c1 = min(range.lo + (to - before) * kUnit, range.hi);
+        const int blocks = (c1 - c0 + S::TOK - 1) / S::TOK;
+        const int32_t* table = c.table + (int64_t)b * c.table_stride;
 
-    auto clamp = [&](int d) { return FULL ? d : min(d, c.D - S::VEC); };
-    // this lane's rows, and their queries as B operands
-    int row_i[RB];
-    u32x4 qf[RB][S::KK];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        const int rr = row0 + rb * 16 + r;
-        const bool on = rb * 16 + r < rows;
-        row_i[rb] = on ? rr / p.h : i_lo;
-        const int head = g * p.h + (on ? rr - row_i[rb] * p.h : 0);
-        const char* src = (const char*)a.q.data +
-                          ((int64_t)(s.row0 + row_i[rb]) * a.q.stride_row + (int64_t)head * a.q.stride_head) * E::kBytes;
-#pragma unroll
-        for (int kk = 0; kk < S::KK; ++kk) {
-            const int d = kk * S::KSTEP + q * S::VEC;
-            qf[rb][kk] = *(const u32x4*)(src + clamp(d) * E::kBytes);
-        }
-    }
-    // (unconditional loads; rows and dimensions that are not there count as zero)
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int kk = 0; kk < S::KK; ++kk) {
-            const bool none = rb * 16 + r >= rows || kk * S::KSTEP + q * S::VEC >= c.D;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) qf[rb][kk][e] = none ? 0u : qf[rb][kk][e];
-        }
-
-    f32x4 o[RB][DB];
-    float m[RB], l[RB];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        m[rb] = kNoScore;
-        l[rb] = 0.f;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    // A block's tokens: lane t < TOK finds token t's place; -1: nothing there.  The page number is loaded
-    // a block before it is used, so that no load in between has to be waited for with it.
-    auto token_of = [&](int blk) { return c0 + blk * S::TOK + lane; };
-    auto page_of = [&](int blk) {
-        const int j = token_of(blk);
-        const int at = lane < S::TOK && j < c1 ? j : 0;
-        return table[p.page_shift >= 0 ? at >> p.page_shift : at / c.P];
-    };
-    auto place = [&](int blk, int page) -> int64_t {
-        const int j = token_of(blk);
-        const int pi = p.page_shift >= 0 ? j >> p.page_shift : j / c.P;
-        if (lane >= S::TOK || j >= c1 || (unsigned)page >= (unsigned)c.pages) return -1;
-        return (int64_t)page * c.stride_page + (int64_t)(j - pi * c.P) * c.stride_token;
-    };
-    // Loads are unconditional: a token that is not there reads the pool's first one instead, whose
-    // scores are masked and whose values are zeroed, and a piece past the head's end reads its
-    // last piece, which counts as zero in a key and goes to no output in a value.
-    // float32 products bound their kernel, so those past the head's end are left out
-    auto in_head = [&](int d) { return FULL || BF16 || d < c.D; };
-    u32x4 kf[S::TT][S::KK], vf[S::NV];
-    auto load_keys = [&](int slot) {
-#pragma unroll
-        for (int t = 0; t < S::TT; ++t) {
-            const char* src = (const char*)c.k + (s_off[wave][slot][16 * t + r] + head_at) * E::kBytes;
-#pragma unroll
-            for (int kk = 0; kk < S::KK; ++kk)
-                kf[t][kk] = *(const u32x4*)(src + clamp(kk * S::KSTEP + q * S::VEC) * E::kBytes);
-        }
-    };
-    auto load_values = [&](int slot) {
-        const int d = clamp((lane % S::LPR) * S::VEC);
-        const char* src = (const char*)c.v + (head_at + d) * E::kBytes;
-#pragma unroll
-        for (int k = 0; k < S::NV; ++k)
-            vf[k] = stream_load<BF16>(src + s_off[wave][slot][k * S::TPI + lane / S::LPR] * E::kBytes);
-    };
-    auto wave_sync = [&]() {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    };
-
-    int64_t off = place(wave, page_of(wave));
-    int page_next = page_of(wave + NW);
-    if (lane < S::TOK) s_off[wave][0][lane] = max(off, (int64_t)0);
-    wave_sync();
-    load_keys(0);
-    __builtin_amdgcn_sched_barrier(0);  // keys before values, as in the loop: their wait counts on it
-    load_values(0);
-    int slot = 0;
-    for (int round = 0; round < blocks; round += NW, slot ^= 1) {
-        // The CU serves its older waves first; left alone, they would be done in half the time, and the
-        // others could not keep memory busy.  The next blocks' loads are in flight meanwhile.
-        __builtin_amdgcn_s_barrier();
-        const int blk = round + wave;
-        if (blk >= blocks) continue;
-        const int j0 = c0 + blk * S::TOK;
-        const uint32_t there = (uint32_t)__ballot(lane < S::TOK && off >= 0);
-        // every row sees the whole block, or bits say which tokens
-        const uint32_t every = S::TOK == 32 ? ~0u : (1u << S::TOK) - 1u;
-        const bool whole = there == every &&
-                           (a.mask ? j0 + S::TOK <= s.first
-                                   : j0 + S::TOK - 1 <= s.first + i_lo && (a.window == 0 || j0 > s.first + i_hi - a.window));
-#pragma unroll
-        for (int kk = 0; kk < S::KK; ++kk) {
-            if (FULL || ((kk + 1) * S::KSTEP <= DP / 2 && DP > 64)) continue;  // D > DP / 2 there
-            const bool past = kk * S::KSTEP + q * S::VEC >= c.D;
-#pragma unroll
-            for (int t = 0; t < S::TT; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) kf[t][kk][e] = past ? 0u : kf[t][kk][e];
-        }
-        Weights<BF16> w[RB];
+        auto clamp = [&](int d) { return FULL ? d : min(d, c.D - S::VEC); };
+        // this lane's rows, and their queries as B operands
+        int row_i[RB];
+        u32x4 qf[RB][S::KK];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-            f32x4 sv[S::TT];
+            const int rr = row0 + rb * 16 + r;
+            const bool on = rb * 16 + r < rows;
+            row_i[rb] = on ? rr / p.h : i_lo;
+            const int head = g * p.h + (on ? rr - row_i[rb] * p.h : 0);
+            const char* src = (const char*)a.q.data +
+                              ((int64_t)(s.row0 + row_i[rb]) * a.q.stride_row + (int64_t)head * a.q.stride_head) * E::kBytes;
+#pragma unroll
+            for (int kk = 0; kk < S::KK; ++kk) {
+                const int d = kk * S::KSTEP + q * S::VEC;
+                qf[rb][kk] = *(const u32x4*)(src + clamp(d) * E::kBytes);
+            }
+        }
+        // (unconditional loads; rows and dimensions that are not there count as zero)
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int kk = 0; kk < S::KK; ++kk) {
+                const bool none = rb * 16 + r >= rows || kk * S::KSTEP + q * S::VEC >= c.D;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) qf[rb][kk][e] = none ? 0u : qf[rb][kk][e];
+            }
+
+        f32x4 o[RB][DB];
+        float m[RB], l[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            m[rb] = kNoScore;
+            l[rb] = 0.f;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        // A block's tokens: lane t < TOK finds token t's place; -1: nothing there.  The page number is loaded
+        // a block before it is used, so that no load in between has to be waited for with it.
+        auto token_of = [&](int blk) { return c0 + blk * S::TOK + lane; };
+        auto page_of = [&](int blk) {
+            const int j = token_of(blk);
+            const int at = lane < S::TOK && j < c1 ? j : 0;
+            return table[p.page_shift >= 0 ? at >> p.page_shift : at / c.P];
+        };
+        auto place = [&](int blk, int page) -> int64_t {
+            const int j = token_of(blk);
+            const int pi = p.page_shift >= 0 ? j >> p.page_shift : j / c.P;
+            if (lane >= S::TOK || j >= c1 || (unsigned)page >= (unsigned)c.pages) return -1;
+            return (int64_t)page * c.stride_page + (int64_t)(j - pi * c.P) * c.stride_token;
+        };
+        // Loads are unconditional: a token that is not there reads the pool's first one instead, whose
+        // scores are masked and whose values are zeroed, and a piece past the head's end reads its
+        // last piece, which counts as zero in a key and goes to no output in a value.
+        // float32 products bound their kernel, so those past the head's end are left out
+        auto in_head = [&](int d) { return FULL || BF16 || d < c.D; };
+        u32x4 kf[S::TT][S::KK], vf[S::NV];
+        auto load_keys = [&](int slot) {
 #pragma unroll
             for (int t = 0; t < S::TT; ++t) {
-                sv[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                const char* src = (const char*)c.k + (s_off[wave][slot][16 * t + r] + head_at) * E::kBytes;
 #pragma unroll
                 for (int kk = 0; kk < S::KK; ++kk)
-                    if (in_head(kk * S::KSTEP)) sv[t] = multiply<BF16>(kf[t][kk], qf[rb][kk], sv[t]);
+                    kf[t][kk] = *(const u32x4*)(src + clamp(kk * S::KSTEP + q * S::VEC) * E::kBytes);
             }
-            if (rb == RB - 1) {
-                // the next block's keys set out
-                off = place(blk + NW, page_next);
-                if (lane < S::TOK) s_off[wave][slot ^ 1][lane] = max(off, (int64_t)0);
-                wave_sync();
-                load_keys(slot ^ 1);
-                page_next = page_of(blk + 2 * NW);
-            }
-            float top = kNoScore;
+        };
+        auto load_values = [&](int slot) {
+            const int d = clamp((lane % S::LPR) * S::VEC);
+            const char* src = (const char*)c.v + (head_at + d) * E::kBytes;
 #pragma unroll
-            for (int t = 0; t < S::TT; ++t) sv[t] *= sc;
-            if (!whole) {
-                // this lane's tokens 4q .. 4q + 3 of each tile
-                const uint32_t bits = (there & row_bits(a, s, row_i[rb], s.row0 + row_i[rb], j0)) >> (4 * q);
+            for (int k = 0; k < S::NV; ++k)
+                vf[k] = stream_load<BF16>(src + s_off[wave][slot][k * S::TPI + lane / S::LPR] * E::kBytes);
+        };
+        auto wave_sync = [&]() {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        };
+
+        int64_t off = place(wave, page_of(wave));
+        int page_next = page_of(wave + NW);
+        if (lane < S::TOK) s_off[wave][0][lane] = max(off, (int64_t)0);
+        wave_sync();
+        load_keys(0);
+        __builtin_amdgcn_sched_barrier(0);  // keys before values, as in the loop: their wait counts on it
+        load_values(0);
+        int slot = 0;
+        for (int round = 0; round < blocks; round += NW, slot ^= 1) {
+            // The CU serves its older waves first; left alone, they would be done in half the time, and the
+            // others could not keep memory busy.  The next blocks' loads are in flight meanwhile.
+            __builtin_amdgcn_s_barrier();
+            const int blk = round + wave;
+            if (blk >= blocks) continue;
+            const int j0 = c0 + blk * S::TOK;
+            const uint32_t there = (uint32_t)__ballot(lane < S::TOK && off >= 0);
+            // every row sees the whole block, or bits say which tokens
+            const uint32_t every = S::TOK == 32 ? ~0u : (1u << S::TOK) - 1u;
+            const bool whole = there == every &&
+                               (a.mask ? j0 + S::TOK <= s.first
+                                       : j0 + S::TOK - 1 <= s.first + i_lo && (a.window == 0 || j0 > s.first + i_hi - a.window));
+#pragma unroll
+            for (int kk = 0; kk < S::KK; ++kk) {
+                if (FULL || ((kk + 1) * S::KSTEP <= DP / 2 && DP > 64)) continue;  // D > DP / 2 there
+                const bool past = kk * S::KSTEP + q * S::VEC >= c.D;
 #pragma unroll
                 for (int t = 0; t < S::TT; ++t)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        sv[t][e] = bits & (1u << (16 * t + e)) ? sv[t][e] : kNoScore;
+                    for (int e = 0; e < 4; ++e) kf[t][kk][e] = past ? 0u : kf[t][kk][e];
             }
-#pragma unroll
-            for (int t = 0; t < S::TT; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) top = fmaxf(top, sv[t][e]);
-            if (__any(top > m[rb] + kSlack)) {
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float next = fmaxf(m[rb], top);
-                const float by = next == kNoScore ? 1.f : exp2_hw(m[rb] - next);
-                m[rb] = next;
-                l[rb] *= by;
-#pragma unroll
-                for (int db = 0; db < DB; ++db) o[rb][db] *= by;
-            }
-            const float from = m[rb] == kNoScore ? 0.f : m[rb];
-#pragma unroll
-            for (int t = 0; t < S::TT; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    sv[t][e] = exp2_hw(sv[t][e] - from);
-                    l[rb] += sv[t][e];
-                }
-            w[rb].take(sv);
-        }
-
-        // Values.  A row's weight 0 times an infinite or NaN value that the row does not see would be
-        // NaN: where rows differ in what they see, such elements are taken out, and a second
-        // product of the largest finite numbers puts infinity where a row does see one.
-        bool odd = false;
-        if (!whole) {
-            bool any = false;
-#pragma unroll
-            for (int k = 0; k < S::NV; ++k) {
-                const bool gone = !((there >> (k * S::TPI + lane / S::LPR)) & 1u);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (gone) vf[k][e] = 0;
-                    any |= odd_lo<BF16>(vf[k][e]) || odd_hi(vf[k][e]);
-                }
-            }
-            odd = __any(any);
-            if (odd) {
-#pragma unroll
-                for (int k = 0; k < S::NV; ++k)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (odd_lo<BF16>(vf[k][e])) vf[k][e] &= 0xFFFF0000u;
-                        if (odd_hi(vf[k][e])) vf[k][e] &= BF16 ? 0xFFFFu : 0u;
-                    }
-            }
-        }
-        auto piece_at = [&](int k) {
-            return (u32x4*)(s_v + ((k * S::TPI + lane / S::LPR) * S::PITCH + (lane % S::LPR) * S::VEC) * E::kBytes);
-        };
-        // o += V^T of 16 dimensions (this lane's dimension of the tokens of its weights) times the weights
-        auto add_values = [&]() {
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                if (!in_head(16 * db)) break;
-                u32x4 v;
-                if constexpr (BF16) {
-                    char* at = s_v + ((4 * q + r / 4) * S::PITCH + db * 16 + (r % 4) * 4) * 2;
-                    union {
-                        s16x4 half[2];
-                        u32x4 all;
-                    } both;
-                    both.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at));
-                    both.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (__attribute__((address_space(3))) s16x4*)(at + 16 * S::PITCH * 2));
-                    v = both.all;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = *(const uint32_t*)(s_v + ((4 * q + e) * S::PITCH + db * 16 + r) * 4);
-                }
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) o[rb][db] = multiply<BF16>(v, w[rb].all, o[rb][db]);
-            }
-        };
-#pragma unroll
-        for (int k = 0; k < S::NV; ++k) *piece_at(k) = vf[k];
-        wave_sync();
-        load_values(slot ^ 1);
-        add_values();
-        wave_sync();
-        if (odd) {
-            constexpr uint32_t kLo = BF16 ? 0x7F7Fu : 0u, kHi = BF16 ? 0x7F7F0000u : 0x7F7FFFFFu;  // largest finite
-            const int ol = again(lane);
-            const int d = clamp((ol % S::LPR) * S::VEC);
-#pragma unroll 1
-            for (int k = 0; k < S::NV; ++k) {
-                const int t = k * S::TPI + ol / S::LPR;
-                u32x4 v = *(const u32x4*)((const char*)c.v + (head_at + d + s_off[wave][slot][t]) * E::kBytes);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[e] = there >> t & 1u ? (odd_lo<BF16>(v[e]) ? kLo : 0u) | (odd_hi(v[e]) ? kHi : 0u) : 0u;
-                *piece_at(k) = v;
-            }
-            wave_sync();
+            Weights<BF16> w[RB];
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
-                const uint32_t bits = (there & row_bits(a, s, row_i[rb], s.row0 + row_i[rb], j0)) >> (4 * q);
-                f32x4 one[S::TT];
+                f32x4 sv[S::TT];
+#pragma unroll
+                for (int t = 0; t < S::TT; ++t) {
+                    sv[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int kk = 0; kk < S::KK; ++kk)
+                        if (in_head(kk * S::KSTEP)) sv[t] = multiply<BF16>(kf[t][kk], qf[rb][kk], sv[t]);
+                }
+                if (rb == RB - 1) {
+                    // the next block's keys set out
+                    off = place(blk + NW, page_next);
+                    if (lane < S::TOK) s_off[wave][slot ^ 1][lane] = max(off, (int64_t)0);
+                    wave_sync();
+                    load_keys(slot ^ 1);
+                    page_next = page_of(blk + 2 * NW);
+                }
+                float top = kNoScore;
+#pragma unroll
+                for (int t = 0; t < S::TT; ++t) sv[t] *= sc;
+                if (!whole) {
+                    // this lane's tokens 4q .. 4q + 3 of each tile
+                    const uint32_t bits = (there & row_bits(a, s, row_i[rb], s.row0 + row_i[rb], j0)) >> (4 * q);
+#pragma unroll
+                    for (int t = 0; t < S::TT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            sv[t][e] = bits & (1u << (16 * t + e)) ? sv[t][e] : kNoScore;
+                }
 #pragma unroll
                 for (int t = 0; t < S::TT; ++t)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) one[t][e] = bits & (1u << (16 * t + e)) ? kHuge : 0.f;
-                w[rb].take(one);
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, sv[t][e]);
+                if (__any(top > m[rb] + kSlack)) {
+                    top = fmaxf(top, __shfl_xor(top, 16));
+                    top = fmaxf(top, __shfl_xor(top, 32));
+                    const float next = fmaxf(m[rb], top);
+                    const float by = next == kNoScore ? 1.f : exp2_hw(m[rb] - next);
+                    m[rb] = next;
+                    l[rb] *= by;
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) o[rb][db] *= by;
+                }
+                const float from = m[rb] == kNoScore ? 0.f : m[rb];
+#pragma unroll
+                for (int t = 0; t < S::TT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        sv[t][e] = exp2_hw(sv[t][e] - from);
+                        l[rb] += sv[t][e];
+                    }
+                w[rb].take(sv);
             }
-            add_values();
-            wave_sync();
-        }
-    }
 
-    // Join the waves: a common maximum, then the outputs through LDS, summed by all threads, each for NP
-    // pairs of neighbouring dimensions.
-    constexpr int NP = ROWS * DP / 2 / NT;
-    constexpr int OP = DP + 4;
-    const int el = again(lane), et = again(tid), er = el & 15, eq = el >> 4;
+            // Values.  A row's weight 0 times an infinite or NaN value that the row does not see would be
+            // NaN: where rows differ in what they see, such elements are taken out, and a second
+            // product of the largest finite numbers puts infinity where a row does see one.
+            bool odd = false;
+            if (!whole) {
+                bool any = false;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        l[rb] += __shfl_xor(l[rb], 16);
-        l[rb] += __shfl_xor(l[rb], 32);
-        if (eq == 0) {
-            s_m[wave][rb * 16 + er] = m[rb];
-            s_l[wave][rb * 16 + er] = l[rb];
-        }
-    }
-    __syncthreads();
-    float* s_o = (float*)s_mem;
+                for (int k = 0; k < S::NV; ++k) {
+                    const bool gone = !((there >> (k * S::TPI + lane / S::LPR)) & 1u);
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        const int row = rb * 16 + er;
-        float top = kNoScore;
-        for (int w = 0; w < NW; ++w) top = fmaxf(top, s_m[w][row]);
-        const float by = m[rb] == kNoScore ? 0.f : exp2_hw(m[rb] - top);
+                    for (int e = 0; e < 4; ++e) {
+                        if (gone) vf[k][e] = 0;
+                        any |= odd_lo<BF16>(vf[k][e]) || odd_hi(vf[k][e]);
+                    }
+                }
+                odd = __any(any);
+                if (odd) {
 #pragma unroll
-        for (int db = 0; db < DB; ++db) *(f32x4*)(s_o + (wave * ROWS + row) * OP + db * 16 + 4 * eq) = o[rb][db] * by;
-        if (wave == 0 && eq == 0) {
-            float sum = 0.f;
-            if (top != kNoScore)
-                for (int w = 0; w < NW; ++w) sum += s_l[w][row] * exp2_hw(s_m[w][row] - top);
-            s_top[row] = top;
-            s_sum[row] = sum;
-        }
-    }
-    __syncthreads();
-    float2 y[NP];
+                    for (int k = 0; k < S::NV; ++k)
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int e = (i * NT + et) * 2;
-        y[i] = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const float2 x = *(const float2*)(s_o + (w * ROWS + e / DP) * OP + e % DP);
-            y[i].x += x.x;
-            y[i].y += x.y;
-        }
-    }
-    if (from != before || to != before + n_units) {
-        // A part of an item.  What a workgroup leaves of an item that its stretch begins with goes to
-        // its first slot, of one that begins later to its second.
-        const int w_first = owner(before), n_parts = owner(before + n_units - 1) - w_first + 1;
-        float* dst = slot_of(wg, from == u0 ? 0 : 1);
-#pragma unroll
-        for (int i = 0; i < NP; ++i) leave2(dst + (i * NT + et) * 2, y[i].x, y[i].y);
-        if (et < ROWS) leave2(dst + ROWS * DP + 2 * et, s_top[et], s_sum[et]);
-        // all of it is written when the counter goes up: the workgroup that counts last finds every part
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (et == 0) {
-            unsigned* counter = (unsigned*)a.workspace + w_first * c.G + g;
-            const unsigned was = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            s_last = was == (unsigned)(n_parts - 1);
-            if (s_last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        __syncthreads();
-        if (!s_last) continue;  // s_last is written again two barriers later at the earliest
-        // the parts' common maximum and sum of each row, then their outputs, kBatch parts at a time
-        constexpr int kSubs = NT / ROWS, kBatch = 2048 / ROWS;
-        float* s_red = (float*)s_mem;         // [kSubs][ROWS][2]
-        float* s_fac = s_red + 2 * NT;  // [kBatch][ROWS]: the parts' factors
-        const int first_slot = before == start(w_first) ? 0 : 1;
-        auto part_slot = [&](int k) { return slot_of(w_first + k, k == 0 ? first_slot : 0); };
-        const int row = et % ROWS;
-        float mm = kNoScore, ll = 0.f;
-        for (int k = et / ROWS; k < n_parts; k += kSubs) {
-            const float2 x = fetch2(part_slot(k) + ROWS * DP + 2 * row);
-            const float up = fmaxf(mm, x.x);
-            if (up != kNoScore) ll = ll * exp2_hw(mm - up) + x.y * exp2_hw(x.x - up);
-            mm = up;
-        }
-        s_red[2 * et] = mm;
-        s_red[2 * et + 1] = ll;
-        __syncthreads();
-        if (et < ROWS) {
-            for (int k = 1; k < kSubs; ++k) {
-                const float xm = s_red[2 * (k * ROWS + et)], xl = s_red[2 * (k * ROWS + et) + 1];
-                const float up = fmaxf(mm, xm);
-                if (up != kNoScore) ll = ll * exp2_hw(mm - up) + xl * exp2_hw(xm - up);
-                mm = up;
-            }
-            s_top[et] = mm;
-            s_sum[et] = ll;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < NP; ++i) y[i] = make_float2(0.f, 0.f);
-        for (int k0 = 0; k0 < n_parts; k0 += kBatch) {
-            const int nk = min(kBatch, n_parts - k0);
-            for (int i = et; i < nk * ROWS; i += NT) {
-                const float pm = fetch2(part_slot(k0 + i / ROWS) + ROWS * DP + 2 * (i % ROWS)).x;
-                s_fac[i] = pm == kNoScore ? 0.f : exp2_hw(pm - s_top[i % ROWS]);
-            }
-            __syncthreads();
-            // all of a part's loads set out before one is waited for, and the next part's before this one is added
-            float2 x[NP], x_next[NP];
-            auto fetch = [&](int k, float2 (&into)[NP]) {
-                const float* src = part_slot(k0 + k) + 2 * et;
-#pragma unroll
-                for (int i = 0; i < NP; ++i) into[i] = fetch2(src + 2 * i * NT);
-            };
-            fetch(0, x);
-            for (int k = 0; k < nk; ++k) {
-                fetch(min(k + 1, nk - 1), x_next);
-#pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    const float f = s_fac[k * ROWS + (i * NT + et) * 2 / DP];
-                    y[i].x += x[i].x * f;
-                    y[i].y += x[i].y * f;
-                    x[i] = x_next[i];
+                        for (int e = 0; e < 4; ++e) {
+                            if (odd_lo<BF16>(vf[k][e])) vf[k][e] &= 0xFFFF0000u;
+                            if (odd_hi(vf[k][e])) vf[k][e] &= BF16 ? 0xFFFFu : 0u;
+                        }
                 }
             }
-            __syncthreads();
-        }
-    }
+            auto piece_at = [&](int k) {
+                return (u32x4*)(s_v + ((k * S::TPI + lane / S::LPR) * S::PITCH + (lane % S::LPR) * S::VEC) * E::kBytes);
+            };
+            // o += V^T of 16 dimensions (this lane's dimension of the tokens of its weights) times the weights
+            auto add_values = [&]() {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int e = (i * NT + et) * 2;
-        const int row = e / DP, d = e % DP;
-        if (row >= rows || d >= c.D) continue;
-        const int rr = row0 + row, ri = rr / p.h;
-        const int head = g * p.h + rr - ri * p.h;
-        const int64_t t = s.row0 + ri;
-        const bool none = s_top[row] == kNoScore;
-        const float by = none ? 0.f : 1.f / s_sum[row];
-        const float y0 = none ? 0.f : y[i].x * by, y1 = none ? 0.f : y[i].y * by;
-        char* dst = (char*)a.out.data + (t * a.out.stride_row + (int64_t)head * a.out.stride_head + d) * E::kBytes;
-        if constexpr (BF16)
-            *(uint32_t*)dst = pack_bf16(y0, y1);
-        else
-            *(float2*)dst = make_float2(y0, y1);
-        if (d == 0 && a.lse) a.lse[t * a.H + head] = none ? kNoScore : (s_top[row] + log2f(s_sum[row])) * kLn2;
-    }
-    __syncthreads();
+                for (int db = 0; db < DB; ++db) {
+                    if (!in_head(16 * db)) break;
+                    u32x4 v;
+                    if constexpr (BF16) {
+                        char* at = s_v + ((4 * q + r / 4) * S::PITCH + db * 16 + (r % 4) * 4) * 2;
+                        union {
+                            s16x4 half[2];
+                            u32x4 all;
+                        } both;
+                        both.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at));
+                        both.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                            (__attribute__((address_space(3))) s16x4*)(at + 16 * S::PITCH * 2));
+                        v = both.all;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = *(const uint32_t*)(s_v + ((4 * q + e) * S::PITCH + db * 16 + r) * 4);
+                    }
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) o[rb][db] = multiply<BF16>(v, w[rb].all, o[rb][db]);
+                }
+            };
+#pragma unroll
+            for (int k = 0; k < S::NV; ++k) *piece_at(k) = vf[k];
+            wave_sync();
+            load_values(slot ^ 1);
+            add_values();
+            wave_sync();
+            if (odd) {
+                constexpr uint32_t kLo = BF16 ? 0x7F7Fu : 0u, kHi = BF16 ? 0x7F7F0000u : 0x7F7FFFFFu;  // largest finite
+                const int ol = again(lane);
+                const int d = clamp((ol % S::LPR) * S::VEC);
+#pragma unroll 1
+                for (int k = 0; k < S::NV; ++k) {
+                    const int t = k * S::TPI + ol / S::LPR;
+                    u32x4 v = *(const u32x4*)((const char*)c.v + (head_at + d + s_off[wave][slot][t]) * E::kBytes);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        v[e] = there >> t & 1u ? (odd_lo<BF16>(v[e]) ? kLo : 0u) | (odd_hi(v[e]) ? kHi : 0u) : 0u;
+                    *piece_at(k) = v;
+                }
+                wave_sync();
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                    const uint32_t bits = (there & row_bits(a, s, row_i[rb], s.row0 + row_i[rb], j0)) >> (4 * q);
+                    f32x4 one[S::TT];
+#pragma unroll
+                    for (int t = 0; t < S::TT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) one[t][e] = bits & (1u << (16 * t + e)) ? kHuge : 0.f;
+                    w[rb].take(one);
+                }
+                add_values();
+                wave_sync();
+            }
+        }
+
+        // Join the waves: a common maximum, then the outputs through LDS, summed by all threads, each for NP
+        // pairs of neighbouring dimensions.
+        constexpr int NP = ROWS * DP / 2 / NT;
+        constexpr int OP = DP + 4;
+        const int el = again(lane), et = again(tid), er = el & 15, eq = el >> 4;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            l[rb] += __shfl_xor(l[rb], 16);
+            l[rb] += __shfl_xor(l[rb], 32);
+            if (eq == 0) {
+                s_m[wave][rb * 16 + er] = m[rb];
+                s_l[wave][rb * 16 + er] = l[rb];
+            }
+        }
+        __syncthreads();
+        float* s_o = (float*)s_mem;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const int row = rb * 16 + er;
+            float top = kNoScore;
+            for (int w = 0; w < NW; ++w) top = fmaxf(top, s_m[w][row]);
+            const float by = m[rb] == kNoScore ? 0.f : exp2_hw(m[rb] - top);
+#pragma unroll
+            for (int db = 0; db < DB; ++db) *(f32x4*)(s_o + (wave * ROWS + row) * OP + db * 16 + 4 * eq) = o[rb][db] * by;
+            if (wave == 0 && eq == 0) {
+                float sum = 0.f;
+                for (int w = 0; w < NW; ++w) sum = add_sums(sum, top, s_l[w][row], s_m[w][row], top);
+                s_top[row] = top;
+                s_sum[row] = sum;
+            }
+        }
+        __syncthreads();
+        float2 y[NP];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int e = (i * NT + et) * 2;
+            y[i] = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float2 x = *(const float2*)(s_o + (w * ROWS + e / DP) * OP + e % DP);
+                y[i].x += x.x;
+                y[i].y += x.y;
+            }
+        }
+        if (from != before || to != before + n_units) {
+            // A part of an item.  What a workgroup leaves of an item that its stretch begins with goes to
+            // its first slot, of one that begins later to its second.
+            const int w_first = owner(before), n_parts = owner(before + n_units - 1) - w_first + 1;
+            float* dst = slot_of(wg, from == u0 ? 0 : 1);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) leave2(dst + (i * NT + et) * 2, y[i].x, y[i].y);
+            if (et < ROWS) leave2(dst + ROWS * DP + 2 * et, s_top[et], s_sum[et]);
+            // all of it is written when the counter goes up: the workgroup that counts last finds every part
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (et == 0) {
+                unsigned* counter = (unsigned*)a.workspace + w_first * c.G + g;
+                const unsigned was = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                s_last = was == (unsigned)(n_parts - 1);
+                if (s_last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            __syncthreads();
+            if (!s_last) continue;  // s_last is written again two barriers later at the earliest
+            // the parts' common maximum and sum of each row, then their outputs, kBatch parts at a time
+            constexpr int kSubs = NT / ROWS, kBatch = 2048 / ROWS;
+            float* s_red = (float*)s_mem;         // [kSubs][ROWS][2]
+            float* s_fac = s_red + 2 * NT;  // [kBatch][ROWS]: the parts' factors
+            const int first_slot = before == start(w_first) ? 0 : 1;
+            auto part_slot = [&](int k) { return slot_of(w_first + k, k == 0 ? first_slot : 0); };
+            const int row = et % ROWS;
+            float mm = kNoScore, ll = 0.f;
+            for (int k = et / ROWS; k < n_parts; k += kSubs) {
+                const float2 x = fetch2(part_slot(k) + ROWS * DP + 2 * row);
+                const float up = fmaxf(mm, x.x);
+                ll = add_sums(ll, mm, x.y, x.x, up);
+                mm = up;
+            }
+            s_red[2 * et] = mm;
+            s_red[2 * et + 1] = ll;
+            __syncthreads();
+            if (et < ROWS) {
+                for (int k = 1; k < kSubs; ++k) {
+                    const float xm = s_red[2 * (k * ROWS + et)], xl = s_red[2 * (k * ROWS + et) + 1];
+                    const float up = fmaxf(mm, xm);
+                    ll = add_sums(ll, mm, xl, xm, up);
+                    mm = up;
+                }
+                s_top[et] = mm;
+                s_sum[et] = ll;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < NP; ++i) y[i] = make_float2(0.f, 0.f);
+            for (int k0 = 0; k0 < n_parts; k0 += kBatch) {
+                const int nk = min(kBatch, n_parts - k0);
+                for (int i = et; i < nk * ROWS; i += NT) {
+                    const float pm = fetch2(part_slot(k0 + i / ROWS) + ROWS * DP + 2 * (i % ROWS)).x;
+                    s_fac[i] = pm == kNoScore ? 0.f : exp2_hw(pm - s_top[i % ROWS]);
+                }
+                __syncthreads();
+                // all of a part's loads set out before one is waited for, and the next part's before this one is added
+                float2 x[NP], x_next[NP];
+                auto fetch = [&](int k, float2 (&into)[NP]) {
+                    const float* src = part_slot(k0 + k) + 2 * et;
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) into[i] = fetch2(src + 2 * i * NT);
+                };
+                fetch(0, x);
+                for (int k = 0; k < nk; ++k) {
+                    fetch(min(k + 1, nk - 1), x_next);
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) {
+                        const float f = s_fac[k * ROWS + (i * NT + et) * 2 / DP];
+                        y[i].x += x[i].x * f;
+                        y[i].y += x[i].y * f;
+                        x[i] = x_next[i];
+                    }
+                }
+                __syncthreads();
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int e = (i * NT + et) * 2;
+            const int row = e / DP, d = e % DP;
+            if (row >= rows || d >= c.D) continue;
+            const int rr = row0 + row, ri = rr / p.h;
+            const int head = g * p.h + rr - ri * p.h;
+            const int64_t t = s.row0 + ri;
+            const bool none = s_top[row] == kNoScore && s_sum[row] == 0.f;
+            const float by = none ? 0.f : 1.f / s_sum[row];
+            const float y0 = none ? 0.f : y[i].x * by, y1 = none ? 0.f : y[i].y * by;
+            char* dst = (char*)a.out.data + (t * a.out.stride_row + (int64_t)head * a.out.stride_head + d) * E::kBytes;
+            if constexpr (BF16)
+                *(uint32_t*)dst = pack_bf16(y0, y1);
+            else
+                *(float2*)dst = make_float2(y0, y1);
+            if (d == 0 && a.lse) a.lse[t * a.H + head] = none ? kNoScore : (s_top[row] + log2f(s_sum[row])) * kLn2;
+        }
+        __syncthreads();
     }
 }
 
@@ -1065,7 +1063,8 @@ __global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_
     l += __shfl_xor(l, 32);
     if (!on) return;
     if (n_parts == 1) {
-        const float by = m == kNoScore ? 0.f : 1.f / l;
+        const bool none = m == kNoScore && l == 0.f;
+        const float by = 1.f / l;
         char* dst = (char*)a.out.data + (t_row * a.out.stride_row + (int64_t)head * a.out.stride_head) * 2;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -1074,11 +1073,11 @@ __global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_
                 const int d = db * 32 + 2 * e + 4 * hi;
                 if (d >= c.D) continue;
                 uint2 y = make_uint2(0, 0);
-                if (m != kNoScore)
+                if (!none)
                     y = make_uint2(pack_bf16(o[db][e] * by, o[db][e + 1] * by), pack_bf16(o[db][e + 2] * by, o[db][e + 3] * by));
                 *(uint2*)(dst + d * 2) = y;
             }
-        if (hi == 0 && a.lse) a.lse[t_row * a.H + head] = m == kNoScore ? kNoScore : (m + log2f(l)) * kLn2;
+        if (hi == 0 && a.lse) a.lse[t_row * a.H + head] = none ? kNoScore : (m + log2f(l)) * kLn2;
     } else {
         const int64_t at = ((int64_t)part * c.rows + t_row) * a.H + head;
         float* dst = (float*)a.workspace + kCounterFloats + at * c.D;
@@ -1096,10 +1095,8 @@ __global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_
     }
 }
 
-// Joins the parts of each (row, head): one wave each, the weights of up to 64 parts in its lanes.
-template <bool BF16>
+// Joins tile_kernel's parts of each (row, head): one wave each, the weights of up to 64 parts in its lanes.
 __global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a, Plan p) {
-    using E = Elem<BF16>;
     const CacheArgs& c = a.c;
     const int lane = threadIdx.x & 63;
     const int64_t item = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
@@ -1124,10 +1121,10 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a, Plan p)
 #pragma unroll
     for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
     const float by = mine.x == kNoScore ? 0.f : exp2_hw(mine.x - top);
-    float total = mine.y * by;
+    float total = mine.y * by;  // (NaN stays NaN)
 #pragma unroll
     for (int k = 32; k > 0; k >>= 1) total += __shfl_xor(total, k);
-    if (mine.y != mine.y) total = mine.y;
+    const bool none = top == kNoScore && total == 0.f;
     // 4 dimensions a lane, and the parts in turn over what groups of lanes that leaves, four loads in flight each
     const int span = c.D <= 64 ? 16 : c.D <= 128 ? 32 : 64, groups = 64 / span;
     const int d = lane % span * 4, group = lane / span;
@@ -1149,14 +1146,11 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a, Plan p)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], k);
     if (group == 0 && d < c.D) {
-        const f32x4 y = top == kNoScore ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.f / total);
-        char* dst = (char*)a.out.data + ((int64_t)t * a.out.stride_row + (int64_t)head * a.out.stride_head + d) * E::kBytes;
-        if constexpr (BF16)
-            *(uint2*)dst = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-        else
-            *(f32x4*)dst = y;
+        const f32x4 y = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.f / total);
+        char* dst = (char*)a.out.data + ((int64_t)t * a.out.stride_row + (int64_t)head * a.out.stride_head + d) * 2;
+        *(uint2*)dst = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
     }
-    if (lane == 0 && a.lse) a.lse[item] = top == kNoScore ? kNoScore : (top + log2f(total)) * kLn2;
+    if (lane == 0 && a.lse) a.lse[item] = none ? kNoScore : (top + log2f(total)) * kLn2;
 }
 
 constexpr int kMaxParts = 64;     // join_kernel holds a part's weight in a lane
@@ -1233,10 +1227,6 @@ void launch_tiles(const AttentionArgs& a, const Plan& p, dim3 grid, hipStream_t 
         hipLaunchKernelGGL((tile_kernel<DP, 4>), grid, dim3(256), 0, stream, a, p);
 }
 
-}  // namespace
-
-namespace {
-
 size_t plan_bytes(const Plan& p, const CacheArgs& c, int H) {
     if (!p.many)
         return align256(kCounterFloats * 4 + (size_t)p.wgs * c.G * 2 * p.tile_rows * (padded(c.D) + 2) * 4);
@@ -1286,10 +1276,7 @@ hipError_t launch_attention(const AttentionArgs& a, bool bf16, hipStream_t strea
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.parts <= 1) return e;
     const dim3 joins((unsigned)(((long)c.rows * a.H + kWaves - 1) / kWaves));
-    if (bf16)
-        hipLaunchKernelGGL(join_kernel<true>, joins, dim3(kThreads), 0, stream, a, p);
-    else
-        hipLaunchKernelGGL(join_kernel<false>, joins, dim3(kThreads), 0, stream, a, p);
+    hipLaunchKernelGGL(join_kernel, joins, dim3(kThreads), 0, stream, a, p);
     return hipGetLastError();
 }
 

@@ -441,8 +441,9 @@ size_t given_workspace(int B, int gamma, int V, bool bf16) { return layout(B, ga
 
 hipError_t launch_given(const GivenArgs& a, bool bf16, hipStream_t stream) {
     Layout L = layout(a.B, a.gamma, a.V, bf16);
-    if (given_whole(a.B, a.gamma, a.V)) L.rseg = 1, L.rlen = a.V;
     if (given_whole(a.B, a.gamma, a.V)) {
+        L.rseg = 1;
+        L.rlen = a.V;
         if (bf16)
             hipLaunchKernelGGL((given_race_kernel<true, true>), dim3(a.B), dim3(kWholeThreads), 0, stream, a, L);
         else

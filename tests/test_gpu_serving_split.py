@@ -85,6 +85,26 @@ def test_unseen_values_in_parts(psd, n, dtype):
 
 
 @TYPES
+@pytest.mark.parametrize("n,kv", [(2, 90), (2, 3000), (70, 90), (70, 3000)])
+def test_rows_of_nan_scores_alone(psd, n, kv, dtype):
+    """A NaN query makes every score of its row NaN: so are its output and lse, whole or in parts, and the
+    other rows stay as they are.  (A row that sees nothing stays zeros.)"""
+    s = ref.Sequences([(n, kv), (3, 2)], 1, 64, 16, dtype, seed=4)
+    q = torch.randn((s.rows, 4, 64), generator=s.gen).to(dtype)
+    want, want_lse, *_ = ref.attention(s, q, 0.125)
+    q[n - 2, 1, 5] = math.nan
+    cache, seqs, dk, dv = s.handles(psd)
+    o = psd.attention(cache, seqs, q.cuda(), psd.new_attention_workspace(cache, seqs, 4), scale=0.125, want_lse=True)
+    out, lse = o["out"].cpu().double(), o["lse"].cpu().double()
+    assert bool(torch.isnan(out[n - 2, 1]).all()) and math.isnan(float(lse[n - 2, 1]))
+    others = torch.ones((s.rows, 4), dtype=torch.bool)
+    others[n - 2, 1] = False
+    assert float((out - want)[others].abs().max()) < (0.03 if dtype == BF16 else 1e-4)
+    assert bool(torch.equal(lse[others] == -math.inf, want_lse[others] == -math.inf))
+    assert bool((lse[n] == -math.inf).all()) and bool((out[n] == 0).all())
+
+
+@TYPES
 def test_same_bits_every_time(psd, dtype):
     """Who finishes a part first does not change its sum, and one workspace serves calls of other shapes."""
     g = torch.Generator(device="cuda").manual_seed(1)
