@@ -160,6 +160,12 @@ __device__ __forceinline__ u32x4 stream_load(const char* at) {
 // takes an equal stretch of all items' W units in a row.  An item
 // inside one workgroup's stretch is finished by it; of an item that is cut, every workgroup leaves its
 // output, maximum and sum in the workspace, and the one that leaves last joins them.
+//
+// Memory bounds it, a key/value element for every 2 RB x 16 products: H=32, G=8, D=128, bfloat16, 32 sequences
+// of one new token and up to 16384 cached, 1.37 GB: 237 us, 5.75 TB/s (a plain read of memory in the same
+// order reads 5.9 - 6.2); 5 new tokens of 64 sequences, up to 4096 cached, 676 MB: 137 us.  One token of 4
+// sequences, up to 512 cached: 13 us, of them 2 to divide the work, 2 to the first key, 5 in the loop and
+// 2 to join.  Float32 is bound by its products (12 heads of 80, 37 tokens, window 700: 38 us).
 template <bool BF16, int DP>
 struct StreamShape {
     static constexpr int TOK = BF16 ? 32 : 16;
@@ -721,6 +727,8 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
 // block n is computed, block n + 1 is on its way into registers, and is stored behind the
 // arithmetic.  Two waves a SIMD, so one wave's exponentials overlap the other's products: one
 // workgroup of 8 waves a CU, which loads and stores half as much a row, or two of 4 for fewer rows.
+// 2048 new tokens behind 14336, H=32, G=8, D=128: 531 us, 970 TFLOP/s (a large library product reaches
+// 1370); without its loads and stores of keys and values 440.  In LDS two buffers of 20 KB of values and 17 of keys.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 template <int DP, int NW>
@@ -1153,9 +1161,12 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a, Plan p)
     if (lane == 0 && a.lse) a.lse[item] = none ? kNoScore : (top + log2f(total)) * kLn2;
 }
 
-constexpr int kMaxParts = 64;     // join_kernel holds a part's weight in a lane
-constexpr int kMinChunk = 256;    // tile_kernel: cached tokens of a part at least
-constexpr double kWide = 0.9;    // a block's time in 8 waves of one workgroup to that in 4 of each of two
+constexpr int kMaxParts = 64;   // join_kernel holds a part's weight in a lane
+constexpr int kMinChunk = 256;  // tile_kernel: cached tokens of a part at least
+// A block's time in 8 waves of one workgroup to that in 4 of each of two (D=128, 2048 tokens behind 14336:
+// 568 us and 624; D=64: 388 and 402; 8 x 512 behind 1536: 110 and 114; 4 x 2048 behind none: 118 and 115,
+// where the wider tile's triangle costs more).
+constexpr double kWide = 0.9;
 constexpr int kCus = 256;
 
 int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
@@ -1164,10 +1175,22 @@ Plan make_plan(const CacheArgs& c, int H, bool bf16, int span) {
     Plan p;
     p.h = H / c.G;
     const long most = (long)c.max_new * p.h;
-    p.many = bf16 && most > 64;
+    // tile_kernel for more rows than the other has registers for, and for fewer over a cache of up to 2^19
+    // tokens of all key/value heads (2^20 with more than 32 rows; a fourth of either where a head's outputs
+    // leave one workgroup a CU), which end before the other's division and joins pay.  D=128, G=8, us here
+    // and there: 4 rows, 8 x 1500 18 and 24, 2 x 8000 20 and 25, 16 x 4096 43 and 42, 32 x 4096 74 and 66;
+    // 20 rows, 64 x 1024 39 and 54, 16 x 4096 43 and 45, 32 x 4096 78 and 70; 48 rows, 64 x 1024 44 and 79,
+    // 64 x 4096 163 and 160; D=256, G=4, 48 rows, 16 x 4096 70 and 99, 4 rows 65 and 43.  Up to 32 rows stay
+    // there where it has a workgroup for each sequence and no more to gain by joins: 4 rows, 4 x 512 15 and
+    // 13, 32 x 1000 31 and 23 (64 x 512, two sequences a workgroup: 24 and 33).
+    const long tokens = (long)c.B * c.G * span * (c.D > 128 ? 4 : 1);
+    const long units = (span + kUnit - 1) / kUnit;
+    const bool alone = (long)c.B * c.G <= kCus && units <= units * c.B * c.G / kCus + 5;
+    p.many = bf16 && (most > 64 || (most > 32 ? tokens <= 1 << 20 : tokens <= 1 << 19 && !alone));
     p.wgs = p.parts = p.chunk = 0;
     if (!p.many) {
-        // float32 rows in tiles of 32 while tiles of 64 would leave CUs without one
+        // float32 rows in tiles of 32 while tiles of 64 would leave CUs without one (12 heads of 80, 37 tokens
+        // of 6 sequences: 40 us and 45; 1024 new of 4096 tokens of 16 heads, CUs full: 450 and 408)
         const bool few = !bf16 && c.D > 64 && (long)c.B * c.G * ((most + 63) / 64) < kCus;
         const int limit = c.D > 128 || few ? 32 : 64;
         p.tile_rows = most <= 16 ? 16 : most <= 32 ? 32 : limit;

