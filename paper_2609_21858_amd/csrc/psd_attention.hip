@@ -727,8 +727,9 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
 // block n is computed, block n + 1 is on its way into registers, and is stored behind the
 // arithmetic.  Two waves a SIMD, so one wave's exponentials overlap the other's products: one
 // workgroup of 8 waves a CU, which loads and stores half as much a row, or two of 4 for fewer rows.
-// 2048 new tokens behind 14336, H=32, G=8, D=128: 531 us, 970 TFLOP/s (a large library product reaches
-// 1370); without its loads and stores of keys and values 440.  In LDS two buffers of 20 KB of values and 17 of keys.
+// 2048 new tokens behind 14336, H=32, G=8, D=128: 531 - 556 us, 925 - 970 TFLOP/s (a large library product
+// reaches 1370); without its loads and stores of keys and values 440.  In LDS two buffers of 20 KB of values
+// and 17 of keys.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 template <int DP, int NW>
