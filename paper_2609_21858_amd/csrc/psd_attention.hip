@@ -197,10 +197,12 @@ constexpr int stream_lds() {
 
 constexpr int kUnit = 128;  // cached tokens: a block of each wave (two in float32)
 // Units that a workgroup has at least, if it has to join: leaving and joining the parts of an item
-// takes as long as about so many (float32 rows are bound by their products).
-template <bool BF16, int RB>
+// takes as long as about so many (4 bfloat16 sequences of up to 512 tokens 13 us, with 2 units 20; under a
+// far bound 8 sequences of 5 rows, up to 1500 tokens 28, with 8 units 40).  Float32 rows are bound by their
+// products (37 rows of 12 heads 38 us, with 4 units 49).
+template <bool BF16>
 constexpr int join_units() {
-    return BF16 ? 4 : RB == 1 ? 2 : 1;
+    return BF16 ? 4 : 1;
 }
 
 // Values that are the same in all lanes, into scalar registers.
@@ -289,7 +291,7 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
     const int units = uniform(s_units[NT]);
     // R workgroups: the first W mod R have W / R + 1 units.  While no item is much longer than that,
     // each workgroup takes one item whole and none is joined.
-    constexpr int kMinUnits = join_units<BF16, RB>();
+    constexpr int kMinUnits = join_units<BF16>();
     const int wgs = min(p.wgs, max(units / kMinUnits, 1));
     const int share = units / wgs, more = units - share * wgs;
     const bool whole_items = each == 1 && items <= p.wgs && uniform(longest) <= units / p.wgs + 1 + kMinUnits;
