@@ -40,37 +40,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// How a call is cut, by the host's bounds alone.
-struct Plan {
-    int h;          // rows per new token: H / G
-    int tile_rows;  // rows of a workgroup
-    int tiles;      // row tiles of the longest sequence
-    int wgs;        // few rows: workgroups of each key/value head
-    bool many;      // many rows: tile_kernel, with
-    int parts;      // parts of the longest range of cached tokens and
-    int chunk;      // cached tokens of a part
-    int page_shift; // log2 of the page size, or -1
-};
-
-// The workspace: a counter for each workgroup of the few-row kernel (zero between calls), then
-// what workgroups leave for the join.
-constexpr int kCounters = 1024;
-constexpr int kCounterFloats = kCounters;
-
-struct Range {
-    int lo, hi;  // cached positions that some row of a tile sees
-};
-
-// Rows [row0, row0 + rows) of a sequence see positions [lo, hi) at most.
 __device__ __forceinline__ Range tile_range(const AttentionArgs& a, const Seq& s, int i_lo, int i_hi) {
-    Range r;
-    r.lo = 0;
-    r.hi = s.kv;
-    if (!a.mask) {
-        r.hi = max(min(s.kv, s.first + i_hi + 1), 0);
-        if (a.window > 0) r.lo = min(max(s.first + i_lo - a.window + 1, 0), r.hi);
-    }
-    return r;
+    return tile_range(a.mask != nullptr, a.window, s, i_lo, i_hi);
 }
 
 // Bit t of the result: the row of new token i sees position j0 + t (causal, window or mask; the end
@@ -182,9 +153,6 @@ struct StreamShape {
     static constexpr int V_BYTES = TOK * PITCH * (BF16 ? 2 : 4);
 };
 
-// One workgroup a CU: two waves a SIMD, or one where the rows' outputs take the registers of two.
-constexpr int stream_waves(int DP, int RB) { return RB * DP >= 512 || DP == 256 ? 4 : 8; }
-
 // The waves' values; at an item's end, their outputs (rows of DP + 4 floats: the 16 rows of a store
 // fall on different banks).
 template <bool BF16, int DP, int RB>
@@ -193,16 +161,6 @@ constexpr int stream_lds() {
     constexpr int values = stream_waves(DP, RB) * S::V_BYTES;
     constexpr int join = stream_waves(DP, RB) * 16 * RB * (DP + 4) * 4;
     return values > join ? values : join;
-}
-
-constexpr int kUnit = 128;  // cached tokens: a block of each wave (two in float32)
-// Units that a workgroup has at least, if it has to join: leaving and joining the parts of an item
-// takes as long as about so many (4 bfloat16 sequences of up to 512 tokens 13 us, with 2 units 20; under a
-// far bound 8 sequences of 5 rows, up to 1500 tokens 28, with 8 units 40).  Float32 rows are bound by their
-// products (37 rows of 12 heads 38 us, with 4 units 49).
-template <bool BF16>
-constexpr int join_units() {
-    return BF16 ? 4 : 1;
 }
 
 // Values that are the same in all lanes, into scalar registers.
@@ -215,15 +173,6 @@ __device__ __forceinline__ Seq uniform(const Seq& s) {
 __device__ __forceinline__ int again(int x) {
     asm volatile("" : "+v"(x));
     return x;
-}
-
-// Units of one item, row tile `tile` of a sequence; 0 without rows, and at least 1 with them.
-__device__ __forceinline__ int item_units(const AttentionArgs& a, const Plan& p, const Seq& s, int tile) {
-    const int row0 = tile * p.tile_rows;
-    const int rows = min(s.n * p.h - row0, p.tile_rows);
-    if (rows <= 0) return 0;
-    const Range range = tile_range(a, s, row0 / p.h, (row0 + rows - 1) / p.h);
-    return max((range.hi - range.lo + kUnit - 1) / kUnit, 1);
 }
 
 // What workgroups leave for each other: written through and read past the caches that are not
@@ -260,7 +209,7 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
     const int items = c.B * p.tiles;
     const int each = (items + NT - 1) / NT;
     auto seq_at = [&](int i) { return load_seq(c, i / p.tiles); };
-    auto units_at = [&](int i, const Seq& s) { return item_units(a, p, s, i % p.tiles); };
+    auto units_at = [&](int i, const Seq& s) { return item_units(a.mask != nullptr, a.window, p, s, i % p.tiles); };
     int mine = 0, longest = 0;
     for (int i = tid * each; i < min((tid + 1) * each, items); ++i) {
         const Seq s = seq_at(i);
@@ -289,15 +238,12 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
     if (tid == 0) s_units[0] = 0;
     __syncthreads();
     const int units = uniform(s_units[NT]);
-    // R workgroups: the first W mod R have W / R + 1 units.  While no item is much longer than that,
-    // each workgroup takes one item whole and none is joined.
-    constexpr int kMinUnits = join_units<BF16>();
-    const int wgs = min(p.wgs, max(units / kMinUnits, 1));
-    const int share = units / wgs, more = units - share * wgs;
+    // While no item is much longer than a stretch, each workgroup takes one item whole and none is joined.
+    constexpr int kMinUnits = join_units(BF16);
+    const Division cut = divide(units, p.wgs, kMinUnits);
     const bool whole_items = each == 1 && items <= p.wgs && uniform(longest) <= units / p.wgs + 1 + kMinUnits;
-    auto start = [&](int w) { return whole_items ? s_units[min(w, items)] : w * share + min(w, more); };
-    auto owner = [&](int u) { return u < more * (share + 1) ? u / (share + 1) : more + (u - more * (share + 1)) / share; };
-    if (wg >= (whole_items ? items : wgs)) return;
+    auto start = [&](int w) { return whole_items ? s_units[min(w, items)] : cut.start(w); };
+    if (wg >= (whole_items ? items : cut.wgs)) return;
     const int u0 = uniform(start(wg)), u1 = uniform(start(wg + 1));  // this workgroup's
     if (u0 == u1) return;
     if (s_units[tid] <= u0 && u0 < s_units[tid + 1]) s_chunk = tid;
@@ -315,11 +261,11 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
     for (int n_units; before < u1; before += n_units, ++item) {
         const Seq s = uniform(each == 1 ? s_seq[item] : seq_at(item));
         n_units = each == 1 ? uniform(s_units[item + 1]) - before : uniform(units_at(item, s));
-        if (before + n_units <= u0) continue;
+        if (!works_on(before, n_units, u0)) continue;
         const int b = item / p.tiles, tile = item - b * p.tiles;
-        const int row0 = tile * p.tile_rows;
-        const int rows = min(s.n * p.h - row0, p.tile_rows);
-        const int i_lo = uniform(row0 / p.h), i_hi = uniform((row0 + rows - 1) / p.h);
+        const Tile its = item_tile(p, s, tile);
+        const int row0 = its.row0, rows = its.rows;
+        const int i_lo = uniform(its.i_lo), i_hi = uniform(its.i_hi);
         const Range range = tile_range(a, s, i_lo, i_hi);
         const int from = max(u0, before), to = min(u1, before + n_units);
         const int c0 = range.lo + (from - before) * kUnit, c1 = min(range.lo + (to - before) * kUnit, range.hi);
@@ -625,7 +571,7 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
         if (from != before || to != before + n_units) {
             // A part of an item.  What a workgroup leaves of an item that its stretch begins with goes to
             // its first slot, of one that begins later to its second.
-            const int w_first = owner(before), n_parts = owner(before + n_units - 1) - w_first + 1;
+            const int w_first = cut.owner(before), n_parts = cut.owner(before + n_units - 1) - w_first + 1;
             float* dst = slot_of(wg, from == u0 ? 0 : 1);
 #pragma unroll
             for (int i = 0; i < NP; ++i) leave2(dst + (i * NT + et) * 2, y[i].x, y[i].y);
@@ -1164,69 +1110,6 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a, Plan p)
     if (lane == 0 && a.lse) a.lse[item] = none ? kNoScore : (top + log2f(total)) * kLn2;
 }
 
-constexpr int kMaxParts = 64;   // join_kernel holds a part's weight in a lane
-constexpr int kMinChunk = 256;  // tile_kernel: cached tokens of a part at least
-// A block's time in 8 waves of one workgroup to that in 4 of each of two (D=128, 2048 tokens behind 14336:
-// 568 us and 624; D=64: 388 and 402; 8 x 512 behind 1536: 110 and 114; 4 x 2048 behind none: 118 and 115,
-// where the wider tile's triangle costs more).
-constexpr double kWide = 0.9;
-constexpr int kCus = 256;
-
-int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
-
-Plan make_plan(const CacheArgs& c, int H, bool bf16, int span) {
-    Plan p;
-    p.h = H / c.G;
-    const long most = (long)c.max_new * p.h;
-    // tile_kernel for more rows than the other has registers for, and for fewer over a cache of up to 2^19
-    // tokens of all key/value heads (2^20 with more than 32 rows; a fourth of either where a head's outputs
-    // leave one workgroup a CU), which end before the other's division and joins pay.  D=128, G=8, us here
-    // and there: 4 rows, 8 x 1500 18 and 24, 2 x 8000 20 and 25, 16 x 4096 43 and 42, 32 x 4096 74 and 66;
-    // 20 rows, 64 x 1024 39 and 54, 16 x 4096 43 and 45, 32 x 4096 78 and 70; 48 rows, 64 x 1024 44 and 79,
-    // 64 x 4096 163 and 160; D=256, G=4, 48 rows, 16 x 4096 70 and 99, 4 rows 65 and 43.  Up to 32 rows stay
-    // there where it has a workgroup for each sequence and no more to gain by joins: 4 rows, 4 x 512 15 and
-    // 13, 32 x 1000 31 and 23 (64 x 512, two sequences a workgroup: 24 and 33).
-    const long tokens = (long)c.B * c.G * span * (c.D > 128 ? 4 : 1);
-    const long units = (span + kUnit - 1) / kUnit;
-    const bool alone = (long)c.B * c.G <= kCus && units <= units * c.B * c.G / kCus + 5;
-    p.many = bf16 && (most > 64 || (most > 32 ? tokens <= 1 << 20 : tokens <= 1 << 19 && !alone));
-    p.wgs = p.parts = p.chunk = 0;
-    if (!p.many) {
-        // float32 rows in tiles of 32 while tiles of 64 would leave CUs without one (12 heads of 80, 37 tokens
-        // of 6 sequences: 40 us and 45; 1024 new of 4096 tokens of 16 heads, CUs full: 450 and 408)
-        const bool few = !bf16 && c.D > 64 && (long)c.B * c.G * ((most + 63) / 64) < kCus;
-        const int limit = c.D > 128 || few ? 32 : 64;
-        p.tile_rows = most <= 16 ? 16 : most <= 32 ? 32 : limit;
-        p.tiles = (int)((most + p.tile_rows - 1) / p.tile_rows);
-        p.wgs = std::max(kCus / c.G, 1);  // one a CU
-    } else {
-        // Rows of a workgroup and parts of the longest range, by the time they take in 64-token blocks:
-        // every round of resident workgroups takes a part and about 3 blocks to start and end; the join of
-        // 2 parts of 512 groups of 128 rows took as long as 13 blocks.
-        double best = -1;
-        for (int rows = 128; rows <= (c.D > 128 ? 128 : 256); rows *= 2) {
-            const long tiles = (most + rows - 1) / rows, groups = (long)c.B * c.G * tiles;
-            const long resident = kCus * (c.D > 128 || rows == 256 ? 1 : 2);
-            for (int parts = 1; parts <= kMaxParts && (parts - 1) * kMinChunk < span; ++parts) {
-                const int chunk = ((span + parts - 1) / parts + kMinChunk - 1) / kMinChunk * kMinChunk;
-                const double rounds = (double)((groups * parts + resident - 1) / resident);
-                const double join = parts > 1 ? 1.5 + groups * parts * (rows / 128) * (13.0 / 1024) : 0;
-                const double cost = rounds * (chunk / 64.0 + 3) * (rows == 256 ? kWide : 1.0) + join;
-                if (best >= 0 && cost >= best) continue;
-                best = cost;
-                p.tile_rows = rows;
-                p.tiles = (int)tiles;
-                p.chunk = chunk;
-            }
-        }
-        p.parts = (span + p.chunk - 1) / p.chunk;
-    }
-    p.page_shift = -1;
-    for (int k = 0; k <= 16; ++k)
-        if (c.P == 1 << k) p.page_shift = k;
-    return p;
-}
-
 template <bool BF16, int DP, bool FULL>
 void launch_stream(const AttentionArgs& a, const Plan& p, dim3 grid, hipStream_t stream) {
     if (p.tile_rows == 16)
@@ -1253,21 +1136,7 @@ void launch_tiles(const AttentionArgs& a, const Plan& p, dim3 grid, hipStream_t 
         hipLaunchKernelGGL((tile_kernel<DP, 4>), grid, dim3(256), 0, stream, a, p);
 }
 
-size_t plan_bytes(const Plan& p, const CacheArgs& c, int H) {
-    if (!p.many)
-        return align256(kCounterFloats * 4 + (size_t)p.wgs * c.G * 2 * p.tile_rows * (padded(c.D) + 2) * 4);
-    return p.parts == 1 ? 0 : align256(kCounterFloats * 4 + (size_t)p.parts * c.rows * H * (c.D + 2) * 4);
-}
-
 }  // namespace
-
-size_t attention_workspace(const CacheArgs& c, int H, bool bf16) { return plan_bytes(make_plan(c, H, bf16, c.max_kv), c, H); }
-
-bool attention_fits(const CacheArgs& c, int H, bool bf16) {
-    const Plan p = make_plan(c, H, bf16, c.max_kv);
-    if (!p.many) return (long)c.B * p.tiles * (c.max_kv / kUnit + 2) < 1L << 30;  // units
-    return (long)c.B * c.G * p.tiles * p.parts < 1L << 23;
-}
 
 hipError_t launch_attention(const AttentionArgs& a, bool bf16, hipStream_t stream) {
     const CacheArgs& c = a.c;

@@ -4,24 +4,10 @@
 
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
-
+#include "psd_attention_plan.hpp"
 #include "psd_layout.hpp"
 
 namespace psd {
-
-// Where a sequence's cached tokens lie (psd_cache, psd_seqs of the C ABI).
-struct CacheArgs {
-    void* k;
-    void* v;
-    int64_t stride_layer, stride_page, stride_token, stride_head;  // elements
-    int G, D, P, pages, layers;
-    int B, rows, max_new, max_kv, table_width;
-    int64_t table_stride;
-    const int32_t* new_start;
-    const int32_t* kv_len;
-    const int32_t* table;
-};
 
 struct RowsArgs {
     void* data;
@@ -64,8 +50,6 @@ struct AttentionArgs {
     void* workspace;
     size_t workspace_bytes;
 };
-size_t attention_workspace(const CacheArgs& c, int H, bool bf16);
-bool attention_fits(const CacheArgs& c, int H, bool bf16);  // the launch stays inside a grid's limits
 hipError_t launch_attention(const AttentionArgs& a, bool bf16, hipStream_t stream);
 
 struct GivenArgs {

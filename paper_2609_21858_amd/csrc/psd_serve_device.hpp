@@ -56,29 +56,6 @@ struct Elem<false> {
     }
 };
 
-// One sequence of the call, with the host's bounds applied.
-struct Seq {
-    int row0;   // packed row of its first new token
-    int n;      // new tokens computed (at most max_new, rows inside the call's)
-    int first;  // cache position of its first new token (may be negative)
-    int kv;     // cached tokens that can be seen (positions [0, kv))
-    int total;  // its new tokens, computed or not
-};
-__device__ __forceinline__ Seq load_seq(const CacheArgs& c, int b) {
-    // lengths that no call can have are cut, so that positions and their differences stay inside 32 bits
-    Seq s;
-    const int lo = max(c.new_start[b], 0), hi = min(c.new_start[b + 1], 1 << 24);
-    const int len = min(max(c.kv_len[b], 0), 1 << 30);
-    const int total = max(hi - lo, 0);
-    s.total = total;
-    s.row0 = lo;
-    s.n = min(min(total, c.max_new), max(c.rows - s.row0, 0));
-    s.first = len - total;
-    const long width = (long)c.table_width * c.P;
-    s.kv = max(min(min(len, c.max_kv), (int)min(width, (long)c.max_kv)), 0);
-    return s;
-}
-
 // The sequence of packed row t: the number of b with new_start[b + 1] <= t.  Called by whole
 // waves; 64 probes a step, so that up to 64 sequences cost one load's latency and 4096 two.
 __device__ __forceinline__ int find_seq(const int32_t* new_start, int B, int t) {
