@@ -419,7 +419,7 @@ typedef struct {
 typedef struct {
     int32_t batch;         /* B, 1..PSD_MAX_BATCH */
     int32_t rows;          /* T, 1..PSD_MAX_ROWS: packed rows of the call (an upper bound of new_start[B]) */
-    int32_t max_new;       /* >= 1: upper bound of n_b */
+    int32_t max_new;       /* >= 1: upper bound of n_b (taken as at most rows) */
     int32_t max_kv;        /* 1..PSD_MAX_KV: upper bound of kv_len[b] */
     int32_t table_width;   /* >= 1: entries of a table row */
     int64_t table_stride;  /* entries from one row of the table to the next */

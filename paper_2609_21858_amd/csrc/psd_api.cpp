@@ -437,7 +437,7 @@ psd::CacheArgs cache_args(const psd_cache* c, const psd_seqs* s) {
     a.layers = c->layers;
     a.B = s->batch;
     a.rows = s->rows;
-    a.max_new = s->max_new;
+    a.max_new = std::min(s->max_new, s->rows);  // no sequence has more rows than the call
     a.max_kv = s->max_kv;
     a.table_width = s->table_width;
     a.table_stride = s->table_stride;

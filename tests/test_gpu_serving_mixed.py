@@ -46,3 +46,11 @@ def test_two_tiles_of_large_heads(psd):
 def test_bounds_far_above_the_lengths(psd, dtype):
     check_attention(psd, [(5, 300), (1, 40), (1, 900)], 32, 8, 128, 16, dtype, max_new=400)
     check_attention(psd, [(3, 300), (2, 40), (1, 900)], 8, 8, 64, 16, dtype, max_new=1000, max_kv=1 << 20)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("most", [1 << 16, (1 << 31) - 1])
+def test_any_bound_of_new_tokens(psd, most, dtype):
+    """A bound above the call's rows is that of its rows: the work is done, and no index passes 32 bits."""
+    check_attention(psd, [(5, 300), (1, 40)], 8, 2, 64, 16, dtype, max_new=most)
+    check_attention(psd, [(3, 100), (70, 80)], 64, 1, 128, 16, dtype, max_new=most)
