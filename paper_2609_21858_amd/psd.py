@@ -460,6 +460,17 @@ def _ints(t, what: str, dim: int, rows: int = 0):
         _refuse(f"{what}: int32 with {dim} dimensions, at least {rows} long, the last dimension contiguous")
 
 
+def _row_stride(t, what: str) -> int:
+    """Elements from one row of a matrix of indices to the next; rows that overlap (an expanded tensor's lie on one
+    another) have no stride that the calls could take."""
+    rows, width = t.shape
+    if rows == 1:
+        return width
+    if t.stride(0) < width:
+        _refuse(f"{what}: rows overlap (stride {t.stride(0)}, width {width}); .contiguous() gives each its own")
+    return t.stride(0)
+
+
 def make_cache(k, v) -> Cache:
     """Pools [pages][page tokens][heads][head dim] (or [layers][pages]...) of any strides with a contiguous
     last dimension; keeps both tensors alive."""
@@ -484,7 +495,7 @@ def make_seqs(new_start, kv_len, table, rows: int, max_new: int, max_kv: int) ->
     B = int(kv_len.shape[0])
     if new_start.shape[0] != B + 1 or table.shape[0] != B:
         _refuse("new_start [B+1], kv_len [B] and table [B][width] disagree")
-    s = Seqs(B, int(rows), int(max_new), int(max_kv), table.shape[1], max(table.stride(0), table.shape[1]),
+    s = Seqs(B, int(rows), int(max_new), int(max_kv), table.shape[1], _row_stride(table, "table"),
              new_start.data_ptr(), kv_len.data_ptr(), table.data_ptr())
     s.tensors = (new_start, kv_len, table)
     return s
@@ -588,8 +599,8 @@ def kv_keep(cache: Cache, seqs: Seqs, keep, n_keep, kv_out=None, stream=None):
         kv_out = torch.empty((B,), dtype=torch.int32, device=keep.device)
     else:
         _ints(kv_out, "kv_out", 1, B)
-    _check(_lib.psd_kv_keep(ctypes.byref(cache), ctypes.byref(seqs), _ptr(keep), max(keep.stride(0), keep.shape[1]),
-                            keep.shape[1], _ptr(n_keep), _ptr(kv_out), _stream(stream)))
+    _check(_lib.psd_kv_keep(ctypes.byref(cache), ctypes.byref(seqs), _ptr(keep), _row_stride(keep, "keep"), keep.shape[1],
+                            _ptr(n_keep), _ptr(kv_out), _stream(stream)))
     return kv_out
 
 

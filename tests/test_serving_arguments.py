@@ -24,3 +24,56 @@ def test_far_bound_of_new_tokens(psd, H, G, D, dtype):
         n = psd.attention_workspace_bytes(c, s, H)
         assert want is None or n == want, most
         want = n
+
+
+class Calls:
+    """Stands for the library: records the calls, launches nothing."""
+
+    def __init__(self):
+        self.seen = []
+
+    def psd_kv_keep(self, *args):
+        self.seen.append(args)
+        return 0
+
+
+def small_call(psd, B=3):
+    pool = torch.zeros((8, 16, 2, 64), dtype=torch.bfloat16)
+    start, kv = torch.arange(B + 1, dtype=torch.int32), torch.full((B,), 9, dtype=torch.int32)
+    seqs = psd.make_seqs(start, kv, torch.zeros((B, 2), dtype=torch.int32), B, 1, 32)
+    return psd.make_cache(pool, pool.clone()), seqs, start, kv
+
+
+def test_rows_of_the_page_table(psd):
+    start, kv = torch.arange(4, dtype=torch.int32), torch.full((3,), 9, dtype=torch.int32)
+    one = torch.zeros((1, 5), dtype=torch.int32)
+    wide = torch.zeros((3, 9), dtype=torch.int32)
+    overlapping = torch.zeros(30, dtype=torch.int32).as_strided((3, 5), (4, 1))
+    for bad in (one.expand(3, -1), one[:, :1].expand(3, 1), overlapping):
+        with pytest.raises(psd.PsdError) as e:
+            psd.make_seqs(start, kv, bad, 3, 1, 32)
+        assert e.value.status == psd.PSD_E_ARG
+    assert psd.make_seqs(start, kv, wide[:, 2:7], 3, 1, 32).table_stride == 9
+    assert psd.make_seqs(start, kv, torch.zeros(30, dtype=torch.int32).as_strided((3, 5), (5, 1)), 3, 1, 32).table_stride == 5
+    for single in (one, one.expand(1, -1), torch.zeros(9, dtype=torch.int32).as_strided((1, 5), (0, 1))):
+        assert psd.make_seqs(start[:2], kv[:1], single, 1, 1, 32).table_stride == 5
+
+
+def test_rows_of_kept_indices(psd, monkeypatch):
+    """One path's indices, the same for every sequence: an expanded tensor has one row in memory, not B."""
+    cache, seqs, start, kv = small_call(psd)
+    calls = Calls()
+    monkeypatch.setattr(psd, "_lib", calls)
+    monkeypatch.setattr(psd, "_stream", lambda stream=None: None)
+    n_keep = torch.ones(3, dtype=torch.int32)
+    path = torch.arange(5, dtype=torch.int32)
+    for bad in (path.expand(3, -1), path[:1].expand(3, 1), torch.zeros(30, dtype=torch.int32).as_strided((3, 5), (3, 1))):
+        with pytest.raises(psd.PsdError) as e:
+            psd.kv_keep(cache, seqs, bad, n_keep)
+        assert e.value.status == psd.PSD_E_ARG and not calls.seen
+    for good, stride in ((path.expand(3, -1).contiguous(), 5), (torch.zeros((3, 8), dtype=torch.int32)[:, 1:6], 8)):
+        psd.kv_keep(cache, seqs, good, n_keep)
+        assert calls.seen.pop()[3:5] == (stride, 5)
+    one_cache, one_seqs, _, _ = small_call(psd, 1)
+    psd.kv_keep(one_cache, one_seqs, path.expand(1, -1), n_keep[:1])
+    assert calls.seen.pop()[3:5] == (5, 5)
