@@ -35,6 +35,8 @@ constexpr float kNoScore = -__builtin_inff();
 // 2^8, sums exact to float32 as before, and most blocks need no exchange between lanes.
 constexpr float kSlack = 8.f;
 constexpr float kHuge = 3e38f;
+// Scores above this (units of ln 2) are taken from the maximum before they are scaled, see tile_kernel.
+constexpr float kFar = 1 << 20;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -755,7 +757,7 @@ __global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[db][e] = 0.f;
-    float m = kNoScore, l = 0.f;
+    float m = kNoScore, l = 0.f;  // m: of products, scaled at the end
 
     const int64_t head_at = (int64_t)g * c.stride_head;
     const int piece = tid % S::LPR, token = tid / S::LPR;
@@ -924,17 +926,30 @@ __global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) top = fmaxf(top, sv[t][e]);
-            top *= sc;
-            if (__any(top > m + kSlack)) {
+            float from = m * sc;
+            if (__any(top * sc > from + kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 32));
                 const float next = fmaxf(m, top);
-                const float by = next == kNoScore ? 1.f : exp2_hw(m - next);
+                const float by = next == kNoScore ? 1.f : exp2_hw((m - next) * sc);
                 m = next;
+                from = m * sc;
                 l *= by;
 #pragma unroll
                 for (int db = 0; db < DB; ++db) o[db] *= by;
             }
-            const float from = m == kNoScore ? 0.f : m;
+            // The exponent is fma(sv, sc, -from): a row's weights have the rounding of `from` in common, which the
+            // division by their sum takes out, but which is no rounding error any more where scores are so large
+            // that it reaches float32's range of exponents.  There the maximum is taken out before the scale.
+            const bool none = from == kNoScore;
+            from = none ? 0.f : from;
+            if (__any(fabsf(from) > kFar)) {
+                const float base = none ? 0.f : m;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sv[t][e] -= base;
+                from -= from;  // (a maximum that is infinite when scaled: NaN)
+            }
             // Weights of 16 tokens at a time, and their product with the values, whose pieces are read 16 tokens ahead:
             // exponentials and reads go between the products.
             auto weights = [&](int ks) {
@@ -1018,6 +1033,7 @@ __global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_
     }
 
     l += __shfl_xor(l, 32);
+    m *= sc;
     if (!on) return;
     if (n_parts == 1) {
         const bool none = m == kNoScore && l == 0.f;
