@@ -497,7 +497,8 @@ size_t psd_attention_workspace_bytes(const psd_cache *cache, const psd_seqs *seq
  *   keep     device [B][keep_stride] int32, strictly ascending in each row (other orders give
  *            undefined values); an index outside [0, n_b) moves nothing
  *   n_keep   device [B] int32, taken as at most keep_width and n_b; at least 0
- *   kv_out   device [B] int32, nullable: kv_len - n_b + n_keep; not seqs->kv_len itself
+ *   kv_out   device [B] int32, nullable: kv_len - n_b + n_keep; it shares no memory with kv_len,
+ *            new_start, n_keep or keep, which are read while it is written
  * 1 <= keep_width <= keep_stride.  One launch. */
 psd_status psd_kv_keep(const psd_cache *cache, const psd_seqs *seqs, const int32_t *keep, int64_t keep_stride,
                        int32_t keep_width, const int32_t *n_keep, int32_t *kv_out, hipStream_t stream);

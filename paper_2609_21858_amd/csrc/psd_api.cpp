@@ -422,6 +422,11 @@ psd_status check_heads(const psd_cache* c, int q_heads) {
     return PSD_OK;
 }
 
+// Do n elements at a and m at b share memory?
+bool overlap(const int32_t* a, int64_t n, const int32_t* b, int64_t m) {
+    return (uintptr_t)a < (uintptr_t)b + 4 * (uintptr_t)m && (uintptr_t)b < (uintptr_t)a + 4 * (uintptr_t)n;
+}
+
 psd::CacheArgs cache_args(const psd_cache* c, const psd_seqs* s) {
     psd::CacheArgs a;
     a.k = c->k;
@@ -1228,7 +1233,11 @@ psd_status psd_kv_keep(const psd_cache* cache, const psd_seqs* seqs, const int32
     if ((st = check_cache(cache, true)) != PSD_OK || (st = check_seqs(seqs, true)) != PSD_OK) return st;
     if (!keep || !n_keep) return fail(PSD_E_ARG, "keep / n_keep is NULL");
     if (keep_width < 1 || keep_stride < keep_width) return fail(PSD_E_ARG, "keep_width must be in [1, keep_stride]");
-    if (kv_out == seqs->kv_len) return fail(PSD_E_ARG, "kv_out must not be kv_len");
+    // its first workgroup writes kv_out while the others still read these
+    const int64_t B = seqs->batch;
+    if (kv_out && (overlap(kv_out, B, seqs->kv_len, B) || overlap(kv_out, B, seqs->new_start, B + 1) ||
+                   overlap(kv_out, B, n_keep, B) || overlap(kv_out, B, keep, (B - 1) * keep_stride + keep_width)))
+        return fail(PSD_E_ARG, "kv_out must not share memory with kv_len, new_start, n_keep or keep");
     const long blocks = (2L * cache->heads * cache->head_dim / 4 + 255) / 256 * seqs->batch;
     if (blocks > kMaxGrid) return fail(PSD_E_ARG, "call too large (%ld workgroups)", blocks);
     psd::KeepArgs a;

@@ -77,3 +77,15 @@ def test_rows_of_kept_indices(psd, monkeypatch):
     one_cache, one_seqs, _, _ = small_call(psd, 1)
     psd.kv_keep(one_cache, one_seqs, path.expand(1, -1), n_keep[:1])
     assert calls.seen.pop()[3:5] == (5, 5)
+
+
+def test_new_lengths_share_no_memory_with_what_is_read(psd):
+    """kv_out is written by one workgroup while others read the lengths, row starts and kept indices."""
+    from test_serving_abi import keep
+
+    base = 1 << 20
+    parts = structs(psd, s__kv_len=base, s__new_start=base + 4096)  # four sequences
+    for out in (base, base - 12, base + 12, base + 4096, base + 4096 + 16, base + 8192, base + 8192 + 12, base + 12288,
+                base + 12288 + 4 * 19):
+        assert keep(psd, *parts, idx=base + 12288, n=base + 8192, out=out) == psd.PSD_E_ARG, out - base
+        assert b"kv_out" in psd.lib().psd_last_error()
