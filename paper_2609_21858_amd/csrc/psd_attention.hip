@@ -96,7 +96,11 @@ __device__ __forceinline__ f32x4 multiply(const u32x4 x, const u32x4 y, f32x4 ac
     }
 }
 
-// A block's softmax weights of this lane's row as a B operand.
+// A block's softmax weights of this lane's row as a B operand.  In bfloat16 they are rounded to it, since the
+// matrix instructions take both operands in one type, and a second product of what the rounding left out would
+// double the half of the products that are O^T = V^T P^T.  Each weight errs by 2^-8 of itself at most; maxima, sums
+// (of the weights before they are rounded), lse and outputs stay in float32.  Normally distributed inputs: outputs
+// 2.3e-3 of their size from those of 64 bits, where the rounding of the result alone is 1.7e-3.
 template <bool BF16>
 struct Weights {
     u32x4 all;
@@ -138,7 +142,13 @@ __device__ __forceinline__ u32x4 stream_load(const char* at) {
 // of one new token and up to 16384 cached, 1.37 GB: 237 us, 5.75 TB/s (a plain read of memory in the same
 // order reads 5.9 - 6.2); 5 new tokens of 64 sequences, up to 4096 cached, 676 MB: 137 us.  One token of 4
 // sequences, up to 512 cached: 13 us, of them 2 to divide the work, 2 to the first key, 5 in the loop and
-// 2 to join.  Float32 is bound by its products (12 heads of 80, 37 tokens, window 700: 38 us).
+// 2 to join.
+// Float32, one token of 32 sequences, up to 4096 cached, 683 MB: 131 us; up to 16384: 452, 6.0 TB/s, memory again.
+// More rows: 5 tokens of 32 sequences, up to 4096 cached, 239; 1024 new of 4096 804, 75 TFLOP/s (a library
+// product 153).  Tiles of 32 and 64 rows spill there: DP=128 43 - 63 registers, DP=256 126 - 161, DP=64 with 64 rows 5 - 14
+// (in bfloat16 DP=256 with 32 rows, 26 - 59).  12 heads of 80, 37 tokens, window 700: 38 us with the products busy 13 %
+// of it.  About 25 are the same for any length (without a window 300 cached tokens take 26, 3000 65, 6000 105): starts of
+// stretches of one or two units, 135 KB of the waves' outputs joined through LDS, parts.  Heads of 64, unpadded: 25.
 template <bool BF16, int DP>
 struct StreamShape {
     static constexpr int TOK = BF16 ? 32 : 16;
@@ -677,9 +687,11 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
 // block n is computed, block n + 1 is on its way into registers, and is stored behind the
 // arithmetic.  Two waves a SIMD, so one wave's exponentials overlap the other's products: one
 // workgroup of 8 waves a CU, which loads and stores half as much a row, or two of 4 for fewer rows.
-// 2048 new tokens behind 14336, H=32, G=8, D=128: 531 - 556 us, 925 - 970 TFLOP/s (a large library product
-// reaches 1370); without its loads and stores of keys and values 440.  In LDS two buffers of 20 KB of values
-// and 17 of keys.
+// 2048 new tokens behind 14336, H=32, G=8, D=128: 544 - 570 us, 904 - 948 TFLOP/s (a large library product
+// reaches 1370), the products busy 44 % of it; without its loads and stores of keys and values 440.  In LDS two
+// buffers of 20 KB of values and 17 of keys.  Other heads, the same tokens: D=64 368 - 418 us; D=80, 96 and 112, padded to
+// 128, 534 - 557; D=192, padded to 256, 1652; D=256 1625 - 1672 (one workgroup a CU, 24 registers spilled).  Window 4096,
+// D=128: 157.  One token of 64 sequences, up to 4096 cached, window 1000, 263 MB: 46.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 template <int DP, int NW>

@@ -73,8 +73,8 @@ struct Plan {
 constexpr int kUnit = 128;  // cached tokens: a block of each wave (two in float32)
 // Units that a workgroup has at least, if it has to join: leaving and joining the parts of an item
 // takes as long as about so many (4 bfloat16 sequences of up to 512 tokens 13 us, with 2 units 20; under a
-// far bound 8 sequences of 5 rows, up to 1500 tokens 28, with 8 units 40).  Float32 rows are bound by their
-// products (37 rows of 12 heads 38 us, with 4 units 49).
+// far bound 8 sequences of 5 rows, up to 1500 tokens 28, with 8 units 40).  A float32 unit takes so much longer that
+// joins pay from one on (37 tokens of 12 heads 38 us, with 4 units 49).
 constexpr int join_units(bool bf16) { return bf16 ? 4 : 1; }
 
 // Threads of the few-row kernel: one workgroup a CU, two waves a SIMD, or one where the rows' outputs take
@@ -161,7 +161,10 @@ inline Plan make_plan(const CacheArgs& c, int H, bool bf16, int span) {
     // 20 rows, 64 x 1024 39 and 54, 16 x 4096 43 and 45, 32 x 4096 78 and 70; 48 rows, 64 x 1024 44 and 79,
     // 64 x 4096 163 and 160; D=256, G=4, 48 rows, 16 x 4096 70 and 99, 4 rows 65 and 43.  Up to 32 rows stay
     // there where it has a workgroup for each sequence and no more to gain by joins: 4 rows, 4 x 512 15 and
-    // 13, 32 x 1000 31 and 23 (64 x 512, two sequences a workgroup: 24 and 33).
+    // 13, 32 x 1000 31 and 23 (64 x 512, two sequences a workgroup: 24 and 33).  With one or two heads tile_kernel
+    // has 64 or 128 parts for 256 CUs and is ahead all the same, since one workgroup joins a long item there: 8 rows,
+    // G=1, 1 x 8192 15 and 22, 1 x 131072 59 and 107, 4 x 131072 59 and 68; G=2, 1 x 131072 59 and 73; 48 rows, G=1,
+    // 1 x 131072 60 and 245.
     const long tokens = (long)c.B * c.G * span * (c.D > 128 ? 4 : 1);
     const long units = (span + kUnit - 1) / kUnit;
     const bool alone = (long)c.B * c.G <= kCus && units <= units * c.B * c.G / kCus + 5;

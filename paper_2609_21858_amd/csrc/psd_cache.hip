@@ -5,8 +5,9 @@
 //   (y_a, y_b) <- (y_a cos - y_b sin, y_b cos + y_a sin)  for the R/2 pairs (a, b) of the first
 //   R dimensions, with the row's cosine and sine; one rounding to the output's type.
 // It reads and writes each element once, so memory bounds it: (H + 2G) D elements a row both
-// ways.  8 prompts of up to 2048 tokens, H=32, G=8, D=128, bfloat16, normed: 53.8 us, 5.2 TB/s read
-// and written (a device copy moves 4.9); one token of 4 sequences, three dependent loads: 4.5 us.
+// ways.  8 prompts of up to 2048 tokens, H=32, G=8, D=128, bfloat16, normed: 53.4 us, 5.2 TB/s read
+// and written (a device copy moves 4.9), float32 119.5 us, 4.7 TB/s; one token of 4 sequences, three dependent
+// loads: 4.4 us, float32 6.5.
 #include <hip/hip_runtime.h>
 
 #include "psd_serve.hpp"
@@ -238,8 +239,8 @@ constexpr int kKeepBatch = 4;
 constexpr int kKeepPlaces = 64;
 
 // Moves 2 G D elements a kept token and layer, both ways.  The chain of dependent loads bounds it: 32
-// layers of 64 sequences, K=4, gamma=4, G=8, D=128: 8.5 us (25 MB, 5.1 us at a copy's rate); 4 layers of
-// one sequence: 3.3 us.
+// layers of 64 sequences, K=4, gamma=4, G=8, D=128: 7.9 us (25 MB, 5.1 us at a copy's rate), float32 12.4; 4
+// layers of one sequence: 3.2 us.
 //
 // One thread moves one 16-byte column (keys or values, head, piece) of a sequence's kept
 // tokens in one layer.  The places of 64 tokens at a time are found by 64 threads together: the

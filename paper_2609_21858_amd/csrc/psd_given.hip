@@ -12,9 +12,10 @@
 // first launch has just brought into the caches; only e comes new from memory.  The last
 // workgroup of a sequence writes its tokens.
 //
-// V=128256, gamma=4, 64 sequences, bfloat16: 26.0 us for the rows (5.7 TB/s), then 20.8 us for the race,
-// which its chain bounds: segments' sums, acceptance, the row's and e's first pieces, then the join (35 MB).
-// V=1024, gamma=4, one sequence: 9.0 us in one launch, two chains of load, exponentials and exchange.
+// V=128256, gamma=4, 64 sequences, bfloat16: 26 us for the rows (5.7 TB/s), then 21 - 22 us for the race,
+// which its chain bounds: segments' sums, acceptance, the row's and e's first pieces, the second round's pieces of
+// the rows, which are asked for only when it begins, then the join (35 MB).  Float32, 32 sequences: 24 us (6.1 TB/s)
+// and 17.  V=1024, gamma=4, one sequence: 8.9 us in one launch, two chains of load, exponentials and exchange.
 //
 // Rounding: maxima are exact; exponentials are of (l - max) / T, where the subtraction is
 // exact near the top of a row, and sums are float32 sums of at most a few thousand values a
