@@ -503,6 +503,152 @@ size_t psd_attention_workspace_bytes(const psd_cache *cache, const psd_seqs *seq
 psd_status psd_kv_keep(const psd_cache *cache, const psd_seqs *seqs, const int32_t *keep, int64_t keep_stride,
                        int32_t keep_width, const int32_t *n_keep, int32_t *kv_out, hipStream_t stream);
 
+/* ---- the same over a cache held in 4 bits -------------------------------------- */
+
+/* Keys and values in pages of 4-bit codes.  Each 32 dimensions of a head (a group; the last
+ * may be shorter) take 16 bytes of codes and one scale byte:
+ *   dimension d is the nibble d % 2 (0: the low one) of byte d / 2 of its head's codes,
+ *   code c stands for the (c & 7)th of 0, 0.5, 1, 1.5, 2, 3, 4, 6, negative with c & 8,
+ *   times 2^(s - 127) for scale byte s; s = 255 makes the whole group NaN (253 and 254, whose
+ *   larger codes pass float32's range, are never written and count as no finite number).
+ * A quarter and a bit of bfloat16's bytes; every value is exact in bfloat16, and gfx950
+ * converts two codes in one instruction.  With groups = ceil(D / 32), the codes of (layer l,
+ * page p, place i, head g) are the 16 groups bytes at l * stride_layer + p * stride_page +
+ * i * stride_token + g * stride_head from k (keys) or v (values), their scales the `groups`
+ * bytes at the same sum of scale_* from k_scale or v_scale.  All strides in bytes; code
+ * pointers and strides are multiples of 16, scales have any.  Codes past dimension D are
+ * written as 0 and count as nothing.  No two elements of the four pools overlap.
+ * Fastest with a head's page in one piece: places before heads in stride (stride_token =
+ * 16 groups), since one workgroup reads one head. */
+typedef struct {
+    void *k;              /* device: codes of the keys */
+    void *v;              /* device: codes of the values */
+    void *k_scale;        /* device: scale bytes of the keys */
+    void *v_scale;        /* device: scale bytes of the values */
+    int32_t dtype;        /* psd_dtype of new keys and values, queries and outputs */
+    int32_t heads;        /* G, 1..PSD_MAX_HEADS */
+    int32_t head_dim;     /* D, a multiple of 8, 8..PSD_MAX_HEAD_DIM */
+    int32_t page_tokens;  /* P, 1..65536 */
+    int32_t pages;        /* >= 1 */
+    int32_t layers;       /* as in psd_cache */
+    int64_t stride_layer; /* bytes; read with layers > 1 */
+    int64_t stride_page;
+    int64_t stride_token;
+    int64_t stride_head;
+    int64_t scale_layer;  /* bytes; read with layers > 1 */
+    int64_t scale_page;
+    int64_t scale_token;
+    int64_t scale_head;
+} psd_cache4;
+
+/* psd_kv_append into 4 bits.  A group whose largest magnitude is m takes the scale 2^k, k the
+ * least integer in [-126, 125] with m <= 7 * 2^k (125 where there is none), so that no element errs
+ * by more than 2^k; its codes are the nearest, ties to the even code, at most 6, and a negative
+ * element that rounds to 0 is -0.  A group with a NaN or an infinite element (or one past float32's
+ * range) becomes NaN.  Keys are normed
+ * and turned in 64 bits before that, so that a key's code is its definition's; queries in float32
+ * as in psd_kv_append.
+ *   k_held, v_held  [T][G][D] (dtype), nullable: the values that the cache now holds for the new
+ *                   keys and values (also of tokens that have no place) */
+psd_status psd_kv_append4(const psd_cache4 *cache, const psd_seqs *seqs, const psd_rotation *rotation,
+                          const psd_rows *k, const psd_rows *v, const psd_rows *q, const psd_rows *q_out,
+                          int32_t q_heads, const psd_rows *k_held, const psd_rows *v_held, hipStream_t stream);
+
+/* psd_attention over the values that a 4-bit cache stands for: same rows, windows, masks, outputs
+ * and workspace rules.  bfloat16 rows as there; float32 rows are computed to float32's precision:
+ * queries and softmax weights as three bfloat16 terms each (24 bits), whose products with codes are
+ * exact, summed in float32. */
+psd_status psd_attention4(const psd_cache4 *cache, const psd_seqs *seqs, const psd_rows *q, int32_t q_heads, float scale,
+                          int32_t window, const uint32_t *mask, int32_t mask_words, const psd_rows *out, float *lse,
+                          void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* As psd_attention_workspace_bytes. */
+size_t psd_attention4_workspace_bytes(const psd_cache4 *cache, const psd_seqs *seqs, int32_t q_heads);
+
+/* psd_kv_keep over a 4-bit cache: codes and scales move as they are. */
+psd_status psd_kv_keep4(const psd_cache4 *cache, const psd_seqs *seqs, const int32_t *keep, int64_t keep_stride,
+                        int32_t keep_width, const int32_t *n_keep, int32_t *kv_out, hipStream_t stream);
+
+/* ---- places for a call's tokens ------------------------------------------------ */
+
+/* The free pages of a pool, in a ring: free page i is ring[(state[0] + i) % pages], i < state[1].
+ * All of them at first: ring = 0 .. pages - 1, state = {0, pages, 0, 0}. */
+typedef struct {
+    int32_t page_tokens; /* P, 1..65536 */
+    int32_t pages;       /* entries of the ring, >= 1 */
+    int32_t *ring;       /* device [pages] */
+    int32_t *state;      /* device [4]: first free page, free pages, two words that are 0 between calls */
+} psd_pages;
+
+/* What each sequence asks for, and what it got. */
+typedef struct {
+    const int32_t *n_new;   /* device [B]: new tokens asked for (negative: 0) */
+    const int32_t *kv_have; /* device [B]: cached tokens that stay (psd_kv_keep's kv_out; 0: a new or an ended one) */
+    int32_t *held;          /* device [B], in/out: pages that the sequence holds, table[b][0 .. held) */
+    int32_t *table;         /* device [B][seqs->table_stride], in/out */
+    int32_t *new_start;     /* device [B+1], out */
+    int32_t *kv_len;        /* device [B], out */
+    int32_t *granted;       /* device [B], out, nullable: new tokens granted: all that were asked for, or 0 */
+    int32_t *row_seq;       /* device [T], out, nullable: sequence of each packed row, -1 past the last */
+    int32_t *positions;     /* device [T], out, nullable: its cache position, -1 past the last */
+    int64_t *slots;         /* device [T], out, nullable: page * P + place, -1 past the last */
+} psd_reservation;
+
+/* Reserve places for each sequence's new tokens behind the kv_have that stay, and take back the
+ * pages that no token needs any more: lengths go in, and what psd_kv_append, psd_attention and
+ * psd_kv_keep read (psd_seqs) comes out, without the host.
+ *   need  = pages of kv_have + n_new past `held`.  A sequence gets all or nothing.  It is refused, and
+ *           keeps kv_have, if n_new passes seqs->max_new, or kv_have + n_new seqs->max_kv or the
+ *           table's width; or if, summed over the sequences up to it that are not refused by that,
+ *           n_new passes seqs->rows, or (it needs pages) `need` passes the pages that are free when
+ *           the call begins.  So earlier sequences go first, and one that is refused for want
+ *           of pages holds back those behind it that need some.
+ *   pages past the end of kv_len = kv_have + granted go back behind the free ones, in the order of sequences
+ *           and of their tables, for the next call; their table entries become -1.  Pages that are
+ *           taken come off the front in the order of sequences.
+ * Of `seqs` batch, rows, max_new, max_kv, table_width and table_stride are read, its pointers not (they may be
+ * the reservation's own).  kv_have above a sequence's max_kv or table is cut.  The outputs share no memory
+ * with each other or with what is read.  One call at a time on a ring.  One launch. */
+psd_status psd_kv_reserve(const psd_pages *pages, const psd_seqs *seqs, const psd_reservation *r, hipStream_t stream);
+
+/* ---- logits before a race or a draw --------------------------------------------- */
+
+#define PSD_MAX_TEXT ((1 << 20) - 64) /* tokens of a text that psd_adjust_logits counts */
+#define PSD_MAX_BIAS 1024             /* biased tokens of a sequence */
+
+/* Penalties for repeated tokens, biases and masks.  Every pointer is nullable: without it the
+ * term is left out. */
+typedef struct {
+    const int32_t *text;        /* device [B][text_stride]: tokens so far; those outside [0, V) are passed over */
+    int64_t text_stride;        /* >= text_max */
+    int32_t text_max;           /* 0..PSD_MAX_TEXT: upper bound of length (longer ones are cut) */
+    const int64_t *length;      /* device [B] (with text): text[b][from[b] .. length[b]) counts */
+    const int64_t *from;        /* device [B]: first token that counts; NULL: 0 */
+    const int32_t *draft_tokens; /* device [B][K][gamma]: the row of depth s on path k has also seen the path's
+                                    tokens before depth s */
+    int32_t gamma;              /* entries of a path in draft_tokens */
+    const float *repetition;    /* device [B]: rho > 0; NULL: 1 */
+    const float *presence;      /* device [B]; NULL: 0 */
+    const float *frequency;     /* device [B]; NULL: 0 */
+    const int32_t *bias_tokens; /* device [B][bias_width]; one outside [0, V) is passed over */
+    const float *bias;          /* device [B][bias_width] (with bias_tokens) */
+    int32_t bias_width;         /* 0..PSD_MAX_BIAS */
+    const uint32_t *allowed;    /* device: bit v % 32 of word v / 32 of a row's mask: token v may come */
+    int64_t allowed_seq;        /* words from one sequence's first mask to the next */
+    int64_t allowed_row;        /* words from one row's mask to the next; 0: a sequence's rows share one */
+} psd_adjustments;
+
+/* Adjust logits [B][K][S][V] (params' num_drafts K, vocab, dtype), row s of a path at depth depth0 + s: the target's
+ * rows for psd_verify (target_rows K, S = gamma + 1) or psd_verify_given (K = 1), a path's draft rows for psd_draft
+ * (S = s_count, depth0 = s_begin).  Token v that came c times in what its row has seen, with logit l:
+ *   c > 0:  l / rho if l > 0, else l rho; then minus frequency c + presence
+ *   then plus the sum of v's biases; -inf where v may not come.
+ * In float32, one rounding.  out may be logits itself (then only what changes is read or written) or shares no
+ * memory with it; -inf stays -inf for finite parameters.  0 <= depth0, depth0 + S <= gamma + 1 with
+ * draft_tokens.  Rows are PSD_MAX_DRAFTS paths of PSD_MAX_GAMMA + 1 at most.  One launch. */
+psd_status psd_adjust_logits(const psd_params *params, const psd_adjustments *adjust, int32_t batch, int32_t rows,
+                             int32_t depth0, const void *logits, void *out, hipStream_t stream);
+
 /* Verification of drafted tokens from given random numbers: the unkeyed rejection rule
  * that the paper's races are compared with.  With p_s = softmax(target row s / T_P) and
  * q_s = softmax(draft row s / T_Q), draft x_s is accepted while

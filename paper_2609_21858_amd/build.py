@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "lib", "libpsd.so")
 SOURCES = ["psd_race.hip", "psd_mpfr.hip", "psd_topk.hip", "psd_gen.hip", "psd_detect.hip", "psd_cache.hip",
-           "psd_attention.hip", "psd_given.hip", "psd_api.cpp"]
+           "psd_attention.hip", "psd_attention4.hip", "psd_given.hip", "psd_pages.hip", "psd_adjust.hip", "psd_api.cpp"]
 ARCH = "gfx950"
 # Packed-fp32 VALU forms are kept out of every kernel.
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang",

@@ -378,7 +378,9 @@ bool good_stride(int64_t elements, int bytes) {
     return elements >= 0 && elements < (int64_t)1 << 44 && (elements * bytes) % 16 == 0;
 }
 
-psd_status check_cache(const psd_cache* c, bool pointers) {
+// What a cache in either form is made of.
+template <class Cache>
+psd_status check_pages(const Cache* c) {
     if (!c) return fail(PSD_E_ARG, "cache is NULL");
     if (c->dtype != PSD_F32 && c->dtype != PSD_BF16) return fail(PSD_E_ARG, "unknown dtype %d", c->dtype);
     if (c->heads < 1 || c->heads > PSD_MAX_HEADS) return fail(PSD_E_ARG, "heads %d outside [1, %d]", c->heads, PSD_MAX_HEADS);
@@ -387,13 +389,33 @@ psd_status check_cache(const psd_cache* c, bool pointers) {
     if (c->page_tokens < 1 || c->page_tokens > 65536) return fail(PSD_E_ARG, "page_tokens %d outside [1, 65536]", c->page_tokens);
     if (c->pages < 1) return fail(PSD_E_ARG, "pages must be at least 1");
     if (c->layers < 1 || c->layers > 65535) return fail(PSD_E_ARG, "layers %d outside [1, 65535]", c->layers);
-    const int bytes = c->dtype == PSD_BF16 ? 2 : 4;
+    return PSD_OK;
+}
+
+// Strides and pointers of its keys and values, in units of `bytes`.
+template <class Cache>
+psd_status check_pools(const Cache* c, int bytes, bool pointers) {
     if (!good_stride(c->stride_page, bytes) || !good_stride(c->stride_token, bytes) || !good_stride(c->stride_head, bytes) ||
         (c->layers > 1 && !good_stride(c->stride_layer, bytes)))
         return fail(PSD_E_ARG, "cache strides must be multiples of 16 bytes");
     if (!pointers) return PSD_OK;
     if (!c->k || !c->v) return fail(PSD_E_ARG, "cache k / v is NULL");
     if (!aligned16(c->k) || !aligned16(c->v)) return fail(PSD_E_ARG, "cache k / v must be 16-byte aligned");
+    return PSD_OK;
+}
+
+psd_status check_cache(const psd_cache* c, bool pointers) {
+    const psd_status st = check_pages(c);
+    return st != PSD_OK ? st : check_pools(c, c->dtype == PSD_BF16 ? 2 : 4, pointers);
+}
+
+psd_status check_cache4(const psd_cache4* c, bool pointers) {
+    psd_status st = check_pages(c);
+    if (st != PSD_OK || (st = check_pools(c, 1, pointers)) != PSD_OK) return st;
+    const int64_t most = (int64_t)1 << 44;
+    for (const int64_t x : {c->scale_page, c->scale_token, c->scale_head, c->layers > 1 ? c->scale_layer : 0})
+        if (x < 0 || x >= most) return fail(PSD_E_ARG, "scale strides must be in [0, 2^44)");
+    if (pointers && (!c->k_scale || !c->v_scale)) return fail(PSD_E_ARG, "cache k_scale / v_scale is NULL");
     return PSD_OK;
 }
 
@@ -416,9 +438,9 @@ psd_status check_rows(const psd_rows* r, int bytes, const char* what) {
     return PSD_OK;
 }
 
-psd_status check_heads(const psd_cache* c, int q_heads) {
-    if (q_heads < 1 || q_heads > PSD_MAX_HEADS || q_heads % c->heads)
-        return fail(PSD_E_ARG, "q_heads %d is not a multiple of the cache's %d heads in [1, %d]", q_heads, c->heads, PSD_MAX_HEADS);
+psd_status check_heads(int heads, int q_heads) {
+    if (q_heads < 1 || q_heads > PSD_MAX_HEADS || q_heads % heads)
+        return fail(PSD_E_ARG, "q_heads %d is not a multiple of the cache's %d heads in [1, %d]", q_heads, heads, PSD_MAX_HEADS);
     return PSD_OK;
 }
 
@@ -427,7 +449,8 @@ bool overlap(const int32_t* a, int64_t n, const int32_t* b, int64_t m) {
     return (uintptr_t)a < (uintptr_t)b + 4 * (uintptr_t)m && (uintptr_t)b < (uintptr_t)a + 4 * (uintptr_t)n;
 }
 
-psd::CacheArgs cache_args(const psd_cache* c, const psd_seqs* s) {
+template <class Cache>
+psd::CacheArgs cache_args(const Cache* c, const psd_seqs* s) {
     psd::CacheArgs a;
     a.k = c->k;
     a.v = c->v;
@@ -453,6 +476,103 @@ psd::CacheArgs cache_args(const psd_cache* c, const psd_seqs* s) {
 }
 
 psd::RowsArgs rows_args(const psd_rows* r) { return psd::RowsArgs{r->data, r->stride_row, r->stride_head}; }
+
+psd::ScaleArgs scale_args(const psd_cache4* c) {
+    return psd::ScaleArgs{c->k_scale, c->v_scale, c->layers > 1 ? c->scale_layer : 0, c->scale_page, c->scale_token, c->scale_head};
+}
+
+int groups4(const psd_cache4* c) { return (c->head_dim + 31) / 32; }
+
+// What psd_kv_append and psd_kv_append4 check and take alike.
+psd_status append_args(const psd_rotation* rotation, const psd_rows* k, const psd_rows* v, const psd_rows* q, const psd_rows* q_out,
+                       int32_t q_heads, int heads, int head_dim, int bytes, psd::AppendArgs& a) {
+    psd_status st;
+    if (!rotation) return fail(PSD_E_ARG, "rotation is NULL");
+    if (rotation->rotary < 0 || rotation->rotary > head_dim || rotation->rotary % 2)
+        return fail(PSD_E_ARG, "rotary %d is not even in [0, %d]", rotation->rotary, head_dim);
+    if (rotation->rotary > 0 && (!rotation->cos || !rotation->sin || rotation->positions_max < 1))
+        return fail(PSD_E_ARG, "rotary > 0 needs cos, sin and positions_max >= 1");
+    if (!(rotation->eps >= 0.f) || !isfinite(rotation->eps)) return fail(PSD_E_ARG, "eps must be finite and >= 0");
+    if (!aligned16(rotation->q_norm) || !aligned16(rotation->k_norm))
+        return fail(PSD_E_ARG, "q_norm / k_norm must be 16-byte aligned");
+    if ((st = check_rows(k, bytes, "k")) != PSD_OK || (st = check_rows(v, bytes, "v")) != PSD_OK) return st;
+    if (!q != !q_out) return fail(PSD_E_ARG, "q and q_out come together");
+    if (q) {
+        if ((st = check_rows(q, bytes, "q")) != PSD_OK || (st = check_rows(q_out, bytes, "q_out")) != PSD_OK) return st;
+        if ((st = check_heads(heads, q_heads)) != PSD_OK) return st;
+    }
+    a.k = rows_args(k);
+    a.v = rows_args(v);
+    if (q) {
+        a.q = rows_args(q);
+        a.q_out = rows_args(q_out);
+        a.H = q_heads;
+    }
+    a.R = rotation->rotary;
+    a.interleaved = rotation->interleaved != 0;
+    a.positions_max = rotation->positions_max;
+    a.cos = rotation->cos;
+    a.sin = rotation->sin;
+    a.positions = rotation->positions;
+    a.q_norm = rotation->q_norm;
+    a.k_norm = rotation->k_norm;
+    a.eps = rotation->eps;
+    return PSD_OK;
+}
+
+// What psd_attention and psd_attention4 check and take alike; `need`: bytes of workspace, `fits`: inside a launch's limits.
+psd_status attention_args(const psd_seqs* seqs, const psd_rows* q, int32_t q_heads, float scale, int32_t window,
+                          const uint32_t* mask, int32_t mask_words, const psd_rows* out, float* lse, void* workspace,
+                          size_t workspace_bytes, int heads, int bytes, bool (*fits)(const psd::CacheArgs&, int, bool),
+                          size_t (*size)(const psd::CacheArgs&, int, bool), psd::AttentionArgs& a) {
+    psd_status st;
+    const bool bf16 = bytes == 2;
+    if ((st = check_heads(heads, q_heads)) != PSD_OK) return st;
+    if ((st = check_rows(q, bytes, "q")) != PSD_OK || (st = check_rows(out, bytes, "out")) != PSD_OK) return st;
+    if (!isfinite(scale)) return fail(PSD_E_ARG, "scale must be finite");
+    if (window < 0) return fail(PSD_E_ARG, "window must be at least 0");
+    if (mask && mask_words < 1) return fail(PSD_E_ARG, "mask_words must be at least 1");
+    if (mask && window > 0) return fail(PSD_E_ARG, "a mask takes no window");
+    if (!fits(a.c, q_heads, bf16) || (long)seqs->rows * q_heads / 4 >= kMaxGrid)
+        return fail(PSD_E_ARG, "call too large: batch %d, rows %d, max_new %d", seqs->batch, seqs->rows, seqs->max_new);
+    const size_t need = size(a.c, q_heads, bf16);
+    if (need > 0 && !workspace) return fail(PSD_E_WORKSPACE, "workspace is NULL");
+    if (workspace) {
+        if (((uintptr_t)workspace & 255u) != 0) return fail(PSD_E_WORKSPACE, "workspace must be 256-byte aligned");
+        if (workspace_bytes < need) return fail(PSD_E_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
+    }
+    a.q = rows_args(q);
+    a.out = rows_args(out);
+    a.H = q_heads;
+    a.scale = scale;
+    a.window = std::min<int32_t>(window, PSD_MAX_KV);  // wider ones see no more
+    a.mask = mask;
+    a.mask_words = mask ? mask_words : 0;
+    a.lse = lse;
+    a.workspace = workspace;
+    a.workspace_bytes = workspace ? workspace_bytes : 0;
+    return PSD_OK;
+}
+
+// What psd_kv_keep and psd_kv_keep4 check and take alike; `columns` of 16 bytes that one token has in a layer.
+psd_status keep_args(const psd_seqs* seqs, const int32_t* keep, int64_t keep_stride, int32_t keep_width, const int32_t* n_keep,
+                     int32_t* kv_out, long columns, psd::KeepArgs& a) {
+    if (!keep || !n_keep) return fail(PSD_E_ARG, "keep / n_keep is NULL");
+    if (keep_width < 1 || keep_stride < keep_width) return fail(PSD_E_ARG, "keep_width must be in [1, keep_stride]");
+    // its first workgroup writes kv_out while the others still read these
+    const int64_t B = seqs->batch;
+    if (kv_out && (overlap(kv_out, B, seqs->kv_len, B) || overlap(kv_out, B, seqs->new_start, B + 1) ||
+                   overlap(kv_out, B, n_keep, B) || overlap(kv_out, B, keep, (B - 1) * keep_stride + keep_width)))
+        return fail(PSD_E_ARG, "kv_out must not share memory with kv_len, new_start, n_keep or keep");
+    const long blocks = (columns + 255) / 256 * seqs->batch;
+    if (blocks > kMaxGrid) return fail(PSD_E_ARG, "call too large (%ld workgroups)", blocks);
+    a.keep = keep;
+    a.keep_stride = keep_stride;
+    a.keep_width = keep_width;
+    a.n_keep = n_keep;
+    a.kv_out = kv_out;
+    return PSD_OK;
+}
 
 }  // namespace
 
@@ -1144,47 +1264,39 @@ psd_status psd_kv_append(const psd_cache* cache, const psd_seqs* seqs, const psd
                          const psd_rows* v, const psd_rows* q, const psd_rows* q_out, int32_t q_heads, hipStream_t stream) {
     psd_status st;
     if ((st = check_cache(cache, true)) != PSD_OK || (st = check_seqs(seqs, true)) != PSD_OK) return st;
-    const int bytes = cache->dtype == PSD_BF16 ? 2 : 4;
-    if (!rotation) return fail(PSD_E_ARG, "rotation is NULL");
-    if (rotation->rotary < 0 || rotation->rotary > cache->head_dim || rotation->rotary % 2)
-        return fail(PSD_E_ARG, "rotary %d is not even in [0, %d]", rotation->rotary, cache->head_dim);
-    if (rotation->rotary > 0 && (!rotation->cos || !rotation->sin || rotation->positions_max < 1))
-        return fail(PSD_E_ARG, "rotary > 0 needs cos, sin and positions_max >= 1");
-    if (!(rotation->eps >= 0.f) || !isfinite(rotation->eps)) return fail(PSD_E_ARG, "eps must be finite and >= 0");
-    if (!aligned16(rotation->q_norm) || !aligned16(rotation->k_norm))
-        return fail(PSD_E_ARG, "q_norm / k_norm must be 16-byte aligned");
-    if ((st = check_rows(k, bytes, "k")) != PSD_OK || (st = check_rows(v, bytes, "v")) != PSD_OK) return st;
-    if (!q != !q_out) return fail(PSD_E_ARG, "q and q_out come together");
-    if (q) {
-        if ((st = check_rows(q, bytes, "q")) != PSD_OK || (st = check_rows(q_out, bytes, "q_out")) != PSD_OK) return st;
-        if ((st = check_heads(cache, q_heads)) != PSD_OK) return st;
-    }
     psd::AppendArgs a;
     memset(&a, 0, sizeof a);
     a.c = cache_args(cache, seqs);
-    a.k = rows_args(k);
-    a.v = rows_args(v);
-    if (q) {
-        a.q = rows_args(q);
-        a.q_out = rows_args(q_out);
-        a.H = q_heads;
-    }
-    a.R = rotation->rotary;
-    a.interleaved = rotation->interleaved != 0;
-    a.positions_max = rotation->positions_max;
-    a.cos = rotation->cos;
-    a.sin = rotation->sin;
-    a.positions = rotation->positions;
-    a.q_norm = rotation->q_norm;
-    a.k_norm = rotation->k_norm;
-    a.eps = rotation->eps;
+    st = append_args(rotation, k, v, q, q_out, q_heads, cache->heads, cache->head_dim, cache->dtype == PSD_BF16 ? 2 : 4, a);
+    if (st != PSD_OK) return st;
     const hipError_t e = psd::launch_kv_append(a, cache->dtype == PSD_BF16, stream);
     if (e != hipSuccess) return hip_fail(e, "append kernel launch");
     return PSD_OK;
 }
 
+psd_status psd_kv_append4(const psd_cache4* cache, const psd_seqs* seqs, const psd_rotation* rotation, const psd_rows* k,
+                          const psd_rows* v, const psd_rows* q, const psd_rows* q_out, int32_t q_heads, const psd_rows* k_held,
+                          const psd_rows* v_held, hipStream_t stream) {
+    psd_status st;
+    if ((st = check_cache4(cache, true)) != PSD_OK || (st = check_seqs(seqs, true)) != PSD_OK) return st;
+    const int bytes = cache->dtype == PSD_BF16 ? 2 : 4;
+    psd::Append4Args a;
+    memset(&a, 0, sizeof a);
+    a.a.c = cache_args(cache, seqs);
+    a.s = scale_args(cache);
+    if ((st = append_args(rotation, k, v, q, q_out, q_heads, cache->heads, cache->head_dim, bytes, a.a)) != PSD_OK) return st;
+    if ((k_held && (st = check_rows(k_held, bytes, "k_held")) != PSD_OK) ||
+        (v_held && (st = check_rows(v_held, bytes, "v_held")) != PSD_OK))
+        return st;
+    if (k_held) a.k_held = rows_args(k_held);
+    if (v_held) a.v_held = rows_args(v_held);
+    const hipError_t e = psd::launch_kv_append4(a, cache->dtype == PSD_BF16, stream);
+    if (e != hipSuccess) return hip_fail(e, "append kernel launch");
+    return PSD_OK;
+}
+
 size_t psd_attention_workspace_bytes(const psd_cache* cache, const psd_seqs* seqs, int32_t q_heads) {
-    if (check_cache(cache, false) != PSD_OK || check_seqs(seqs, false) != PSD_OK || check_heads(cache, q_heads) != PSD_OK)
+    if (check_cache(cache, false) != PSD_OK || check_seqs(seqs, false) != PSD_OK || check_heads(cache->heads, q_heads) != PSD_OK)
         return (size_t)-1;
     return psd::attention_workspace(cache_args(cache, seqs), q_heads, cache->dtype == PSD_BF16);
 }
@@ -1195,34 +1307,37 @@ psd_status psd_attention(const psd_cache* cache, const psd_seqs* seqs, const psd
     psd_status st;
     if ((st = check_cache(cache, true)) != PSD_OK || (st = check_seqs(seqs, true)) != PSD_OK) return st;
     const bool bf16 = cache->dtype == PSD_BF16;
-    if ((st = check_heads(cache, q_heads)) != PSD_OK) return st;
-    if ((st = check_rows(q, bf16 ? 2 : 4, "q")) != PSD_OK || (st = check_rows(out, bf16 ? 2 : 4, "out")) != PSD_OK) return st;
-    if (!isfinite(scale)) return fail(PSD_E_ARG, "scale must be finite");
-    if (window < 0) return fail(PSD_E_ARG, "window must be at least 0");
-    if (mask && mask_words < 1) return fail(PSD_E_ARG, "mask_words must be at least 1");
-    if (mask && window > 0) return fail(PSD_E_ARG, "a mask takes no window");
     psd::AttentionArgs a;
     memset(&a, 0, sizeof a);
     a.c = cache_args(cache, seqs);
-    if (!psd::attention_fits(a.c, q_heads, bf16) || (long)seqs->rows * q_heads / 4 >= kMaxGrid)
-        return fail(PSD_E_ARG, "call too large: batch %d, rows %d, max_new %d", seqs->batch, seqs->rows, seqs->max_new);
-    const size_t need = psd::attention_workspace(a.c, q_heads, bf16);
-    if (need > 0 && !workspace) return fail(PSD_E_WORKSPACE, "workspace is NULL");
-    if (workspace) {
-        if (((uintptr_t)workspace & 255u) != 0) return fail(PSD_E_WORKSPACE, "workspace must be 256-byte aligned");
-        if (workspace_bytes < need) return fail(PSD_E_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
-    }
-    a.q = rows_args(q);
-    a.out = rows_args(out);
-    a.H = q_heads;
-    a.scale = scale;
-    a.window = std::min<int32_t>(window, PSD_MAX_KV);  // wider ones see no more
-    a.mask = mask;
-    a.mask_words = mask ? mask_words : 0;
-    a.lse = lse;
-    a.workspace = workspace;
-    a.workspace_bytes = workspace ? workspace_bytes : 0;
+    st = attention_args(seqs, q, q_heads, scale, window, mask, mask_words, out, lse, workspace, workspace_bytes, cache->heads,
+                        bf16 ? 2 : 4, psd::attention_fits, psd::attention_workspace, a);
+    if (st != PSD_OK) return st;
     const hipError_t e = psd::launch_attention(a, bf16, stream);
+    if (e != hipSuccess) return hip_fail(e, "attention kernel launch");
+    return PSD_OK;
+}
+
+size_t psd_attention4_workspace_bytes(const psd_cache4* cache, const psd_seqs* seqs, int32_t q_heads) {
+    if (check_cache4(cache, false) != PSD_OK || check_seqs(seqs, false) != PSD_OK || check_heads(cache->heads, q_heads) != PSD_OK)
+        return (size_t)-1;
+    return psd::attention4_workspace(cache_args(cache, seqs), q_heads, cache->dtype == PSD_BF16);
+}
+
+psd_status psd_attention4(const psd_cache4* cache, const psd_seqs* seqs, const psd_rows* q, int32_t q_heads, float scale,
+                          int32_t window, const uint32_t* mask, int32_t mask_words, const psd_rows* out, float* lse,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    psd_status st;
+    if ((st = check_cache4(cache, true)) != PSD_OK || (st = check_seqs(seqs, true)) != PSD_OK) return st;
+    const bool bf16 = cache->dtype == PSD_BF16;
+    psd::Attention4Args a;
+    memset(&a, 0, sizeof a);
+    a.a.c = cache_args(cache, seqs);
+    a.s = scale_args(cache);
+    st = attention_args(seqs, q, q_heads, scale, window, mask, mask_words, out, lse, workspace, workspace_bytes, cache->heads,
+                        bf16 ? 2 : 4, psd::attention4_fits, psd::attention4_workspace, a.a);
+    if (st != PSD_OK) return st;
+    const hipError_t e = psd::launch_attention4(a, bf16, stream);
     if (e != hipSuccess) return hip_fail(e, "attention kernel launch");
     return PSD_OK;
 }
@@ -1231,24 +1346,153 @@ psd_status psd_kv_keep(const psd_cache* cache, const psd_seqs* seqs, const int32
                        int32_t keep_width, const int32_t* n_keep, int32_t* kv_out, hipStream_t stream) {
     psd_status st;
     if ((st = check_cache(cache, true)) != PSD_OK || (st = check_seqs(seqs, true)) != PSD_OK) return st;
-    if (!keep || !n_keep) return fail(PSD_E_ARG, "keep / n_keep is NULL");
-    if (keep_width < 1 || keep_stride < keep_width) return fail(PSD_E_ARG, "keep_width must be in [1, keep_stride]");
-    // its first workgroup writes kv_out while the others still read these
-    const int64_t B = seqs->batch;
-    if (kv_out && (overlap(kv_out, B, seqs->kv_len, B) || overlap(kv_out, B, seqs->new_start, B + 1) ||
-                   overlap(kv_out, B, n_keep, B) || overlap(kv_out, B, keep, (B - 1) * keep_stride + keep_width)))
-        return fail(PSD_E_ARG, "kv_out must not share memory with kv_len, new_start, n_keep or keep");
-    const long blocks = (2L * cache->heads * cache->head_dim / 4 + 255) / 256 * seqs->batch;
-    if (blocks > kMaxGrid) return fail(PSD_E_ARG, "call too large (%ld workgroups)", blocks);
     psd::KeepArgs a;
     a.c = cache_args(cache, seqs);
-    a.keep = keep;
-    a.keep_stride = keep_stride;
-    a.keep_width = keep_width;
-    a.n_keep = n_keep;
-    a.kv_out = kv_out;
+    st = keep_args(seqs, keep, keep_stride, keep_width, n_keep, kv_out, 2L * cache->heads * cache->head_dim / 4, a);
+    if (st != PSD_OK) return st;
     const hipError_t e = psd::launch_kv_keep(a, cache->dtype == PSD_BF16, stream);
     if (e != hipSuccess) return hip_fail(e, "keep kernel launch");
+    return PSD_OK;
+}
+
+psd_status psd_kv_keep4(const psd_cache4* cache, const psd_seqs* seqs, const int32_t* keep, int64_t keep_stride,
+                        int32_t keep_width, const int32_t* n_keep, int32_t* kv_out, hipStream_t stream) {
+    psd_status st;
+    if ((st = check_cache4(cache, true)) != PSD_OK || (st = check_seqs(seqs, true)) != PSD_OK) return st;
+    psd::KeepArgs a;
+    a.c = cache_args(cache, seqs);
+    st = keep_args(seqs, keep, keep_stride, keep_width, n_keep, kv_out, 2L * cache->heads * groups4(cache), a);
+    if (st != PSD_OK) return st;
+    const hipError_t e = psd::launch_kv_keep4(a, scale_args(cache), stream);
+    if (e != hipSuccess) return hip_fail(e, "keep kernel launch");
+    return PSD_OK;
+}
+
+psd_status psd_kv_reserve(const psd_pages* pages, const psd_seqs* seqs, const psd_reservation* r, hipStream_t stream) {
+    psd_status st;
+    if (!pages) return fail(PSD_E_ARG, "pages is NULL");
+    if (pages->page_tokens < 1 || pages->page_tokens > 65536)
+        return fail(PSD_E_ARG, "page_tokens %d outside [1, 65536]", pages->page_tokens);
+    if (pages->pages < 1) return fail(PSD_E_ARG, "pages must be at least 1");
+    if (!pages->ring || !pages->state) return fail(PSD_E_ARG, "ring / state is NULL");
+    if ((st = check_seqs(seqs, false)) != PSD_OK) return st;
+    if (!r) return fail(PSD_E_ARG, "reservation is NULL");
+    if (!r->n_new || !r->kv_have || !r->held || !r->table || !r->new_start || !r->kv_len)
+        return fail(PSD_E_ARG, "n_new / kv_have / held / table / new_start / kv_len is NULL");
+    // every workgroup reads the first two while others write the rest
+    const int64_t B = seqs->batch, T = seqs->rows;
+    const struct {
+        const void* at;
+        int64_t words;
+        bool out;
+    } parts[] = {{r->n_new, B, false},
+                 {r->kv_have, B, false},
+                 {r->held, B, true},
+                 {r->table, (B - 1) * seqs->table_stride + seqs->table_width, true},
+                 {pages->ring, pages->pages, true},
+                 {pages->state, 4, true},
+                 {r->new_start, B + 1, true},
+                 {r->kv_len, B, true},
+                 {r->granted, B, true},
+                 {r->row_seq, T, true},
+                 {r->positions, T, true},
+                 {r->slots, 2 * T, true}};
+    const int n = sizeof parts / sizeof parts[0];
+    for (int i = 0; i < n; ++i)
+        for (int j = 0; j < i; ++j)
+            if (parts[i].at && parts[j].at && (parts[i].out || parts[j].out) &&
+                overlap((const int32_t*)parts[i].at, parts[i].words, (const int32_t*)parts[j].at, parts[j].words))
+                return fail(PSD_E_ARG, "what a reservation writes shares memory with what it reads or writes besides");
+    if (((uintptr_t)r->slots & 7u) != 0) return fail(PSD_E_ARG, "slots must be 8-byte aligned");
+    psd::ReserveArgs a;
+    a.P = pages->page_tokens;
+    a.pages = pages->pages;
+    a.page_shift = -1;
+    a.ring = pages->ring;
+    a.state = pages->state;
+    a.B = seqs->batch;
+    a.rows = seqs->rows;
+    a.max_new = seqs->max_new;
+    a.max_kv = seqs->max_kv;
+    a.table_width = seqs->table_width;
+    a.table_stride = seqs->table_stride;
+    a.n_new = r->n_new;
+    a.kv_have = r->kv_have;
+    a.held = r->held;
+    a.table = r->table;
+    a.new_start = r->new_start;
+    a.kv_len = r->kv_len;
+    a.granted = r->granted;
+    a.row_seq = r->row_seq;
+    a.positions = r->positions;
+    a.slots = r->slots;
+    const hipError_t e = psd::launch_kv_reserve(a, stream);
+    if (e != hipSuccess) return hip_fail(e, "reservation kernel launch");
+    return PSD_OK;
+}
+
+psd_status psd_adjust_logits(const psd_params* params, const psd_adjustments* adjust, int32_t batch, int32_t rows,
+                             int32_t depth0, const void* logits, void* out, hipStream_t stream) {
+    psd_status st = check_params(params);
+    if (st != PSD_OK) return st;
+    if (!adjust) return fail(PSD_E_ARG, "adjustments are NULL");
+    if (batch < 1 || batch > PSD_MAX_BATCH) return fail(PSD_E_ARG, "batch %d outside [1, %d]", batch, PSD_MAX_BATCH);
+    if (rows < 1 || rows > PSD_MAX_GAMMA + 1) return fail(PSD_E_ARG, "rows %d outside [1, %d]", rows, PSD_MAX_GAMMA + 1);
+    if (depth0 < 0 || depth0 > PSD_MAX_GAMMA) return fail(PSD_E_ARG, "depth0 %d outside [0, %d]", depth0, PSD_MAX_GAMMA);
+    if (!logits || !out) return fail(PSD_E_ARG, "logits / out is NULL");
+    const psd_adjustments& j = *adjust;
+    if (j.text) {
+        if (!j.length) return fail(PSD_E_ARG, "text comes with length");
+        if (j.text_max < 0 || j.text_max > PSD_MAX_TEXT) return fail(PSD_E_ARG, "text_max %d outside [0, %d]", j.text_max, PSD_MAX_TEXT);
+        if (j.text_stride < j.text_max) return fail(PSD_E_ARG, "text_stride is below text_max");
+    }
+    if (j.draft_tokens) {
+        if (j.gamma < 1 || j.gamma > PSD_MAX_GAMMA) return fail(PSD_E_ARG, "gamma %d outside [1, %d]", j.gamma, PSD_MAX_GAMMA);
+        if (depth0 + rows > j.gamma + 1)
+            return fail(PSD_E_ARG, "depth0 %d and %d rows pass the %d drafts of a path", depth0, rows, j.gamma);
+    }
+    if (j.bias_width < 0 || j.bias_width > PSD_MAX_BIAS)
+        return fail(PSD_E_ARG, "bias_width %d outside [0, %d]", j.bias_width, PSD_MAX_BIAS);
+    if (j.bias_width > 0 && (!j.bias_tokens || !j.bias)) return fail(PSD_E_ARG, "bias_tokens / bias is NULL");
+    if (j.allowed && (j.allowed_seq < 0 || j.allowed_row < 0 || j.allowed_seq > (int64_t)1 << 40 || j.allowed_row > (int64_t)1 << 40))
+        return fail(PSD_E_ARG, "allowed_seq / allowed_row outside [0, 2^40]");
+    const int bytes = params->dtype == PSD_BF16 ? 2 : 4;
+    if (((uintptr_t)logits | (uintptr_t)out) % bytes) return fail(PSD_E_ARG, "logits / out must be aligned to their elements");
+    const uintptr_t size = (uintptr_t)batch * params->num_drafts * rows * params->vocab * bytes;
+    if (logits != out && (uintptr_t)logits < (uintptr_t)out + size && (uintptr_t)out < (uintptr_t)logits + size)
+        return fail(PSD_E_ARG, "out is logits itself or shares no memory with it");
+    psd::AdjustArgs a;
+    memset(&a, 0, sizeof a);
+    a.logits = logits;
+    a.out = out;
+    a.B = batch;
+    a.K = params->num_drafts;
+    a.S = rows;
+    a.V = params->vocab;
+    a.depth0 = depth0;
+    if (j.text) {
+        a.text = j.text;
+        a.text_stride = j.text_stride;
+        a.text_max = j.text_max;
+        a.length = j.length;
+        a.from = j.from;
+    }
+    if (j.draft_tokens) {
+        a.drafts = j.draft_tokens;
+        a.gamma = j.gamma;
+    }
+    a.repetition = j.repetition;
+    a.presence = j.presence;
+    a.frequency = j.frequency;
+    a.bias_tokens = j.bias_tokens;
+    a.bias = j.bias;
+    a.bias_width = j.bias_width;
+    a.allowed = j.allowed;
+    a.allowed_seq = j.allowed_seq;
+    a.allowed_row = j.allowed_row;
+    if (!psd::adjust_fits(a)) return fail(PSD_E_ARG, "call too large: batch %d", batch);
+    const hipError_t e = psd::launch_adjust(a, params->dtype == PSD_BF16, stream);
+    if (e != hipSuccess) return hip_fail(e, "adjustment kernel launch");
     return PSD_OK;
 }
 

@@ -19,82 +19,12 @@
 // A lane then rescales its own column: maximum, sum and output of a row share its lanes.
 #include <hip/hip_runtime.h>
 
-#include "psd_serve.hpp"
-#include "psd_serve_device.hpp"
+#include "psd_attention_device.hpp"
+#include "psd_attention_tile.hpp"
 
 namespace psd {
 
 namespace {
-
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLn2 = 0.69314718055994530942f;
-constexpr float kNoScore = -__builtin_inff();
-// A running maximum is raised only when a score passes it by this much: weights stay below
-// 2^8, sums exact to float32 as before, and most blocks need no exchange between lanes.
-constexpr float kSlack = 8.f;
-constexpr float kHuge = 3e38f;
-// Scores above this (units of ln 2) are taken from the maximum before they are scaled, see tile_kernel.
-constexpr float kFar = 1 << 20;
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ Range tile_range(const AttentionArgs& a, const Seq& s, int i_lo, int i_hi) {
-    return tile_range(a.mask != nullptr, a.window, s, i_lo, i_hi);
-}
-
-// Bit t of the result: the row of new token i sees position j0 + t (causal, window or mask; the end
-// of the cache and its pages aside).
-__device__ __forceinline__ uint32_t row_bits(const AttentionArgs& a, const Seq& s, int i, int row, int j0) {
-    if (a.mask) {
-        const int n0 = j0 - s.first;
-        if (n0 <= -32) return ~0u;
-        const uint32_t* words = a.mask + (int64_t)row * a.mask_words;
-        auto word = [&](int w) { return w < a.mask_words ? words[w] : 0u; };
-        if (n0 < 0) return (word(0) << -n0) | ((1u << -n0) - 1u);
-        const int w = n0 / 32, shift = n0 % 32;
-        return (uint32_t)(((uint64_t)word(w + 1) << 32 | word(w)) >> shift);
-    }
-    const int seen = s.first + i - j0 + 1;  // positions of the block up to the row's own
-    uint32_t bits = seen >= 32 ? ~0u : seen <= 0 ? 0u : (1u << seen) - 1u;
-    if (a.window > 0) {
-        const int gone = seen - a.window;
-        if (gone > 0) bits = gone >= 32 ? 0u : bits & (~0u << gone);
-    }
-    return bits;
-}
-
-// Infinite or NaN: the upper (float32: the) element of a word, and the lower one of two bfloat16.
-__device__ __forceinline__ bool odd_hi(uint32_t w) { return (w & 0x7F800000u) == 0x7F800000u; }
-template <bool BF16>
-__device__ __forceinline__ bool odd_lo(uint32_t w) {
-    return BF16 && (w & 0x7F80u) == 0x7F80u;
-}
-
-__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// Sums of weights with maxima m and m2 as one with maximum `top` of both.  Maxima pass over NaN, sums do
-// not: a row that sees nothing but NaN scores has no maximum and a NaN sum, one that sees nothing sum 0.
-__device__ __forceinline__ float add_sums(float l, float m, float l2, float m2, float top) {
-    return top == kNoScore ? l + l2 : l * exp2_hw(m - top) + l2 * exp2_hw(m2 - top);
-}
-
-// acc += A B of 16 x 16 results: 16 bytes of A's row and of B's column from each lane (32 products
-// a result in bfloat16, 16 in float32, where element e of all lanes makes one instruction).
-template <bool BF16>
-__device__ __forceinline__ f32x4 multiply(const u32x4 x, const u32x4 y, f32x4 acc) {
-    if constexpr (BF16) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x[e]), __uint_as_float(y[e]), acc, 0, 0, 0);
-        return acc;
-    }
-}
 
 // A block's softmax weights of this lane's row as a B operand.  In bfloat16 they are rounded to it, since the
 // matrix instructions take both operands in one type, and a second product of what the rounding left out would
@@ -175,29 +105,6 @@ constexpr int stream_lds() {
     return values > join ? values : join;
 }
 
-// Values that are the same in all lanes, into scalar registers.
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ Seq uniform(const Seq& s) {
-    return Seq{uniform(s.row0), uniform(s.n), uniform(s.first), uniform(s.kv), uniform(s.total)};
-}
-
-// A value anew, so that what rare code computes from it is not kept in registers through the common.
-__device__ __forceinline__ int again(int x) {
-    asm volatile("" : "+v"(x));
-    return x;
-}
-
-// What workgroups leave for each other: written through and read past the caches that are not
-// shared (relaxed accesses of agent scope), so that no fence has to empty those.
-__device__ __forceinline__ void leave2(float* at, float x, float y) {
-    const uint64_t w = (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x);
-    __hip_atomic_store((uint64_t*)at, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 fetch2(const float* at) {
-    const uint64_t w = __hip_atomic_load((const uint64_t*)at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
-}
-
 template <bool BF16, int DP, int RB, bool FULL>
 __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(AttentionArgs a, Plan p) {
     using S = StreamShape<BF16, DP>;
@@ -207,79 +114,31 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
     constexpr int ROWS = 16 * RB;
     __shared__ __align__(16) char s_mem[stream_lds<BF16, DP, RB>()];
     __shared__ int64_t s_off[NW][2][S::TOK];
-    __shared__ float s_m[NW][ROWS], s_l[NW][ROWS], s_top[ROWS], s_sum[ROWS];
-    __shared__ int s_units[NT + 1], s_wave[NW], s_longest[NW];
-    __shared__ Seq s_seq[NT];  // of the items, while there are no more than threads
-    __shared__ int s_chunk, s_last;
+    __shared__ StreamShared<NT, ROWS> sh;
 
     const CacheArgs& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int r = lane & 15, q = lane >> 4;
     const int g = blockIdx.x % c.G, wg = blockIdx.x / c.G;
 
-    // units before each thread's items, by a scan over the workgroup
-    const int items = c.B * p.tiles;
-    const int each = (items + NT - 1) / NT;
-    auto seq_at = [&](int i) { return load_seq(c, i / p.tiles); };
-    auto units_at = [&](int i, const Seq& s) { return item_units(a.mask != nullptr, a.window, p, s, i % p.tiles); };
-    int mine = 0, longest = 0;
-    for (int i = tid * each; i < min((tid + 1) * each, items); ++i) {
-        const Seq s = seq_at(i);
-        const int n = units_at(i, s);
-        s_seq[tid] = s;
-        mine += n;
-        longest = max(longest, n);
-    }
-    int upto = mine;
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) {
-        const int below = __shfl_up(upto, k);
-        if (lane >= k) upto += below;
-        longest = max(longest, __shfl_xor(longest, k));
-    }
-    if (lane == 63) {
-        s_wave[wave] = upto;
-        s_longest[wave] = longest;
-    }
-    __syncthreads();
-    for (int w = 0; w < NW; ++w) {
-        if (w < wave) upto += s_wave[w];
-        longest = max(longest, s_longest[w]);
-    }
-    s_units[tid + 1] = upto;
-    if (tid == 0) s_units[0] = 0;
-    __syncthreads();
-    const int units = uniform(s_units[NT]);
-    // While no item is much longer than a stretch, each workgroup takes one item whole and none is joined.
-    constexpr int kMinUnits = join_units(BF16);
-    const Division cut = divide(units, p.wgs, kMinUnits);
-    const bool whole_items = each == 1 && items <= p.wgs && uniform(longest) <= units / p.wgs + 1 + kMinUnits;
-    auto start = [&](int w) { return whole_items ? s_units[min(w, items)] : cut.start(w); };
-    if (wg >= (whole_items ? items : cut.wgs)) return;
-    const int u0 = uniform(start(wg)), u1 = uniform(start(wg + 1));  // this workgroup's
-    if (u0 == u1) return;
-    if (s_units[tid] <= u0 && u0 < s_units[tid + 1]) s_chunk = tid;
-    __syncthreads();
-    const int chunk = uniform(s_chunk);
-    int item = chunk * each, before = uniform(s_units[chunk]);
-    constexpr int kSlot = ROWS * DP + 2 * ROWS;  // floats of what a workgroup leaves of an item
-    auto slot_of = [&](int w, int second) {
-        return (float*)a.workspace + kCounterFloats + (((int64_t)w * c.G + g) * 2 + second) * kSlot;
-    };
+    const Stretch st = find_stretch(a, p, sh, wg, join_units(BF16));
+    if (st.u0 == st.u1) return;
     const float sc = a.scale * kLog2e;
     const int64_t head_at = (int64_t)g * c.stride_head;
     char* s_v = s_mem + wave * S::V_BYTES;
 
-    for (int n_units; before < u1; before += n_units, ++item) {
-        const Seq s = uniform(each == 1 ? s_seq[item] : seq_at(item));
-        n_units = each == 1 ? uniform(s_units[item + 1]) - before : uniform(units_at(item, s));
-        if (!works_on(before, n_units, u0)) continue;
+    int item = st.item, before = st.before;
+    for (int n_units; before < st.u1; before += n_units, ++item) {
+        const Seq s = uniform(st.each == 1 ? sh.seq[item] : load_seq(c, item / p.tiles));
+        n_units = st.each == 1 ? uniform(sh.units[item + 1]) - before
+                               : uniform(item_units(a.mask != nullptr, a.window, p, s, item % p.tiles));
+        if (!works_on(before, n_units, st.u0)) continue;
         const int b = item / p.tiles, tile = item - b * p.tiles;
         const Tile its = item_tile(p, s, tile);
         const int row0 = its.row0, rows = its.rows;
         const int i_lo = uniform(its.i_lo), i_hi = uniform(its.i_hi);
         const Range range = tile_range(a, s, i_lo, i_hi);
-        const int from = max(u0, before), to = min(u1, before + n_units);
+        const int from = max(st.u0, before), to = min(st.u1, before + n_units);
         const int c0 = range.lo + (from - before) * kUnit, c1 = min(range.lo + (to - before) * kUnit, range.hi);
         const int blocks = (c1 - c0 + S::TOK - 1) / S::TOK;
         const int32_t* table = c.table + (int64_t)b * c.table_stride;
@@ -536,547 +395,7 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
             }
         }
 
-        // Join the waves: a common maximum, then the outputs through LDS, summed by all threads, each for NP
-        // pairs of neighbouring dimensions.
-        constexpr int NP = ROWS * DP / 2 / NT;
-        constexpr int OP = DP + 4;
-        const int el = again(lane), et = again(tid), er = el & 15, eq = el >> 4;
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            l[rb] += __shfl_xor(l[rb], 16);
-            l[rb] += __shfl_xor(l[rb], 32);
-            if (eq == 0) {
-                s_m[wave][rb * 16 + er] = m[rb];
-                s_l[wave][rb * 16 + er] = l[rb];
-            }
-        }
-        __syncthreads();
-        float* s_o = (float*)s_mem;
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            const int row = rb * 16 + er;
-            float top = kNoScore;
-            for (int w = 0; w < NW; ++w) top = fmaxf(top, s_m[w][row]);
-            const float by = m[rb] == kNoScore ? 0.f : exp2_hw(m[rb] - top);
-#pragma unroll
-            for (int db = 0; db < DB; ++db) *(f32x4*)(s_o + (wave * ROWS + row) * OP + db * 16 + 4 * eq) = o[rb][db] * by;
-            if (wave == 0 && eq == 0) {
-                float sum = 0.f;
-                for (int w = 0; w < NW; ++w) sum = add_sums(sum, top, s_l[w][row], s_m[w][row], top);
-                s_top[row] = top;
-                s_sum[row] = sum;
-            }
-        }
-        __syncthreads();
-        float2 y[NP];
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int e = (i * NT + et) * 2;
-            y[i] = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                const float2 x = *(const float2*)(s_o + (w * ROWS + e / DP) * OP + e % DP);
-                y[i].x += x.x;
-                y[i].y += x.y;
-            }
-        }
-        if (from != before || to != before + n_units) {
-            // A part of an item.  What a workgroup leaves of an item that its stretch begins with goes to
-            // its first slot, of one that begins later to its second.
-            const int w_first = cut.owner(before), n_parts = cut.owner(before + n_units - 1) - w_first + 1;
-            float* dst = slot_of(wg, from == u0 ? 0 : 1);
-#pragma unroll
-            for (int i = 0; i < NP; ++i) leave2(dst + (i * NT + et) * 2, y[i].x, y[i].y);
-            if (et < ROWS) leave2(dst + ROWS * DP + 2 * et, s_top[et], s_sum[et]);
-            // all of it is written when the counter goes up: the workgroup that counts last finds every part
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
-            if (et == 0) {
-                unsigned* counter = (unsigned*)a.workspace + w_first * c.G + g;
-                const unsigned was = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                s_last = was == (unsigned)(n_parts - 1);
-                if (s_last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
-            __syncthreads();
-            if (!s_last) continue;  // s_last is written again two barriers later at the earliest
-            // the parts' common maximum and sum of each row, then their outputs, kBatch parts at a time
-            constexpr int kSubs = NT / ROWS, kBatch = 2048 / ROWS;
-            float* s_red = (float*)s_mem;         // [kSubs][ROWS][2]
-            float* s_fac = s_red + 2 * NT;  // [kBatch][ROWS]: the parts' factors
-            const int first_slot = before == start(w_first) ? 0 : 1;
-            auto part_slot = [&](int k) { return slot_of(w_first + k, k == 0 ? first_slot : 0); };
-            const int row = et % ROWS;
-            float mm = kNoScore, ll = 0.f;
-            for (int k = et / ROWS; k < n_parts; k += kSubs) {
-                const float2 x = fetch2(part_slot(k) + ROWS * DP + 2 * row);
-                const float up = fmaxf(mm, x.x);
-                ll = add_sums(ll, mm, x.y, x.x, up);
-                mm = up;
-            }
-            s_red[2 * et] = mm;
-            s_red[2 * et + 1] = ll;
-            __syncthreads();
-            if (et < ROWS) {
-                for (int k = 1; k < kSubs; ++k) {
-                    const float xm = s_red[2 * (k * ROWS + et)], xl = s_red[2 * (k * ROWS + et) + 1];
-                    const float up = fmaxf(mm, xm);
-                    ll = add_sums(ll, mm, xl, xm, up);
-                    mm = up;
-                }
-                s_top[et] = mm;
-                s_sum[et] = ll;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < NP; ++i) y[i] = make_float2(0.f, 0.f);
-            for (int k0 = 0; k0 < n_parts; k0 += kBatch) {
-                const int nk = min(kBatch, n_parts - k0);
-                for (int i = et; i < nk * ROWS; i += NT) {
-                    const float pm = fetch2(part_slot(k0 + i / ROWS) + ROWS * DP + 2 * (i % ROWS)).x;
-                    s_fac[i] = pm == kNoScore ? 0.f : exp2_hw(pm - s_top[i % ROWS]);
-                }
-                __syncthreads();
-                // all of a part's loads set out before one is waited for, and the next part's before this one is added
-                float2 x[NP], x_next[NP];
-                auto fetch = [&](int k, float2 (&into)[NP]) {
-                    const float* src = part_slot(k0 + k) + 2 * et;
-#pragma unroll
-                    for (int i = 0; i < NP; ++i) into[i] = fetch2(src + 2 * i * NT);
-                };
-                fetch(0, x);
-                for (int k = 0; k < nk; ++k) {
-                    fetch(min(k + 1, nk - 1), x_next);
-#pragma unroll
-                    for (int i = 0; i < NP; ++i) {
-                        const float f = s_fac[k * ROWS + (i * NT + et) * 2 / DP];
-                        y[i].x += x[i].x * f;
-                        y[i].y += x[i].y * f;
-                        x[i] = x_next[i];
-                    }
-                }
-                __syncthreads();
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int e = (i * NT + et) * 2;
-            const int row = e / DP, d = e % DP;
-            if (row >= rows || d >= c.D) continue;
-            const int rr = row0 + row, ri = rr / p.h;
-            const int head = g * p.h + rr - ri * p.h;
-            const int64_t t = s.row0 + ri;
-            const bool none = s_top[row] == kNoScore && s_sum[row] == 0.f;
-            const float by = none ? 0.f : 1.f / s_sum[row];
-            const float y0 = none ? 0.f : y[i].x * by, y1 = none ? 0.f : y[i].y * by;
-            char* dst = (char*)a.out.data + (t * a.out.stride_row + (int64_t)head * a.out.stride_head + d) * E::kBytes;
-            if constexpr (BF16)
-                *(uint32_t*)dst = pack_bf16(y0, y1);
-            else
-                *(float2*)dst = make_float2(y0, y1);
-            if (d == 0 && a.lse) a.lse[t * a.H + head] = none ? kNoScore : (s_top[row] + log2f(s_sum[row])) * kLn2;
-        }
-        __syncthreads();
-    }
-}
-
-// ---------------------------------------------------------------- many rows
-
-// One workgroup: 32 NW rows of one (sequence, key/value head), 32 a wave, over one part of its cache.
-// Blocks of 64 tokens go through LDS, which all waves read: 32x32x16 products, 64 x 32
-// scores a wave in 32 registers, the outputs in D/2 more.  Two buffers, one barrier a block: while
-// block n is computed, block n + 1 is on its way into registers, and is stored behind the
-// arithmetic.  Two waves a SIMD, so one wave's exponentials overlap the other's products: one
-// workgroup of 8 waves a CU, which loads and stores half as much a row, or two of 4 for fewer rows.
-// 2048 new tokens behind 14336, H=32, G=8, D=128: 544 - 570 us, 904 - 948 TFLOP/s (a large library product
-// reaches 1370), the products busy 44 % of it; without its loads and stores of keys and values 440.  In LDS two
-// buffers of 20 KB of values and 17 of keys.  Other heads, the same tokens: D=64 368 - 418 us; D=80, 96 and 112, padded to
-// 128, 534 - 557; D=192, padded to 256, 1652; D=256 1625 - 1672 (one workgroup a CU, 24 registers spilled).  Window 4096,
-// D=128: 157.  One token of 64 sequences, up to 4096 cached, window 1000, 263 MB: 46.
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
-template <int DP, int NW>
-struct TileShape {
-    static constexpr int TOK = 64;
-    static constexpr int NT = 64 * NW;
-    static constexpr int ROWS = 32 * NW;
-    static constexpr int LPR = DP / 8;              // 16-byte pieces of a token
-    static constexpr int TPP = NT / LPR;      // tokens of one load of the workgroup
-    static constexpr int N = TOK / TPP;             // loads a block
-    // Row pitches (elements): 8 lanes reading 16 bytes of 8 consecutive keys, and the 4-token by
-    // 64-byte tiles of the transposing reads, fall on different banks.
-    static constexpr int KP = DP + 8, VP = DP + 32;
-    static constexpr int BYTES = TOK * (KP + VP) * 2;
-};
-
-template <int DP, int NW>
-__global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_kernel(AttentionArgs a, Plan p) {
-    using S = TileShape<DP, NW>;
-    constexpr int KK = DP / 16, DB = DP / 32;
-    __shared__ __align__(16) char s_mem[2 * S::BYTES];  // two buffers of keys and values
-    __shared__ int64_t s_off[4][S::TOK];                // written two blocks ahead, read in two
-    __shared__ uint64_t s_there[4];
-    __shared__ int s_odd[2];
-
-    const CacheArgs& c = a.c;
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-    const int r = lane & 31, hi = lane >> 5;
-    int x = blockIdx.x;
-    const int g = x % c.G;
-    x /= c.G;
-    const int tile = p.tiles - 1 - x % p.tiles;  // causal rows: the longest first
-    x /= p.tiles;
-    const int b = x % c.B, part = x / c.B;
-
-    const Seq s = uniform(load_seq(c, b));
-    const int row0 = tile * S::ROWS;
-    const int rows = min(s.n * p.h - row0, S::ROWS);
-    if (rows <= 0) return;
-    const int i_lo = uniform(row0 / p.h), i_hi = uniform((row0 + rows - 1) / p.h);
-    const Range range = tile_range(a, s, i_lo, i_hi);
-    const int n_parts = max((range.hi - range.lo + p.chunk - 1) / p.chunk, 1);
-    if (part >= n_parts) return;
-    const int c0 = range.lo + part * p.chunk, c1 = min(c0 + p.chunk, range.hi);
-    const int blocks = (c1 - c0 + S::TOK - 1) / S::TOK;
-    const int32_t* table = c.table + (int64_t)b * c.table_stride;
-
-    // this wave's rows: new tokens [w_lo, w_hi]; a wave without rows keeps company with zeros
-    const int mine = min(max(rows - wave * 32, 0), 32);
-    const int w_lo = uniform((row0 + min(wave * 32, rows - 1)) / p.h), w_hi = uniform((row0 + min(wave * 32 + 31, rows - 1)) / p.h);
-    const bool on = r < mine;
-    const int rr = row0 + wave * 32 + r;
-    const int row_i = on ? rr / p.h : w_lo;
-    const int head = g * p.h + (on ? rr - row_i * p.h : 0);
-    const int64_t t_row = s.row0 + row_i;
-    // scores in units of ln 2; a negative scale goes into the queries' signs, so that a maximum
-    // of products is a maximum of scores
-    const float sc = fmaxf(fabsf(a.scale) * kLog2e, 1.17549435e-38f);
-    const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
-    u32x4 qf[KK];
-    {
-        const char* src = (const char*)a.q.data + (t_row * a.q.stride_row + (int64_t)head * a.q.stride_head) * 2;
-        // unconditional loads; rows and dimensions that are not there count as zero
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) qf[kk] = *(const u32x4*)(src + min(kk * 16 + hi * 8, c.D - 8) * 2);
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-            const bool none = !on || kk * 16 + hi * 8 >= c.D;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) qf[kk][e] = none ? 0u : qf[kk][e] ^ sign;
-        }
-    }
-    f32x16 o[DB];
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[db][e] = 0.f;
-    float m = kNoScore, l = 0.f;  // m: of products, scaled at the end
-
-    const int64_t head_at = (int64_t)g * c.stride_head;
-    const int piece = tid % S::LPR, token = tid / S::LPR;
-    const int d_piece = min(piece * 8, c.D - 8);
-    const bool past = piece * 8 >= c.D;  // keys past the head's end count as zero
-    const char* k_src = (const char*)c.k + (head_at + d_piece) * 2;
-    const char* v_src = (const char*)c.v + (head_at + d_piece) * 2;
-
-    // Wave 0 finds the tokens' places; a page number is loaded a block before it is used.
-    auto page_of = [&](int blk) {
-        const int j = c0 + blk * S::TOK + lane;
-        const int at = j < c1 ? j : 0;
-        return table[p.page_shift >= 0 ? at >> p.page_shift : at / c.P];
-    };
-    auto place = [&](int blk, int page) -> int64_t {
-        const int j = c0 + blk * S::TOK + lane;
-        const int pi = p.page_shift >= 0 ? j >> p.page_shift : j / c.P;
-        if (j >= c1 || (unsigned)page >= (unsigned)c.pages) return -1;
-        return (int64_t)page * c.stride_page + (int64_t)(j - pi * c.P) * c.stride_token;
-    };
-    auto publish = [&](int blk, int page) {
-        const int64_t off = place(blk, page);
-        s_off[blk & 3][lane] = max(off, (int64_t)0);
-        const uint64_t bits = __ballot(off >= 0);
-        if (lane == 0) s_there[blk & 3] = bits;
-    };
-    auto there_of = [&](int blk) {
-        const uint64_t bits = s_there[blk & 3];
-        return (uint64_t)(uint32_t)uniform((int)(uint32_t)bits) | (uint64_t)(uint32_t)uniform((int)(bits >> 32)) << 32;
-    };
-    struct Stage {
-        u32x4 k[S::N], v[S::N];
-    };
-    auto load = [&](int blk, Stage& x) {
-#pragma unroll
-        for (int k = 0; k < S::N; ++k) {
-            const int64_t at = s_off[blk & 3][k * S::TPP + token] * 2;
-            x.k[k] = *(const u32x4*)(k_src + at);
-            x.v[k] = *(const u32x4*)(v_src + at);
-        }
-    };
-    // Does every row of new tokens [lo, hi] see the whole block?
-    auto whole = [&](int blk, int lo, int top) {
-        const int j0 = c0 + blk * S::TOK;
-        if (there_of(blk) != ~0ull) return false;
-        if (a.mask) return j0 + S::TOK <= s.first;
-        return j0 + S::TOK - 1 <= s.first + lo && (a.window == 0 || j0 > s.first + top - a.window);
-    };
-    auto key_at = [&](int blk) { return s_mem + (blk & 1) * S::BYTES; };
-    auto value_at = [&](int blk) { return s_mem + (blk & 1) * S::BYTES + S::TOK * S::KP * 2; };
-    // Into LDS.  Where rows differ in what they see, values of tokens that are not there are zeroed
-    // and infinite or NaN values taken out (a weight 0 times them is NaN for rows that do not see them).
-    auto store = [&](int blk, Stage& x) {
-        if (past)
-#pragma unroll
-            for (int k = 0; k < S::N; ++k) x.k[k] = u32x4{0, 0, 0, 0};
-        if (!whole(blk, i_lo, i_hi)) {
-            const uint64_t there = there_of(blk);
-            bool odd = false;
-#pragma unroll
-            for (int k = 0; k < S::N; ++k) {
-                const bool gone = !((there >> (k * S::TPP + token)) & 1u);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    uint32_t w = gone ? 0u : x.v[k][e];
-                    const bool lo_odd = odd_lo<true>(w), hi_odd = odd_hi(w);
-                    odd |= lo_odd || hi_odd;
-                    if (lo_odd) w &= 0xFFFF0000u;
-                    if (hi_odd) w &= 0xFFFFu;
-                    x.v[k][e] = w;
-                }
-            }
-            if (odd) s_odd[blk & 1] = blk + 1;
-        }
-        char* keys = key_at(blk);
-        char* values = value_at(blk);
-#pragma unroll
-        for (int k = 0; k < S::N; ++k) {
-            *(u32x4*)(keys + ((k * S::TPP + token) * S::KP + piece * 8) * 2) = x.k[k];
-            *(u32x4*)(values + ((k * S::TPP + token) * S::VP + piece * 8) * 2) = x.v[k];
-        }
-    };
-    // this lane's dimension of 32 db + .., tokens 16 ks + {4 hi .., 8 + 4 hi ..}, as an A operand
-    const int v_lane = ((4 * hi + (lane & 15) / 4) * S::VP + ((lane >> 4) & 1) * 16 + (lane & 3) * 4) * 2;
-    typedef __attribute__((address_space(3))) char lds_char;
-    auto value = [&](lds_char* mine, int db, int ks) -> bf16x8 {  // mine: the block's values + v_lane
-        lds_char* at = mine + (16 * ks * S::VP + db * 32) * 2;
-        union {
-            s16x4 half[2];
-            bf16x8 all;
-        } v;
-        v.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
-        v.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 8 * S::VP * 2));
-        return v.all;
-    };
-
-    // Blocks on their way into registers: one, or two where a workgroup of 8 waves has the registers (a block
-    // takes it about as long as memory takes to answer).
-    constexpr int AHEAD = NW == 8 ? 2 : 1;
-    if (tid < 2) s_odd[tid] = 0;
-    int pages[AHEAD + 2];
-#pragma unroll
-    for (int n = 0; n < AHEAD + 2; ++n) pages[n] = page_of(n);
-    if (wave == 0)
-#pragma unroll
-        for (int n = 0; n <= AHEAD; ++n) publish(n, pages[n]);
-    int page = pages[AHEAD + 1];
-    __syncthreads();
-    Stage first, second;
-    load(0, first);
-    if (blocks > 0) store(0, first);
-    if (AHEAD == 2) load(1, first);
-    // Block `blk`, which is in LDS, while `into` is loaded; then block blk + 1 goes from `from` into LDS.
-    auto step = [&](int blk, Stage& from_stage, Stage& into) {
-        __syncthreads();
-        const int j0 = c0 + blk * S::TOK;
-        const bool more = blk + 1 < blocks;
-        load(blk + AHEAD, into);  // (past the end: the pool's first tokens, which nothing uses)
-        const bool seen_by_all = whole(blk, w_lo, w_hi);
-        const uint64_t there = there_of(blk);
-        // nothing of the block lies before this wave's last row's end (or behind its window)
-        const bool idle = mine == 0 || (!a.mask && (j0 > s.first + w_hi ||
-                                                    (a.window > 0 && j0 + S::TOK - 1 <= s.first + w_lo - a.window)));
-        uint32_t bits[2] = {~0u, ~0u};
-        if (!idle) {
-            const char* keys = key_at(blk);
-            lds_char* values = (lds_char*)value_at(blk) + v_lane;
-            // Scores: four keys' pieces are read from LDS while the last four are multiplied.
-            f32x16 sv[2];
-            u32x4 kb[2][4];
-            constexpr int CH = KK / 4;  // groups of four pieces of 32 keys
-            auto read_keys = [&](int n, u32x4 (&into)[4]) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    into[i] = *(const u32x4*)(keys + ((32 * (n / CH) + r) * S::KP + (n % CH * 4 + i) * 16 + hi * 8) * 2);
-            };
-            read_keys(0, kb[0]);
-            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-            for (int n = 0; n < 2 * CH; ++n) {
-                if (n + 1 < 2 * CH) read_keys(n + 1, kb[(n + 1) & 1]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (n % CH == 0 && i == 0)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) sv[n / CH][e] = 0.f;
-                    sv[n / CH] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kb[n & 1][i]),
-                                                                        __builtin_bit_cast(bf16x8, qf[n % CH * 4 + i]), sv[n / CH], 0,
-                                                                        0, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);                         // one product,
-                    if (n + 1 < 2 * CH) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // one read
-                }
-            }
-            if (!seen_by_all) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    // this lane's tokens: 8 (e / 4) + 4 hi + e % 4
-                    bits[t] = ((uint32_t)(there >> (32 * t)) & row_bits(a, s, row_i, (int)t_row, j0 + 32 * t)) >> (4 * hi);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) sv[t][e] = bits[t] & (1u << (8 * (e / 4) + e % 4)) ? sv[t][e] : kNoScore;
-                }
-                if (a.mask) __builtin_amdgcn_s_waitcnt(0x0F70);  // no load of this branch is pending behind it
-            }
-            float top = sv[0][0];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) top = fmaxf(top, sv[t][e]);
-            float from = m * sc;
-            if (__any(top * sc > from + kSlack)) {
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float next = fmaxf(m, top);
-                const float by = next == kNoScore ? 1.f : exp2_hw((m - next) * sc);
-                m = next;
-                from = m * sc;
-                l *= by;
-#pragma unroll
-                for (int db = 0; db < DB; ++db) o[db] *= by;
-            }
-            // The exponent is fma(sv, sc, -from): a row's weights have the rounding of `from` in common, which the
-            // division by their sum takes out, but which is no rounding error any more where scores are so large
-            // that it reaches float32's range of exponents.  There the maximum is taken out before the scale.
-            const bool none = from == kNoScore;
-            from = none ? 0.f : from;
-            if (__any(fabsf(from) > kFar)) {
-                const float base = none ? 0.f : m;
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) sv[t][e] -= base;
-                from -= from;  // (a maximum that is infinite when scaled: NaN)
-            }
-            // Weights of 16 tokens at a time, and their product with the values, whose pieces are read 16 tokens ahead:
-            // exponentials and reads go between the products.
-            auto weights = [&](int ks) {
-                u32x4 w;
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float w0 = exp2_hw(__builtin_fmaf(sv[ks / 2][8 * (ks % 2) + e], sc, -from));
-                    const float w1 = exp2_hw(__builtin_fmaf(sv[ks / 2][8 * (ks % 2) + e + 1], sc, -from));
-                    l += w0;
-                    l += w1;
-                    w[e / 2] = pack_bf16(w0, w1);
-                }
-                return w;
-            };
-            bf16x8 vb[2][DB];
-            auto read_values = [&](int ks, bf16x8 (&into)[DB]) {
-#pragma unroll
-                for (int db = 0; db < DB; ++db) into[db] = value(values, db, ks);
-            };
-            read_values(0, vb[0]);
-            u32x4 w = weights(0);
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) {
-                u32x4 w_next = w;
-                if (ks < 3) {
-                    read_values(ks + 1, vb[(ks + 1) & 1]);
-                    w_next = weights(ks + 1);
-                }
-#pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[ks & 1][db], __builtin_bit_cast(bf16x8, w), o[db], 0, 0, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                }
-                w = w_next;
-            }
-        }
-        if (uniform(s_odd[blk & 1]) == blk + 1) {
-            // infinite or NaN values were taken out of this block: a product of the largest finite
-            // numbers puts infinity where a row sees one
-            u32x4 again[S::N];
-#pragma unroll
-            for (int k = 0; k < S::N; ++k) again[k] = *(const u32x4*)(v_src + s_off[blk & 3][k * S::TPP + token] * 2);
-            __syncthreads();
-            char* values = value_at(blk);
-#pragma unroll
-            for (int k = 0; k < S::N; ++k) {
-                const bool gone = !((there >> (k * S::TPP + token)) & 1u);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t v = again[k][e];
-                    again[k][e] = gone ? 0u : (odd_lo<true>(v) ? 0x7F7Fu : 0u) | (odd_hi(v) ? 0x7F7F0000u : 0u);
-                }
-                *(u32x4*)(values + ((k * S::TPP + token) * S::VP + piece * 8) * 2) = again[k];
-            }
-            __syncthreads();
-            if (!idle) {
-                lds_char* ones = (lds_char*)value_at(blk) + v_lane;
-                u32x4 w[4];
-#pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const int bit = 16 * (ks & 1) + 8 * (e / 4) + e % 4;
-                        w[ks][e / 2] = (bits[ks / 2] >> bit & 1u ? 0x7F7Fu : 0u) | (bits[ks / 2] >> (bit + 1) & 1u ? 0x7F7F0000u : 0u);
-                    }
-#pragma unroll
-                for (int db = 0; db < DB; ++db)
-#pragma unroll
-                    for (int ks = 0; ks < 4; ++ks)
-                        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(ones, db, ks), __builtin_bit_cast(bf16x8, w[ks]),
-                                                                        o[db], 0, 0, 0);
-            }
-        }
-        if (more) store(blk + 1, from_stage);
-        if (wave == 0) publish(blk + 1 + AHEAD, page);
-        page = page_of(blk + 2 + AHEAD);
-    };
-    for (int blk = 0; blk < blocks; blk += AHEAD) {
-        step(blk, first, AHEAD == 2 ? second : first);
-        if (AHEAD == 2 && blk + 1 < blocks) step(blk + 1, second, first);
-    }
-
-    l += __shfl_xor(l, 32);
-    m *= sc;
-    if (!on) return;
-    if (n_parts == 1) {
-        const bool none = m == kNoScore && l == 0.f;
-        const float by = 1.f / l;
-        char* dst = (char*)a.out.data + (t_row * a.out.stride_row + (int64_t)head * a.out.stride_head) * 2;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const int d = db * 32 + 2 * e + 4 * hi;
-                if (d >= c.D) continue;
-                uint2 y = make_uint2(0, 0);
-                if (!none)
-                    y = make_uint2(pack_bf16(o[db][e] * by, o[db][e + 1] * by), pack_bf16(o[db][e + 2] * by, o[db][e + 3] * by));
-                *(uint2*)(dst + d * 2) = y;
-            }
-        if (hi == 0 && a.lse) a.lse[t_row * a.H + head] = none ? kNoScore : (m + log2f(l)) * kLn2;
-    } else {
-        const int64_t at = ((int64_t)part * c.rows + t_row) * a.H + head;
-        float* dst = (float*)a.workspace + kCounterFloats + at * c.D;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const int d = db * 32 + 2 * e + 4 * hi;
-                if (d < c.D) *(f32x4*)(dst + d) = f32x4{o[db][e], o[db][e + 1], o[db][e + 2], o[db][e + 3]};
-            }
-        if (hi == 0) {
-            float2* ml = (float2*)((float*)a.workspace + kCounterFloats + (int64_t)p.parts * c.rows * a.H * c.D);
-            ml[at] = make_float2(m, l);
-        }
+        finish_item<BF16, DP, RB, NT>(a, p, sh, s_mem, st, Item{s, row0, rows, before, n_units, from, to}, wg, g, o, m, l);
     }
 }
 
@@ -1159,9 +478,9 @@ void launch_stream(const AttentionArgs& a, const Plan& p, dim3 grid, hipStream_t
 template <int DP>
 void launch_tiles(const AttentionArgs& a, const Plan& p, dim3 grid, hipStream_t stream) {
     if (p.tile_rows == 256)
-        hipLaunchKernelGGL((tile_kernel<DP, 8>), grid, dim3(512), 0, stream, a, p);
+        hipLaunchKernelGGL((tile_kernel<false, DP, 8>), grid, dim3(512), 0, stream, a, p);
     else
-        hipLaunchKernelGGL((tile_kernel<DP, 4>), grid, dim3(256), 0, stream, a, p);
+        hipLaunchKernelGGL((tile_kernel<false, DP, 4>), grid, dim3(256), 0, stream, a, p);
 }
 
 }  // namespace
@@ -1180,7 +499,7 @@ hipError_t launch_attention(const AttentionArgs& a, bool bf16, hipStream_t strea
         else if (c.D <= 128)
             launch_tiles<128>(a, p, grid, stream);
         else
-            hipLaunchKernelGGL((tile_kernel<256, 4>), grid, dim3(256), 0, stream, a, p);
+            hipLaunchKernelGGL((tile_kernel<false, 256, 4>), grid, dim3(256), 0, stream, a, p);
     } else if (bf16) {
         if (c.D <= 64)
             launch_stream<true, 64>(a, p, grid, stream);
@@ -1196,9 +515,12 @@ hipError_t launch_attention(const AttentionArgs& a, bool bf16, hipStream_t strea
         else
             launch_stream<false, 256>(a, p, grid, stream);
     }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.parts <= 1) return e;
-    const dim3 joins((unsigned)(((long)c.rows * a.H + kWaves - 1) / kWaves));
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || p.parts <= 1 ? e : launch_attention_join(a, p, stream);
+}
+
+hipError_t launch_attention_join(const AttentionArgs& a, const Plan& p, hipStream_t stream) {
+    const dim3 joins((unsigned)(((long)a.c.rows * a.H + kWaves - 1) / kWaves));
     hipLaunchKernelGGL(join_kernel, joins, dim3(kThreads), 0, stream, a, p);
     return hipGetLastError();
 }

@@ -81,6 +81,9 @@ constexpr int join_units(bool bf16) { return bf16 ? 4 : 1; }
 // the registers of two.
 constexpr int stream_waves(int DP, int RB) { return RB * DP >= 512 || DP == 256 ? 4 : 8; }
 
+// The same over a cache held in 4 bits, where the converted values and the wider blocks take more LDS and registers.
+constexpr int stream4_waves(int DP, int RB) { return RB * DP >= 256 ? 4 : 8; }
+
 struct Range {
     int lo, hi;  // cached positions that some row of a tile sees
 };
@@ -150,7 +153,7 @@ constexpr int kCus = 256;
 
 inline int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
-inline Plan make_plan(const CacheArgs& c, int H, bool bf16, int span) {
+inline Plan make_plan(const CacheArgs& c, int H, bool bf16, int span, bool q4 = false) {
     Plan p;
     p.h = H / c.G;
     const long most = (long)c.max_new * p.h;
@@ -174,7 +177,8 @@ inline Plan make_plan(const CacheArgs& c, int H, bool bf16, int span) {
         // float32 rows in tiles of 32 while tiles of 64 would leave CUs without one (12 heads of 80, 37 tokens
         // of 6 sequences: 40 us and 45; 1024 new of 4096 tokens of 16 heads, CUs full: 450 and 408)
         const bool few = !bf16 && c.D > 64 && (long)c.B * c.G * ((most + 63) / 64) < kCus;
-        const int limit = c.D > 128 || few ? 32 : 64;
+        // (4 bits: float32 queries as three terms leave registers for 32)
+        const int limit = c.D > 128 || few || (q4 && !bf16) ? 32 : 64;
         p.tile_rows = most <= 16 ? 16 : most <= 32 ? 32 : limit;
         p.tiles = (int)((most + p.tile_rows - 1) / p.tile_rows);
         p.wgs = std::max(kCus / c.G, 1);  // one a CU
@@ -219,11 +223,16 @@ inline size_t plan_bytes(const Plan& p, const CacheArgs& c, int H) {
 
 inline size_t attention_workspace(const CacheArgs& c, int H, bool bf16) { return plan_bytes(make_plan(c, H, bf16, c.max_kv), c, H); }
 
+inline size_t attention4_workspace(const CacheArgs& c, int H, bool bf16) {
+    return plan_bytes(make_plan(c, H, bf16, c.max_kv, true), c, H);
+}
+
 // The launch stays inside a grid's limits.
-inline bool attention_fits(const CacheArgs& c, int H, bool bf16) {
-    const Plan p = make_plan(c, H, bf16, c.max_kv);
+inline bool plan_fits(const Plan& p, const CacheArgs& c) {
     if (!p.many) return (long)c.B * p.tiles * (c.max_kv / kUnit + 2) < 1L << 30;  // units
     return (long)c.B * c.G * p.tiles * p.parts < 1L << 23;
 }
+inline bool attention_fits(const CacheArgs& c, int H, bool bf16) { return plan_fits(make_plan(c, H, bf16, c.max_kv), c); }
+inline bool attention4_fits(const CacheArgs& c, int H, bool bf16) { return plan_fits(make_plan(c, H, bf16, c.max_kv, true), c); }
 
 }  // namespace psd

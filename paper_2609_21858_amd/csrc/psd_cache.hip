@@ -10,6 +10,9 @@
 // loads: 4.4 us, float32 6.5.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
+#include "psd_quant4.hpp"
 #include "psd_serve.hpp"
 #include "psd_serve_device.hpp"
 
@@ -29,6 +32,9 @@ enum Turn {
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
+__host__ __device__ __forceinline__ const AppendArgs& rows_of(const AppendArgs& a) { return a; }
+__host__ __device__ __forceinline__ const AppendArgs& rows_of(const Append4Args& a) { return a.a; }
+
 // One piece of N heads at once.
 template <int N>
 struct Heads {
@@ -42,8 +48,13 @@ struct Heads {
 //   y_d = (x_d A_d + x_partner B_d) / sqrt(mean(x^2) + eps).
 // The row's data sets out before its place is known, which takes three dependent loads.  q_out may
 // be q: a wave has read a head, partners included, before it writes it.
-template <bool BF16, Turn TURN>
-__global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, int GS, int row_threads) {
+//
+// Q4: keys and values go into 4 bits (psd_quant4.hpp), a group of 32 dimensions from 4 or 8 lanes.  Keys
+// are computed in 64 bits, since an error of 2^-24 would put one code in a million on the other side of a border.
+template <bool BF16, Turn TURN, bool Q4>
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(std::conditional_t<Q4, Append4Args, AppendArgs> args, int GS,
+                                                                int row_threads) {
+    const AppendArgs& a = rows_of(args);
     using E = Elem<BF16>;
     constexpr int VEC = E::kVec;
     constexpr int NQ = 4, NK = 2;  // heads of a thread whose loads are in flight together: queries; keys, values
@@ -83,14 +94,16 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, in
     if (i < 0 || i >= s.n) return;
     const int pos = s.first + i;
 
-    // the place in the cache, if the token has one
-    int64_t at = -1;
+    // the place in the cache, if the token has one (elements; Q4: bytes)
+    int64_t at = -1, scale_at = 0;
     if (pos >= 0 && pos < c.max_kv) {
         const int pi = pos / c.P;
         if (pi < c.table_width) {
             const int page = c.table[(int64_t)b * c.table_stride + pi];
-            if ((unsigned)page < (unsigned)c.pages)
+            if ((unsigned)page < (unsigned)c.pages) {
                 at = (int64_t)page * c.stride_page + (int64_t)(pos - pi * c.P) * c.stride_token;
+                if constexpr (Q4) scale_at = (int64_t)page * args.s.page + (int64_t)(pos - pi * c.P) * args.s.token;
+            }
         }
     }
 
@@ -136,10 +149,11 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, in
     }
 
     const float inv_d = 1.f / (float)c.D;
-    // queries or keys: `pool` at `to` (no place: nothing is written)
-    auto turn = [&](auto& w, const RowsArgs& r, int heads, const void* norm, char* to, int64_t stride) {
+    // Queries or keys, in the arithmetic of `zero`'s type; each head's elements go to `emit`.
+    auto turn = [&](auto zero, auto& w, const RowsArgs& r, int heads, const void* norm, auto emit) {
+        using T = decltype(zero);
         constexpr int N = sizeof(w.own) / sizeof(w.own[0]);
-        float A[VEC], B[VEC];
+        T A[VEC], B[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
             A[j] = cs[j];
@@ -181,14 +195,17 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, in
                 const int h = h0 + k * groups + group;
                 float x[VEC], y[VEC];
                 E::widen(w.own[k], x);
-                float scale = 1.f;
+                T scale = 1;
                 if (norm) {
-                    float sum = 0.f;
+                    T sum = 0;
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) sum += x[j] * x[j];
-                    if (!in_head) sum = 0.f;
+                    for (int j = 0; j < VEC; ++j) sum += (T)x[j] * x[j];
+                    if (!in_head) sum = 0;
                     for (int o = GS / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-                    scale = rsqrtf(sum * inv_d + a.eps);
+                    if constexpr (sizeof(T) == 4)
+                        scale = rsqrtf(sum * inv_d + a.eps);
+                    else
+                        scale = 1 / sqrt(sum / c.D + a.eps);
                 }
                 if constexpr (TURN == kPieces) {
                     E::widen(w.other[k], y);
@@ -210,19 +227,64 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, in
                     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                     __builtin_amdgcn_wave_barrier();
                 }
+                T z[VEC];
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
-                    float v = x[j] * A[j];
+                    T v = x[j] * A[j];
                     if (TURN != kNoTurn && turns && (TURN == kPieces || d0 + j < a.R)) v += y[j] * B[j];
-                    x[j] = norm ? v * scale : v;
+                    z[j] = norm ? v * scale : v;
                 }
-                if (in_head && h < heads && to) *(u32x4*)(to + ((int64_t)h * stride + d0) * E::kBytes) = E::narrow(x);
+                emit(h, z);
             }
         }
     };
-    if (a.H > 0)
-        turn(wq, a.q, a.H, a.q_norm, (char*)a.q_out.data + (int64_t)t * a.q_out.stride_row * E::kBytes, a.q_out.stride_head);
-    turn(wk, a.k, c.G, a.k_norm, at >= 0 ? (char*)c.k + at * E::kBytes : nullptr, c.stride_head);
+    if (a.H > 0) {
+        char* to = (char*)a.q_out.data + (int64_t)t * a.q_out.stride_row * E::kBytes;
+        turn(0.f, wq, a.q, a.H, a.q_norm, [&](int h, const float (&z)[VEC]) {
+            if (in_head && h < a.H) *(u32x4*)(to + ((int64_t)h * a.q_out.stride_head + d0) * E::kBytes) = E::narrow(z);
+        });
+    }
+    if constexpr (Q4) {
+        // VEC elements of a head in 4 bits: a group's lanes agree on its scale, its first lane writes it
+        const int padded = (c.D + 31) / 32 * 32;
+        auto put = [&](auto (&z)[VEC], int h, void* codes, void* scales, const RowsArgs& held) {
+            if (!in_head)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) z[j] = 0;
+            int s = quant4::scale_of(z);
+#pragma unroll
+            for (int o = 1; o < 32 / VEC; o <<= 1) s = max(s, __shfl_xor(s, o));
+            const uint32_t w = quant4::encode(z, s);
+            if (h >= c.G) return;
+            if (at >= 0 && d0 < padded) {
+                char* to = (char*)codes + at + (int64_t)h * c.stride_head + d0 / 2;
+                if constexpr (VEC == 8)
+                    *(uint32_t*)to = w;
+                else
+                    *(uint16_t*)to = (uint16_t)w;
+                if (d0 % 32 == 0) ((uint8_t*)scales)[scale_at + (int64_t)h * args.s.head + d0 / 32] = (uint8_t)s;
+            }
+            if (held.data && in_head)
+                *(u32x4*)((char*)held.data + ((int64_t)t * held.stride_row + (int64_t)h * held.stride_head + d0) * E::kBytes) =
+                    quant4::decode<BF16>(w, s);
+        };
+        turn(0., wk, a.k, c.G, a.k_norm, [&](int h, double (&z)[VEC]) { put(z, h, c.k, args.s.k, args.k_held); });
+        for (int h0 = 0; h0 < c.G; h0 += NK * groups) {
+            if (h0 > 0) load(wv, a.v, c.G, h0 + group, false);
+#pragma unroll
+            for (int k = 0; k < NK; ++k) {
+                if (h0 + k * groups >= c.G) break;
+                float z[VEC];
+                E::widen(wv.own[k], z);
+                put(z, h0 + k * groups + group, c.v, args.s.v, args.v_held);
+            }
+        }
+        return;
+    }
+    turn(0.f, wk, a.k, c.G, a.k_norm, [&](int h, const float (&z)[VEC]) {
+        if (in_head && h < c.G && at >= 0)
+            *(u32x4*)((char*)c.k + (at + (int64_t)h * c.stride_head + d0) * E::kBytes) = E::narrow(z);
+    });
     if (at < 0) return;
     for (int h0 = 0; h0 < c.G; h0 += NK * groups) {
         if (h0 > 0) load(wv, a.v, c.G, h0 + group, false);
@@ -247,10 +309,14 @@ constexpr int kKeepPlaces = 64;
 // chain of dependent loads is lengths and indices, page table, data.  Indices ascend strictly,
 // so keep[i] >= i and the places still to be read lie behind those written so far: kKeepBatch
 // tokens are read together, then written.
-__global__ __launch_bounds__(kKeepThreads) void keep_kernel(KeepArgs a, int vec, int bytes) {
+//
+// Q4: a column is a group's 16 bytes of codes, and its scale byte.
+template <bool Q4>
+__global__ __launch_bounds__(kKeepThreads) void keep_kernel(KeepArgs a, ScaleArgs scales, int vec, int bytes) {
     __shared__ int64_t s_from[kKeepPlaces], s_to[kKeepPlaces];
+    __shared__ int64_t s_scale_from[Q4 ? kKeepPlaces : 1], s_scale_to[Q4 ? kKeepPlaces : 1];
     const CacheArgs& c = a.c;
-    const int pieces = c.D / vec;
+    const int pieces = (c.D + vec - 1) / vec;
     const int blocks = (2 * c.G * pieces + kKeepThreads - 1) / kKeepThreads;  // of one sequence and layer
     const int b = blockIdx.x / blocks, part = blockIdx.x - b * blocks;
     const int layer = blockIdx.y;
@@ -263,13 +329,14 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KeepArgs a, int vec,
     const int n = max(min(min(kept, a.keep_width), total), 0);
     if (layer == 0 && part == 0 && tid == 0 && a.kv_out) a.kv_out[b] = s.first + n;
     const int32_t* table = c.table + (int64_t)b * c.table_stride;
-    auto place = [&](int i) -> int64_t {
+    auto place = [&](int i, int64_t* scale) -> int64_t {
         const int pos = s.first + i;
         if (i < 0 || i >= total || pos < 0 || pos >= c.max_kv) return -1;
         const int pi = pos / c.P;
         if (pi >= c.table_width) return -1;
         const int page = table[pi];
         if ((unsigned)page >= (unsigned)c.pages) return -1;
+        if constexpr (Q4) *scale = (int64_t)page * scales.page + (int64_t)(pos - pi * c.P) * scales.token;
         return ((int64_t)page * c.stride_page + (int64_t)(pos - pi * c.P) * c.stride_token) * bytes;
     };
     const int col = part * kKeepThreads + tid;
@@ -277,7 +344,14 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KeepArgs a, int vec,
     const bool value = col >= c.G * pieces;
     const int rest = value ? col - c.G * pieces : col;
     const int g = rest / pieces, d0 = (rest - g * pieces) * vec;
-    char* pool = (char*)(value ? c.v : c.k) + ((int64_t)layer * c.stride_layer + (int64_t)g * c.stride_head + d0) * bytes;
+    char* pool = (char*)(value ? c.v : c.k);
+    uint8_t* scale_pool = nullptr;
+    if constexpr (Q4) {
+        pool += (int64_t)layer * c.stride_layer + (int64_t)g * c.stride_head + d0 / 2;
+        scale_pool = (uint8_t*)(value ? scales.v : scales.k) + (int64_t)layer * scales.layer + (int64_t)g * scales.head + d0 / 32;
+    } else {
+        pool += ((int64_t)layer * c.stride_layer + (int64_t)g * c.stride_head + d0) * bytes;
+    }
     for (int i0 = 0; i0 < n; i0 += kKeepPlaces) {
         if (i0 > 0) {
             __syncthreads();
@@ -285,64 +359,89 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KeepArgs a, int vec,
         }
         if (tid < kKeepPlaces) {
             const int i = i0 + tid;
-            const int64_t src = i < n && from != i ? place(from) : -1, dst = i < n ? place(i) : -1;
+            int64_t scale_src = 0, scale_dst = 0;
+            const int64_t src = i < n && from != i ? place(from, &scale_src) : -1, dst = i < n ? place(i, &scale_dst) : -1;
             s_from[tid] = src;
             s_to[tid] = src >= 0 ? dst : -1;
+            if constexpr (Q4) {
+                s_scale_from[tid] = scale_src;
+                s_scale_to[tid] = scale_dst;
+            }
         }
         __syncthreads();
         const int m = min(kKeepPlaces, n - i0);
         if (!on) continue;
         for (int j0 = 0; j0 < m; j0 += kKeepBatch) {
             u32x4 w[kKeepBatch];
+            uint8_t scale[kKeepBatch];
             int64_t to[kKeepBatch];
 #pragma unroll
             for (int j = 0; j < kKeepBatch; ++j) {
                 to[j] = j0 + j < m ? s_to[j0 + j] : -1;
                 if (to[j] >= 0) w[j] = *(const u32x4*)(pool + s_from[j0 + j]);
+                if (Q4 && to[j] >= 0) scale[j] = scale_pool[s_scale_from[j0 + j]];
             }
 #pragma unroll
-            for (int j = 0; j < kKeepBatch; ++j)
+            for (int j = 0; j < kKeepBatch; ++j) {
                 if (to[j] >= 0) *(u32x4*)(pool + to[j]) = w[j];
+                if (Q4 && to[j] >= 0) scale_pool[s_scale_to[j0 + j]] = scale[j];
+            }
         }
     }
 }
 
 constexpr int kWaveRows = 1024;
 
-template <bool BF16>
-void append(const AppendArgs& a, int gs, hipStream_t stream) {
+template <bool BF16, bool Q4, class Args>
+void append(const Args& args, hipStream_t stream) {
+    const AppendArgs& a = rows_of(args);
+    int gs = 1;
+    while (gs * (BF16 ? 8 : 4) < (Q4 ? (a.c.D + 31) / 32 * 32 : a.c.D)) gs *= 2;
     // A wave a row has the less to set up, a workgroup a row the shorter chain: from 1024 rows on (a wave
     // for each SIMD) the first is ahead (H=32, G=8, D=128, 1300 rows: 9.6 us and 10.8, 5400: 24.5 and 27.8).
     const int row_threads = a.c.rows >= kWaveRows ? 64 : kAppendThreads;
     const int per = kAppendThreads / row_threads;
     const dim3 grid((a.c.rows + per - 1) / per), block(kAppendThreads);
     if (a.R == 0)
-        hipLaunchKernelGGL((append_kernel<BF16, kNoTurn>), grid, block, 0, stream, a, gs, row_threads);
+        hipLaunchKernelGGL((append_kernel<BF16, kNoTurn, Q4>), grid, block, 0, stream, args, gs, row_threads);
     else if (a.interleaved)
-        hipLaunchKernelGGL((append_kernel<BF16, kInterleaved>), grid, block, 0, stream, a, gs, row_threads);
+        hipLaunchKernelGGL((append_kernel<BF16, kInterleaved, Q4>), grid, block, 0, stream, args, gs, row_threads);
     else if (a.R / 2 % Elem<BF16>::kVec == 0)
-        hipLaunchKernelGGL((append_kernel<BF16, kPieces>), grid, block, 0, stream, a, gs, row_threads);
+        hipLaunchKernelGGL((append_kernel<BF16, kPieces, Q4>), grid, block, 0, stream, args, gs, row_threads);
     else
-        hipLaunchKernelGGL((append_kernel<BF16, kAnywhere>), grid, block, 0, stream, a, gs, row_threads);
+        hipLaunchKernelGGL((append_kernel<BF16, kAnywhere, Q4>), grid, block, 0, stream, args, gs, row_threads);
 }
 
 }  // namespace
 
 hipError_t launch_kv_append(const AppendArgs& a, bool bf16, hipStream_t stream) {
-    int gs = 1;
-    while (gs * (bf16 ? 8 : 4) < a.c.D) gs *= 2;
     if (bf16)
-        append<true>(a, gs, stream);
+        append<true, false>(a, stream);
     else
-        append<false>(a, gs, stream);
+        append<false, false>(a, stream);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_append4(const Append4Args& a, bool bf16, hipStream_t stream) {
+    if (bf16)
+        append<true, true>(a, stream);
+    else
+        append<false, true>(a, stream);
     return hipGetLastError();
 }
 
 hipError_t launch_kv_keep(const KeepArgs& a, bool bf16, hipStream_t stream) {
     const int vec = bf16 ? 8 : 4;
     const int cols = 2 * a.c.G * (a.c.D / vec);
-    hipLaunchKernelGGL(keep_kernel, dim3((cols + kKeepThreads - 1) / kKeepThreads * a.c.B, a.c.layers), dim3(kKeepThreads), 0,
-                       stream, a, vec, bf16 ? 2 : 4);
+    hipLaunchKernelGGL((keep_kernel<false>), dim3((cols + kKeepThreads - 1) / kKeepThreads * a.c.B, a.c.layers), dim3(kKeepThreads),
+                       0, stream, a, ScaleArgs{}, vec, bf16 ? 2 : 4);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_keep4(const KeepArgs& a, const ScaleArgs& s, hipStream_t stream) {
+    const int cols = 2 * a.c.G * ((a.c.D + 31) / 32);
+    hipLaunchKernelGGL((keep_kernel<true>), dim3((cols + kKeepThreads - 1) / kKeepThreads * a.c.B, a.c.layers), dim3(kKeepThreads),
+                       0, stream, a, s, 32, 1);
     return hipGetLastError();
 }
 

@@ -73,6 +73,30 @@ class Cache(ctypes.Structure):
     ]
 
 
+class Cache4(ctypes.Structure):
+    """psd_cache4: keys and values in pages of 4-bit codes (make_cache4, new_cache4)."""
+    _fields_ = [
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("dtype", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("page_tokens", ctypes.c_int32),
+        ("pages", ctypes.c_int32),
+        ("layers", ctypes.c_int32),
+        ("stride_layer", ctypes.c_int64),
+        ("stride_page", ctypes.c_int64),
+        ("stride_token", ctypes.c_int64),
+        ("stride_head", ctypes.c_int64),
+        ("scale_layer", ctypes.c_int64),
+        ("scale_page", ctypes.c_int64),
+        ("scale_token", ctypes.c_int64),
+        ("scale_head", ctypes.c_int64),
+    ]
+
+
 class Seqs(ctypes.Structure):
     """psd_seqs: the sequences of one call (make_seqs)."""
     _fields_ = [
@@ -105,6 +129,39 @@ class Rotation(ctypes.Structure):
         ("q_norm", ctypes.c_void_p),
         ("k_norm", ctypes.c_void_p),
         ("eps", ctypes.c_float),
+    ]
+
+
+class Pages(ctypes.Structure):
+    """psd_pages: the free pages of a pool (make_pages, new_pages)."""
+    _fields_ = [("page_tokens", ctypes.c_int32), ("pages", ctypes.c_int32), ("ring", ctypes.c_void_p), ("state", ctypes.c_void_p)]
+
+
+class Reservation(ctypes.Structure):
+    """psd_reservation: what sequences ask psd_kv_reserve for, and what they got."""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("n_new", "kv_have", "held", "table", "new_start", "kv_len", "granted",
+                                                     "row_seq", "positions", "slots")]
+
+
+class Adjustments(ctypes.Structure):
+    """psd_adjustments: penalties, biases and masks of psd_adjust_logits."""
+    _fields_ = [
+        ("text", ctypes.c_void_p),
+        ("text_stride", ctypes.c_int64),
+        ("text_max", ctypes.c_int32),
+        ("length", ctypes.c_void_p),
+        ("from_", ctypes.c_void_p),
+        ("draft_tokens", ctypes.c_void_p),
+        ("gamma", ctypes.c_int32),
+        ("repetition", ctypes.c_void_p),
+        ("presence", ctypes.c_void_p),
+        ("frequency", ctypes.c_void_p),
+        ("bias_tokens", ctypes.c_void_p),
+        ("bias", ctypes.c_void_p),
+        ("bias_width", ctypes.c_int32),
+        ("allowed", ctypes.c_void_p),
+        ("allowed_seq", ctypes.c_int64),
+        ("allowed_row", ctypes.c_int64),
     ]
 
 
@@ -162,6 +219,12 @@ def _load():
         "psd_attention": ([vp, vp, vp, i32, ctypes.c_float, i32, vp, i32, vp, vp, vp, sz, vp], i32),
         "psd_attention_workspace_bytes": ([vp, vp, i32], sz),
         "psd_kv_keep": ([vp, vp, vp, ctypes.c_int64, i32, vp, vp, vp], i32),
+        "psd_kv_append4": ([vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp], i32),
+        "psd_attention4": ([vp, vp, vp, i32, ctypes.c_float, i32, vp, i32, vp, vp, vp, sz, vp], i32),
+        "psd_attention4_workspace_bytes": ([vp, vp, i32], sz),
+        "psd_kv_keep4": ([vp, vp, vp, ctypes.c_int64, i32, vp, vp, vp], i32),
+        "psd_kv_reserve": ([vp, vp, vp, vp], i32),
+        "psd_adjust_logits": ([P, vp, i32, i32, i32, vp, vp, vp], i32),
         "psd_verify_given": ([P, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp], i32),
         "psd_verify_given_workspace_bytes": ([P, i32, i32], sz),
     }
@@ -178,7 +241,9 @@ EXPORTS = ("psd_abi_version", "psd_last_error", "psd_workspace_bytes", "psd_work
            "psd_context_keys", "psd_clock_values", "psd_set_spin_limit", "psd_detect_scores",
            "psd_detect_scores_pvalue", "psd_detection_rate", "psd_advance", "psd_toy_logits",
            "psd_generate_workspace_bytes", "psd_generate", "psd_kv_append", "psd_attention",
-           "psd_attention_workspace_bytes", "psd_kv_keep", "psd_verify_given", "psd_verify_given_workspace_bytes")
+           "psd_attention_workspace_bytes", "psd_kv_keep", "psd_verify_given", "psd_verify_given_workspace_bytes",
+           "psd_kv_append4", "psd_attention4", "psd_attention4_workspace_bytes", "psd_kv_keep4", "psd_kv_reserve",
+           "psd_adjust_logits")
 
 
 def lib():
@@ -486,6 +551,49 @@ def make_cache(k, v) -> Cache:
     return c
 
 
+def make_cache4(k, v, k_scale, v_scale, head_dim: int, dtype=torch.bfloat16) -> Cache4:
+    """Pools of 4-bit codes uint8 [pages][page tokens][heads][16 groups] (or [layers][pages]...) and their scale bytes
+    uint8 [...][groups], groups = ceil(head_dim / 32), of any strides with a contiguous last dimension; dtype: of new keys and
+    values, queries and outputs.  Keeps the tensors alive."""
+    groups = -(-head_dim // 32)
+    for x, like, width, what in ((k, v, 16 * groups, "k and v"), (k_scale, v_scale, groups, "k_scale and v_scale")):
+        if (x.dtype != torch.uint8 or like.dtype != torch.uint8 or x.shape != like.shape or x.stride() != like.stride()
+                or x.dim() not in (4, 5) or x.shape[-1] != width or (width > 1 and x.stride(-1) != 1)):
+            _refuse(f"{what}: uint8 pools [layers][pages][page tokens][heads][{width}] of one layout, the last dimension contiguous")
+    if k.shape[:-1] != k_scale.shape[:-1]:
+        _refuse("codes and scales differ in layers, pages, page tokens or heads")
+    d = _DTYPES.get(dtype)
+    if d is None:
+        _refuse(f"dtype {dtype} is neither bfloat16 nor float32")
+    pages, page, heads = k.shape[-4:-1]
+    st, ss = k.stride(), k_scale.stride()
+    five = k.dim() == 5
+    c = Cache4(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), d, heads, head_dim, page, pages,
+               k.shape[0] if five else 1, st[0] if five else 0, st[-4], st[-3], st[-2], ss[0] if five else 0, ss[-4], ss[-3], ss[-2])
+    c.tensors = (k, v, k_scale, v_scale)
+    return c
+
+
+def new_cache4(pages: int, page_tokens: int, heads: int, head_dim: int, layers: int = 0, dtype=torch.bfloat16,
+               device="cuda") -> Cache4:
+    """A cache of zeros in the layout that attention reads fastest: a head's page in one piece.  layers > 0: all of a
+    model's layers for kv_keep; `layer` gives each layer's own."""
+    groups = -(-head_dim // 32)
+    lead = (layers,) if layers else ()
+
+    def pool(width, value):
+        return torch.full(lead + (pages, heads, page_tokens, width), value, dtype=torch.uint8, device=device).transpose(-3, -2)
+
+    return make_cache4(pool(16 * groups, 0), pool(16 * groups, 0), pool(groups, 127), pool(groups, 127), head_dim, dtype)
+
+
+def layer(cache: Cache4, i: int) -> Cache4:
+    """Layer i of a 4-bit cache with layers, for kv_append and attention."""
+    if cache.tensors[0].dim() != 5 or not 0 <= i < cache.layers:
+        _refuse(f"layer {i} of {cache.layers}")
+    return make_cache4(*(t[i] for t in cache.tensors), cache.head_dim, torch.bfloat16 if cache.dtype == PSD_BF16 else torch.float32)
+
+
 def make_seqs(new_start, kv_len, table, rows: int, max_new: int, max_kv: int) -> Seqs:
     """Sequences of one call: new_start int32 [B+1], kv_len int32 [B], table int32 [B][width]; rows, max_new and
     max_kv bound the lengths, which may change on the device.  Keeps the tensors alive."""
@@ -513,10 +621,11 @@ def _ref(s):
     return None if s is None else ctypes.byref(s)
 
 
-def kv_append(cache: Cache, seqs: Seqs, k, v, q=None, q_out=None, cos=None, sin=None, interleaved: bool = False,
-              positions=None, q_norm=None, k_norm=None, eps: float = 1e-6, stream=None):
+def kv_append(cache, seqs: Seqs, k, v, q=None, q_out=None, cos=None, sin=None, interleaved: bool = False,
+              positions=None, q_norm=None, k_norm=None, eps: float = 1e-6, k_held=None, v_held=None, stream=None):
     """psd_kv_append: keys (normed with k_norm, turned by cos and sin float32 [positions][R/2]) and values into the
-    cache; returns the queries, treated the same way, in q_out (allocated when missing), or None without q."""
+    cache; returns the queries, treated the same way, in q_out (allocated when missing), or None without q.  Over a
+    Cache4 psd_kv_append4: k_held and v_held take the values that the cache then holds for the new tokens."""
     rows, heads = seqs.rows, cache.heads
     rk, rv = _rows(k, "k", cache, rows, heads), _rows(v, "v", cache, rows, heads)
     rq = ro = None
@@ -539,28 +648,37 @@ def kv_append(cache: Cache, seqs: Seqs, k, v, q=None, q_out=None, cos=None, sin=
         if w is not None and (w.shape != (cache.head_dim,) or not w.is_contiguous() or _dtype(w) != cache.dtype):
             _refuse("q_norm and k_norm: [head dim] in the cache's dtype")
     rot = Rotation(R, 1 if interleaved else 0, P, _ptr(cos), _ptr(sin), _ptr(positions), _ptr(q_norm), _ptr(k_norm), eps)
+    if type(cache) is Cache4:
+        kh = None if k_held is None else _rows(k_held, "k_held", cache, rows, heads)
+        vh = None if v_held is None else _rows(v_held, "v_held", cache, rows, heads)
+        _check(_lib.psd_kv_append4(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(rot), ctypes.byref(rk),
+                                   ctypes.byref(rv), _ref(rq), _ref(ro), H, _ref(kh), _ref(vh), _stream(stream)))
+        return q_out
+    if k_held is not None or v_held is not None:
+        _refuse("k_held and v_held: a cache in 4 bits holds other values than it is given, this one does not")
     _check(_lib.psd_kv_append(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(rot), ctypes.byref(rk),
                               ctypes.byref(rv), _ref(rq), _ref(ro), H, _stream(stream)))
     return q_out
 
 
-def attention_workspace_bytes(cache: Cache, seqs: Seqs, q_heads: int) -> int:
-    n = int(_lib.psd_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(seqs), q_heads))
+def attention_workspace_bytes(cache, seqs: Seqs, q_heads: int) -> int:
+    size = _lib.psd_attention4_workspace_bytes if type(cache) is Cache4 else _lib.psd_attention_workspace_bytes
+    n = int(size(ctypes.byref(cache), ctypes.byref(seqs), q_heads))
     if n == ctypes.c_size_t(-1).value:
         raise PsdError(PSD_E_ARG, (_lib.psd_last_error() or b"").decode())
     return n
 
 
-def new_attention_workspace(cache: Cache, seqs: Seqs, q_heads: int, device="cuda") -> torch.Tensor:
+def new_attention_workspace(cache, seqs: Seqs, q_heads: int, device="cuda") -> torch.Tensor:
     """Zero-filled device workspace of psd_attention for these bounds (may be empty)."""
     return torch.zeros(attention_workspace_bytes(cache, seqs, q_heads), dtype=torch.uint8, device=device)
 
 
-def attention(cache: Cache, seqs: Seqs, q, ws, scale: float = None, window: int = 0, mask=None, out=None,
+def attention(cache, seqs: Seqs, q, ws, scale: float = None, window: int = 0, mask=None, out=None,
               want_lse: bool = False, lse=None, stream=None):
     """psd_attention of q [rows][H][head dim] over the cache -> {"out", and "lse" float32 [rows][H] with
     want_lse}.  mask: int32 [rows][words], bit j % 32 of word j / 32 for new token j (draft paths).  scale
-    defaults to 1 / sqrt(head dim)."""
+    defaults to 1 / sqrt(head dim).  Over a Cache4 psd_attention4."""
     H, rows = q.shape[1], seqs.rows
     rq = _rows(q, "q", cache, rows, H)
     if out is None:
@@ -581,15 +699,16 @@ def attention(cache: Cache, seqs: Seqs, q, ws, scale: float = None, window: int 
         words = mask.shape[1]
     if scale is None:
         scale = cache.head_dim ** -0.5
-    _check(_lib.psd_attention(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(rq), H, scale, window, _ptr(mask), words,
-                              ctypes.byref(ro), _ptr(o.get("lse")), _ptr(ws), 0 if ws is None else ws.numel(),
-                              _stream(stream)))
+    call = _lib.psd_attention4 if type(cache) is Cache4 else _lib.psd_attention
+    _check(call(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(rq), H, scale, window, _ptr(mask), words,
+                ctypes.byref(ro), _ptr(o.get("lse")), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
     return o
 
 
-def kv_keep(cache: Cache, seqs: Seqs, keep, n_keep, kv_out=None, stream=None):
+def kv_keep(cache, seqs: Seqs, keep, n_keep, kv_out=None, stream=None):
     """psd_kv_keep: new tokens keep[b][i] (int32 [B][width], strictly ascending), i < n_keep[b] (int32 [B]), move to the
-    first new positions in every layer of the cache; returns the sequences' new lengths (int32 [B])."""
+    first new positions in every layer of the cache; returns the sequences' new lengths (int32 [B]).  Over a Cache4
+    psd_kv_keep4."""
     B = seqs.batch
     _ints(keep, "keep", 2)
     _ints(n_keep, "n_keep", 1)
@@ -599,9 +718,130 @@ def kv_keep(cache: Cache, seqs: Seqs, keep, n_keep, kv_out=None, stream=None):
         kv_out = torch.empty((B,), dtype=torch.int32, device=keep.device)
     else:
         _ints(kv_out, "kv_out", 1, B)
-    _check(_lib.psd_kv_keep(ctypes.byref(cache), ctypes.byref(seqs), _ptr(keep), _row_stride(keep, "keep"), keep.shape[1],
-                            _ptr(n_keep), _ptr(kv_out), _stream(stream)))
+    call = _lib.psd_kv_keep4 if type(cache) is Cache4 else _lib.psd_kv_keep
+    _check(call(ctypes.byref(cache), ctypes.byref(seqs), _ptr(keep), _row_stride(keep, "keep"), keep.shape[1],
+                _ptr(n_keep), _ptr(kv_out), _stream(stream)))
     return kv_out
+
+
+# ---------------------------------------------------------------- places for a call's tokens
+
+def make_pages(ring, state, page_tokens: int) -> Pages:
+    """Free pages: ring int32 [pages] and state int32 [4] (first free page, free pages, 0, 0) on the device.  Keeps both
+    tensors alive."""
+    _ints(ring, "ring", 1)
+    _ints(state, "state", 1)
+    if state.shape[0] != 4:
+        _refuse("state: int32 [4]")
+    p = Pages(int(page_tokens), ring.shape[0], ring.data_ptr(), state.data_ptr())
+    p.tensors = (ring, state)
+    return p
+
+
+def new_pages(pages: int, page_tokens: int, device="cuda") -> Pages:
+    """All pages of a pool, free."""
+    return make_pages(torch.arange(pages, dtype=torch.int32, device=device),
+                      torch.tensor([0, pages, 0, 0], dtype=torch.int32, device=device), page_tokens)
+
+
+def kv_reserve(pages: Pages, seqs: Seqs, n_new, kv_have, held, granted=None, rows_out: bool = True, out=None, stream=None):
+    """psd_kv_reserve: places for n_new (int32 [B]) tokens of each sequence behind the kv_have (int32 [B]) that stay.
+    held (int32 [B]) and the tensors that `seqs` was made of (new_start, kv_len, table) are written, pages come from
+    and go back to `pages`.  Returns {"granted" int32 [B]}, and with rows_out "row_seq", "positions" int32 [rows] and "slots"
+    int64 [rows] (allocated where `out` does not hold them)."""
+    new_start, kv_len, table = seqs.tensors
+    B, T = seqs.batch, seqs.rows
+    for x, what in ((n_new, "n_new"), (kv_have, "kv_have"), (held, "held")):
+        _ints(x, what, 1)
+        if x.shape[0] != B:
+            _refuse(f"{what}: int32 [{B}]")
+    o = {} if out is None else dict(out)
+    if granted is not None:
+        o["granted"] = granted
+    dev = n_new.device
+    names = (("granted", B, torch.int32),)
+    if rows_out:
+        names += (("row_seq", T, torch.int32), ("positions", T, torch.int32), ("slots", T, torch.int64))
+    for name, n, dt in names:
+        if name not in o:
+            o[name] = torch.empty((n,), dtype=dt, device=dev)
+        elif o[name].shape != (n,) or o[name].dtype != dt or not o[name].is_contiguous():
+            _refuse(f"{name}: contiguous {dt} [{n}]")
+    r = Reservation(n_new.data_ptr(), kv_have.data_ptr(), held.data_ptr(), seqs.table, seqs.new_start, seqs.kv_len,
+                    o["granted"].data_ptr())
+    if rows_out:
+        r.row_seq, r.positions, r.slots = o["row_seq"].data_ptr(), o["positions"].data_ptr(), o["slots"].data_ptr()
+    _check(_lib.psd_kv_reserve(ctypes.byref(pages), ctypes.byref(seqs), ctypes.byref(r), _stream(stream)))
+    return o
+
+
+# ---------------------------------------------------------------- logits before a race or a draw
+
+def _per_sequence(t, what: str, B: int, dtype):
+    if t.dtype != dtype or t.shape != (B,) or not t.is_contiguous():
+        _refuse(f"{what}: contiguous {dtype} [{B}]")
+
+
+def adjust_logits(params: Params, logits, text=None, length=None, text_from=None, draft_tokens=None, depth0: int = 0,
+                  repetition=None, presence=None, frequency=None, bias_tokens=None, bias=None, allowed=None, out=None, stream=None):
+    """psd_adjust_logits of logits [B][K][S][V] (or [B][S][V] with one path): penalties (float32 [B]) for the tokens of
+    text int32 [B][width] before length int64 [B] (from text_from int64 [B] on) and of a row's own earlier draft_tokens int32
+    [B][K][gamma], biases float32 [B][n] of bias_tokens int32 [B][n], and allowed: int32 words of 32 tokens' bits, [B][words] for all of
+    a sequence's rows or one mask a row ([B][K][S][words]).  Returns out (allocated when missing; it may be logits)."""
+    K, V = params.num_drafts, params.vocab
+    shape = logits.shape
+    if (len(shape) != 4 and (len(shape) != 3 or K != 1)) or shape[-1] != V or (len(shape) == 4 and shape[1] != K):
+        _refuse(f"logits: [B][{K}][S][{V}]")
+    B, S = shape[0], shape[-2]
+    if _DTYPES.get(logits.dtype) != params.dtype or not logits.is_contiguous():
+        _refuse("logits: contiguous, in params' dtype")
+    if out is None:
+        out = torch.empty_like(logits)
+    elif out.shape != shape or out.dtype != logits.dtype or not out.is_contiguous():
+        _refuse("out: shaped as logits, contiguous, in their dtype")
+    a = Adjustments()
+    if text is not None:
+        _ints(text, "text", 2, B)
+        if text.shape[0] != B or length is None:
+            _refuse("text: int32 [B][width], with length")
+        _per_sequence(length, "length", B, torch.int64)
+        a.text, a.length, a.text_max, a.text_stride = text.data_ptr(), length.data_ptr(), text.shape[1], _row_stride(text, "text")
+        if text_from is not None:
+            _per_sequence(text_from, "text_from", B, torch.int64)
+            a.from_ = text_from.data_ptr()
+    if draft_tokens is not None:
+        if (draft_tokens.dtype != torch.int32 or not draft_tokens.is_contiguous()
+                or draft_tokens.numel() != B * K * draft_tokens.shape[-1] or draft_tokens.shape[0] != B):
+            _refuse("draft_tokens: contiguous int32 [B][K][gamma]")
+        a.draft_tokens, a.gamma = draft_tokens.data_ptr(), draft_tokens.shape[-1]
+    if repetition is not None:
+        _per_sequence(repetition, "repetition", B, torch.float32)
+        a.repetition = repetition.data_ptr()
+    if presence is not None:
+        _per_sequence(presence, "presence", B, torch.float32)
+        a.presence = presence.data_ptr()
+    if frequency is not None:
+        _per_sequence(frequency, "frequency", B, torch.float32)
+        a.frequency = frequency.data_ptr()
+    if bias_tokens is not None:
+        if (bias is None or bias_tokens.dtype != torch.int32 or bias.dtype != torch.float32 or bias_tokens.dim() != 2
+                or bias_tokens.shape[0] != B or bias.shape != bias_tokens.shape or not bias_tokens.is_contiguous()
+                or not bias.is_contiguous()):
+            _refuse("bias_tokens int32 and bias float32: contiguous [B][n]")
+        a.bias_tokens, a.bias, a.bias_width = bias_tokens.data_ptr(), bias.data_ptr(), bias.shape[1]
+    if allowed is not None:
+        words = -(-V // 32)
+        if allowed.dtype != torch.int32 or not allowed.is_contiguous() or allowed.shape[-1] != words or allowed.shape[0] != B:
+            _refuse(f"allowed: contiguous int32 [B][{words}] or one mask a row")
+        if allowed.dim() == 2:
+            a.allowed_seq = words
+        elif allowed.shape[:-1] == shape[:-1]:
+            a.allowed_seq, a.allowed_row = allowed.numel() // B, words
+        else:
+            _refuse(f"allowed: contiguous int32 [B][{words}] or one mask a row")
+        a.allowed = allowed.data_ptr()
+    _check(_lib.psd_adjust_logits(ctypes.byref(params), ctypes.byref(a), B, S, depth0, _ptr(logits), _ptr(out), _stream(stream)))
+    return out
 
 
 # ---------------------------------------------------------------- verification from given random numbers
