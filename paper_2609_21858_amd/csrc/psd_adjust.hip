@@ -16,8 +16,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kSeg = 8192;         // tokens of a workgroup's stretch
 constexpr int kMaxBias = 1024;
+// A workgroup's stretch where there are many: 16 KB of bfloat16 or float32, four pieces a thread.
+constexpr int stretch(bool bf16) { return bf16 ? 8192 : 4096; }
+constexpr int short_stretch(bool bf16) { return stretch(bf16) / 4; }
 // A token's word: bit 31 where it has biases, their place in the list, and its count below.
 constexpr uint32_t kBiased = 1u << 31, kCount = (1u << 20) - 1;
 constexpr float kGone = -__builtin_inff();
@@ -42,24 +44,25 @@ struct Piece<false> {
     __device__ static float narrow1(float x) { return x; }
 };
 
-// One workgroup: a stretch of kSeg tokens of rows [r0, r1) of a sequence.
-template <bool BF16>
+// One workgroup: a stretch of SEG tokens of rows [r0, r1) of a sequence.  A row's next pieces are on their way while
+// this one's are computed; pieces that nothing touches pass through as they are (in place: are not read).
+template <bool BF16, int SEG>
 __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segments, int per) {
     using E = Elem<BF16>;
     using Pc = Piece<BF16>;
     constexpr int VEC = E::kVec;
-    __shared__ __align__(16) uint32_t s_word[kSeg];
+    __shared__ __align__(16) uint32_t s_word[SEG];
     __shared__ float s_bias[kMaxBias];
-    __shared__ int s_bias_token[kMaxBias];
+    __shared__ uint16_t s_bias_token[kMaxBias];  // (less than 4 workgroups of 8192 tokens would fit a CU with 32 bits)
     __shared__ int s_wave[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int seg = blockIdx.x % segments;
     const int rest = blockIdx.x / segments;
     const int R = a.K * a.S, groups = (R + per - 1) / per;
     const int b = rest / groups, r0 = (rest - b * groups) * per, r1 = min(r0 + per, R);
-    const int v0 = seg * kSeg, v1 = min(v0 + kSeg, a.V);
+    const int v0 = seg * SEG, v1 = min(v0 + SEG, a.V);
 
-    for (int i = tid; i < kSeg / 4; i += kThreads) ((u32x4*)s_word)[i] = u32x4{0, 0, 0, 0};
+    for (int i = tid; i < SEG / 4; i += kThreads) ((u32x4*)s_word)[i] = u32x4{0, 0, 0, 0};
     __syncthreads();
     // the stretch's biases, in the order of the list
     int n_bias = 0;
@@ -76,7 +79,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
             n_bias += s_wave[w];
         }
         if (in) {
-            s_bias_token[at] = v - v0;
+            s_bias_token[at] = (uint16_t)(v - v0);
             s_bias[at] = a.bias[(int64_t)b * a.bias_width + i];
             atomicMax(&s_word[v - v0], kBiased | (uint32_t)(kMaxBias - 1 - at) << 20);  // the first of a token's entries stands for it
         }
@@ -120,23 +123,52 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
         if (word & kBiased) z += s_bias[kMaxBias - 1 - (word >> 20 & 1023)];
         return may ? z : kGone;
     };
+    constexpr int N = SEG / (kThreads * VEC);  // pieces of a thread in a row
+    const int64_t row0 = (int64_t)b * R * a.V;
+    const typename Pc::one* src0 = (const typename Pc::one*)a.logits + row0;
+    typename Pc::one* dst0 = (typename Pc::one*)a.out + row0;
+    auto at = [&](int n) { return v0 + (n * kThreads + tid) * VEC; };
+    u32x4 next[N];
+    uint32_t may_next[N];
+    constexpr uint32_t kEvery = (1u << VEC) - 1;
+    auto load = [&](int r) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int v = at(n);
+            may_next[n] = kEvery;
+            if (v >= v1) continue;
+            if (!same && v + VEC <= a.V) next[n] = *(const typename Pc::any*)(src0 + (int64_t)r * a.V + v);
+            if (a.allowed) may_next[n] = a.allowed[b * a.allowed_seq + r * a.allowed_row + v / 32] >> (v % 32) & kEvery;
+        }
+    };
+    load(r0);
     int path = -1, depth = 0;  // the drafts that are counted: `path`'s before `depth`
+    __syncthreads();
     for (int r = r0; r < r1; ++r) {
-        const int k = r / a.S, d = a.depth0 + r - k * a.S;
-        __syncthreads();
         if (drafts) {
+            const int k = r / a.S, d = a.depth0 + r - k * a.S;
             const int keep = k == path ? depth : 0;
+            if (r > r0) __syncthreads();
             if (k != path && tid < depth) count(drafts[path * a.gamma + tid], ~0u);  // (minus one)
             if (tid >= keep && tid < d) count(drafts[k * a.gamma + tid], 1);
             path = k;
             depth = d;
             __syncthreads();
         }
-        const int64_t row = ((int64_t)b * R + r) * a.V;
-        const typename Pc::one* src = (const typename Pc::one*)a.logits + row;
-        typename Pc::one* dst = (typename Pc::one*)a.out + row;
-        const uint32_t* allowed = a.allowed ? a.allowed + b * a.allowed_seq + r * a.allowed_row : nullptr;
-        for (int v = v0 + tid * VEC; v < v1; v += kThreads * VEC) {
+        u32x4 now[N];
+        uint32_t may[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            now[n] = next[n];
+            may[n] = may_next[n];
+        }
+        if (r + 1 < r1) load(r + 1);
+        const typename Pc::one* src = src0 + (int64_t)r * a.V;
+        typename Pc::one* dst = dst0 + (int64_t)r * a.V;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int v = at(n);
+            if (v >= v1) break;
             uint32_t words[VEC];
             uint32_t any = 0;
 #pragma unroll
@@ -148,35 +180,70 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
                     any |= w[e];
                 }
             }
-            const uint32_t every = (1u << VEC) - 1;
-            const uint32_t may = allowed ? allowed[v / 32] >> (v % 32) & every : every;
-            if (same && any == 0 && may == every) continue;
+            const bool touched = any != 0 || may[n] != kEvery;
+            if (same && !touched) continue;
             if (v + VEC <= a.V) {
-                float x[VEC];
-                E::widen(*(const typename Pc::any*)(src + v), x);
+                u32x4 y;
+                if (!touched) {
+                    y = now[n];
+                } else {
+                    float x[VEC];
+                    if (same && may[n] != 0) now[n] = *(const typename Pc::any*)(src + v);
+                    E::widen(now[n], x);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) x[i] = value(x[i], words[i], may >> i & 1);
-                *(typename Pc::any*)(dst + v) = E::narrow(x);
+                    for (int i = 0; i < VEC; ++i) x[i] = value(x[i], words[i], may[n] >> i & 1);
+                    y = E::narrow(x);
+                }
+                *(typename Pc::any*)(dst + v) = y;
             } else {
-                for (int i = 0; v + i < a.V; ++i) dst[v + i] = Pc::narrow1(value(Pc::widen1(src[v + i]), s_word[v - v0 + i], may >> i & 1));
+                for (int i = 0; v + i < a.V; ++i) dst[v + i] = Pc::narrow1(value(Pc::widen1(src[v + i]), s_word[v - v0 + i], may[n] >> i & 1));
             }
         }
     }
 }
 
+// Workgroups: a long stretch and all rows of a sequence each, so that its text is counted once a stretch; fewer
+// rows, then a short stretch, while there are too few to fill the device.
+struct Cut {
+    int seg, segments, per;
+};
+constexpr long kFill = 768;
+inline Cut cut(const AdjustArgs& a, bool bf16) {
+    Cut c;
+    c.seg = stretch(bf16);
+    c.segments = (a.V + c.seg - 1) / c.seg;
+    const int R = a.K * a.S;
+    c.per = R;
+    while (c.per > 1 && (long)c.segments * a.B * ((R + c.per - 1) / c.per) < kFill) c.per = (c.per + 1) / 2;
+    if (c.per == 1 && (long)c.segments * a.B * R < kFill) {
+        c.seg = short_stretch(bf16);
+        c.segments = (a.V + c.seg - 1) / c.seg;
+    }
+    return c;
+}
+
+template <bool BF16>
+void launch(const AdjustArgs& a, const Cut& c, hipStream_t stream) {
+    const dim3 grid((unsigned)((long)c.segments * a.B * ((a.K * a.S + c.per - 1) / c.per)));
+    if (c.seg == short_stretch(BF16))
+        hipLaunchKernelGGL((adjust_kernel<BF16, short_stretch(BF16)>), grid, dim3(kThreads), 0, stream, a, c.segments, c.per);
+    else
+        hipLaunchKernelGGL((adjust_kernel<BF16, stretch(BF16)>), grid, dim3(kThreads), 0, stream, a, c.segments, c.per);
+}
+
 }  // namespace
 
-bool adjust_fits(const AdjustArgs& a) { return (long)((a.V + kSeg - 1) / kSeg) * a.B * a.K * a.S < 1L << 23; }
+bool adjust_fits(const AdjustArgs& a, bool bf16) {
+    const Cut c = cut(a, bf16);
+    return (long)c.segments * a.B * ((a.K * a.S + c.per - 1) / c.per) < 1L << 23;
+}
 
 hipError_t launch_adjust(const AdjustArgs& a, bool bf16, hipStream_t stream) {
-    const int segments = (a.V + kSeg - 1) / kSeg;
-    const int R = a.K * a.S;
-    const int per = R;
-    const dim3 grid((unsigned)((long)segments * a.B * ((R + per - 1) / per)));
+    const Cut c = cut(a, bf16);
     if (bf16)
-        hipLaunchKernelGGL((adjust_kernel<true>), grid, dim3(kThreads), 0, stream, a, segments, per);
+        launch<true>(a, c, stream);
     else
-        hipLaunchKernelGGL((adjust_kernel<false>), grid, dim3(kThreads), 0, stream, a, segments, per);
+        launch<false>(a, c, stream);
     return hipGetLastError();
 }
 

@@ -1490,7 +1490,7 @@ psd_status psd_adjust_logits(const psd_params* params, const psd_adjustments* ad
     a.allowed = j.allowed;
     a.allowed_seq = j.allowed_seq;
     a.allowed_row = j.allowed_row;
-    if (!psd::adjust_fits(a)) return fail(PSD_E_ARG, "call too large: batch %d", batch);
+    if (!psd::adjust_fits(a, params->dtype == PSD_BF16)) return fail(PSD_E_ARG, "call too large: batch %d", batch);
     const hipError_t e = psd::launch_adjust(a, params->dtype == PSD_BF16, stream);
     if (e != hipSuccess) return hip_fail(e, "adjustment kernel launch");
     return PSD_OK;

@@ -115,7 +115,7 @@ struct AdjustArgs {
     const uint32_t* allowed;
     int64_t allowed_seq, allowed_row;
 };
-bool adjust_fits(const AdjustArgs& a);  // the launch stays inside a grid's limits
+bool adjust_fits(const AdjustArgs& a, bool bf16);  // the launch stays inside a grid's limits
 hipError_t launch_adjust(const AdjustArgs& a, bool bf16, hipStream_t stream);
 
 struct GivenArgs {
