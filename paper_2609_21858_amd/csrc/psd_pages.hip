@@ -16,6 +16,10 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
+constexpr int kBatch = 4;
+
+typedef int i32x4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef int64_t i64x2 __attribute__((ext_vector_type(2), aligned(8)));
 
 // Inclusive sums over the workgroup of N values a thread; the totals in `total`.
 template <int N>
@@ -92,8 +96,9 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveArgs a) {
         s.give = max(s.held - s.keep, 0);
         return s;
     };
+    Share s;
     for (int c0 = 0; c0 < a.B; c0 += kThreads) {
-        const Share s = share(c0);
+        s = share(c0);
         int64_t x[3] = {s.n, s.take, s.give}, sum[3];
         block_sums<3>(x, sum, s_wave);
         s_start[tid + 1] = (int)x[0];
@@ -122,30 +127,82 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveArgs a) {
                 if (sums[lo + step] <= i) lo += step;
             return lo;
         };
+        // Four consecutive rows a thread: one search, mostly one page, and stores of 16 bytes.
         if (a.row_seq || a.positions || a.slots)
-            for (int64_t i = (int64_t)wg * kThreads + tid; i < sum[0]; i += (int64_t)wgs * kThreads) {
-                const int q = find(s_start, i);
-                const int pos = s_have[q] + (int)i - s_start[q];
-                const int64_t t = rows + i;
-                if (a.row_seq) a.row_seq[t] = c0 + q;
-                if (a.positions) a.positions[t] = pos;
-                if (a.slots) {
-                    const int pi = page_at(pos);
-                    const int page = pi < s_held[q] ? a.table[(int64_t)(c0 + q) * a.table_stride + pi]
-                                                    : a.ring[ring_at(taken + s_take[q] + pi - s_held[q])];
-                    a.slots[t] = (unsigned)page < (unsigned)a.pages ? (int64_t)page * a.P + (pos - pi * a.P) : -1;
+            for (int64_t t0 = (rows / 4 + (int64_t)wg * kThreads + tid) * 4; t0 < rows + sum[0]; t0 += (int64_t)wgs * kThreads * 4) {
+                int q = find(s_start, max(t0 - rows, (int64_t)0));
+                int had = -1, page = 0;  // position of the page that was found last
+                i32x4 seq, pos;
+                i64x2 slot[2];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = (int)(t0 + e - rows);
+                    if (i < 0 || i >= sum[0]) continue;
+                    while (s_start[q + 1] <= i) {
+                        ++q;
+                        had = -1;
+                    }
+                    seq[e] = c0 + q;
+                    pos[e] = s_have[q] + i - s_start[q];
+                    if (!a.slots) continue;
+                    const int pi = page_at(pos[e]);
+                    if (pi != had)
+                        page = pi < s_held[q] ? a.table[(int64_t)(c0 + q) * a.table_stride + pi]
+                                              : a.ring[ring_at(taken + s_take[q] + pi - s_held[q])];
+                    had = pi;
+                    slot[e / 2][e % 2] = (unsigned)page < (unsigned)a.pages ? (int64_t)page * a.P + (pos[e] - pi * a.P) : -1;
+                }
+                if (t0 >= rows && t0 + 4 <= rows + sum[0]) {
+                    if (a.row_seq) *(i32x4*)(a.row_seq + t0) = seq;
+                    if (a.positions) *(i32x4*)(a.positions + t0) = pos;
+                    if (a.slots) {
+                        *(i64x2*)(a.slots + t0) = slot[0];
+                        *(i64x2*)(a.slots + t0 + 2) = slot[1];
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int64_t t = t0 + e;
+                        if (t < rows || t >= rows + sum[0]) continue;
+                        if (a.row_seq) a.row_seq[t] = seq[e];
+                        if (a.positions) a.positions[t] = pos[e];
+                        if (a.slots) a.slots[t] = slot[e / 2][e % 2];
+                    }
                 }
             }
-        for (int64_t i = (int64_t)wg * kThreads + tid; i < sum[1]; i += (int64_t)wgs * kThreads) {
-            const int q = find(s_take, i);
-            a.table[(int64_t)(c0 + q) * a.table_stride + s_held[q] + (i - s_take[q])] = a.ring[ring_at(taken + i)];
+        // Pages, kBatch of a thread together, so that their loads are in flight together.
+        for (int64_t i0 = (int64_t)wg * kThreads + tid; i0 < sum[1]; i0 += (int64_t)wgs * kThreads * kBatch) {
+            int32_t* to[kBatch];
+            int page[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int64_t i = min(i0 + (int64_t)k * wgs * kThreads, sum[1] - 1);
+                const int q = find(s_take, i);
+                to[k] = a.table + (int64_t)(c0 + q) * a.table_stride + s_held[q] + (i - s_take[q]);
+                page[k] = a.ring[ring_at(taken + i)];
+            }
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k)
+                if (i0 + (int64_t)k * wgs * kThreads < sum[1]) *to[k] = page[k];
         }
-        for (int64_t i = (int64_t)wg * kThreads + tid; i < sum[2]; i += (int64_t)wgs * kThreads) {
-            const int q = find(s_give, i);
-            int32_t* entry = a.table + (int64_t)(c0 + q) * a.table_stride + s_keep[q] + (i - s_give[q]);
-            // (more than the ring holds: the caller's error, dropped)
-            if (free + given + i < a.pages) a.ring[ring_at(free + given + i)] = *entry;
-            *entry = -1;
+        for (int64_t i0 = (int64_t)wg * kThreads + tid; i0 < sum[2]; i0 += (int64_t)wgs * kThreads * kBatch) {
+            int32_t* from[kBatch];
+            int page[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int64_t i = min(i0 + (int64_t)k * wgs * kThreads, sum[2] - 1);
+                const int q = find(s_give, i);
+                from[k] = a.table + (int64_t)(c0 + q) * a.table_stride + s_keep[q] + (i - s_give[q]);
+                page[k] = *from[k];
+            }
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int64_t i = i0 + (int64_t)k * wgs * kThreads;
+                if (i >= sum[2]) continue;
+                // (more than the ring holds: the caller's error, dropped)
+                if (free + given + i < a.pages) a.ring[ring_at(free + given + i)] = page[k];
+                *from[k] = -1;
+            }
         }
         rows += sum[0];
         taken += sum[1];
@@ -165,7 +222,7 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveArgs a) {
     }
     asked = needed = 0;
     for (int c0 = 0; c0 < a.B; c0 += kThreads) {
-        const Share s = share(c0);
+        if (a.B > kThreads) s = share(c0);  // (else it is at hand)
         if (c0 + tid < a.B) a.held[c0 + tid] = s.held - (int)s.give + (int)s.take;
     }
     if (tid == 0) {
@@ -182,8 +239,11 @@ hipError_t launch_kv_reserve(const ReserveArgs& args, hipStream_t stream) {
     a.page_shift = -1;
     for (int k = 0; k <= 16; ++k)
         if (a.P == 1 << k) a.page_shift = k;
+    // Workgroups for four rows a thread, and for half of the tables' entries in turn (how many change only the device knows);
+    // each more takes the sums again.
     const long rows = a.row_seq || a.positions || a.slots ? a.rows : 0;
-    const int wgs = (int)std::min<long>(std::max<long>((rows + 4 * kThreads - 1) / (4 * kThreads), 1), 256);
+    const long work = std::max<long>(rows, (long)a.B * a.table_width / 2);
+    const int wgs = (int)std::min<long>(std::max<long>((work + 4 * kThreads - 1) / (4 * kThreads), 1), 512);
     hipLaunchKernelGGL(reserve_kernel, dim3(wgs), dim3(kThreads), 0, stream, a);
     return hipGetLastError();
 }
