@@ -121,7 +121,7 @@ __global__ __launch_bounds__(64 * stream_waves(DP, RB), 1) void stream_kernel(At
     const int r = lane & 15, q = lane >> 4;
     const int g = blockIdx.x % c.G, wg = blockIdx.x / c.G;
 
-    const Stretch st = find_stretch(a, p, sh, wg, join_units(BF16));
+    const Stretch st = find_stretch<0>(a, p, sh, wg, join_units(BF16));
     if (st.u0 == st.u1) return;
     const float sc = a.scale * kLog2e;
     const int64_t head_at = (int64_t)g * c.stride_head;

@@ -51,23 +51,29 @@ struct Stream4Shape {
     static constexpr int V_BYTES = 32 * PITCH * 2;
 };
 
+// Blocks of a wave on their way into registers: two where they fit.
+template <bool BF16, int DP, int RB>
+constexpr int stream4_ahead() {
+    return 1;
+}
+
 template <int DP, int RB>
 constexpr int stream4_lds() {
-    constexpr int waves = stream4_waves(DP, RB);
-    constexpr int values = waves * Stream4Shape<DP>::V_BYTES, join = waves * 16 * RB * (DP + 4) * 4;
+    constexpr int values = kWaves4 * Stream4Shape<DP>::V_BYTES, join = kWaves4 * 16 * RB * (DP + 4) * 4;
     return values > join ? values : join;
 }
 
 template <bool BF16, int DP, int RB>
-__global__ __launch_bounds__(64 * stream4_waves(DP, RB), 1) void stream4_kernel(Attention4Args args, Plan p) {
+__global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream4_kernel(Attention4Args args, Plan p) {
     using S = Stream4Shape<DP>;
     using E = Elem<BF16>;
     constexpr int TERMS = BF16 ? 1 : 3;
     constexpr int DB = DP / 16;
-    constexpr int NW = stream4_waves(DP, RB), NT = 64 * NW;
+    constexpr int NW = kWaves4, NT = 64 * NW;
     constexpr int ROWS = 16 * RB;
     __shared__ __align__(16) char s_mem[stream4_lds<DP, RB>()];
-    __shared__ int64_t s_off[NW][2][S::TOK], s_scale[NW][2][S::TOK];
+    constexpr int AHEAD = stream4_ahead<BF16, DP, RB>();
+    __shared__ int64_t s_off[NW][AHEAD + 1][S::TOK], s_scale[NW][AHEAD + 1][S::TOK];
     __shared__ StreamShared<NT, ROWS> sh;
 
     const AttentionArgs& a = args.a;
@@ -75,9 +81,10 @@ __global__ __launch_bounds__(64 * stream4_waves(DP, RB), 1) void stream4_kernel(
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int r = lane & 15, q = lane >> 4;
     const int g = blockIdx.x % c.G, wg = blockIdx.x / c.G;
-    const Stretch st = find_stretch(a, p, sh, wg, join_units(BF16));
+    const Stretch st = find_stretch<slack4(BF16, DP)>(a, p, sh, wg, join_units4(BF16));
     if (st.u0 == st.u1) return;
 
+    const bool younger = stream4_resident(DP, RB) > 1 && blockIdx.x >= gridDim.x / 2;
     const float sc = a.scale * kLog2e;
     const int last_group = (c.D + 31) / 32 - 1;
     char* s_v = s_mem + wave * S::V_BYTES;
@@ -112,6 +119,17 @@ __global__ __launch_bounds__(64 * stream4_waves(DP, RB), 1) void stream4_kernel(
         const int blocks = (c1 - c0 + S::TOK - 1) / S::TOK;
         const int32_t* table = c.table + (int64_t)b * c.table_stride;
 
+        // A block's tokens: lane t finds token t's place; -1: nothing there.  The page number is loaded a block before
+        // it is used, so that no load in between has to be waited for with it.
+        auto token_of = [&](int blk) { return c0 + blk * S::TOK + lane; };
+        auto page_of = [&](int blk) {
+            const int j = token_of(blk);
+            const int at = j < c1 ? j : 0;
+            return table[p.page_shift >= 0 ? at >> p.page_shift : at / c.P];
+        };
+        int pages[AHEAD + 1];  // (set out first: the first keys wait for them)
+#pragma unroll
+        for (int n = 0; n <= AHEAD; ++n) pages[n] = page_of(wave + n * NW);
         // this lane's rows, and their queries as B operands (unconditional loads; what is not there counts as zero)
         int row_i[RB];
         u32x4 qf[RB][TERMS][S::KK];
@@ -155,14 +173,6 @@ __global__ __launch_bounds__(64 * stream4_waves(DP, RB), 1) void stream4_kernel(
 #pragma unroll
             for (int db = 0; db < DB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        // A block's tokens: lane t finds token t's place; -1: nothing there.  The page number is loaded a block before
-        // it is used, so that no load in between has to be waited for with it.
-        auto token_of = [&](int blk) { return c0 + blk * S::TOK + lane; };
-        auto page_of = [&](int blk) {
-            const int j = token_of(blk);
-            const int at = j < c1 ? j : 0;
-            return table[p.page_shift >= 0 ? at >> p.page_shift : at / c.P];
-        };
         auto wave_sync = [&]() {
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -180,47 +190,64 @@ __global__ __launch_bounds__(64 * stream4_waves(DP, RB), 1) void stream4_kernel(
             wave_sync();
             return bits;
         };
-        uint32_t kc[S::TT][S::KK], ks[S::TT][S::NS], vs[S::NV];
-        u32x4 vc[S::NV];
-        auto load_keys = [&](int slot) {
+        struct Block {
+            uint64_t there;
+            uint32_t kc[S::TT][S::KK];
+            u32x4 vc[S::NV];
+            // (bytes as loaded: widened to words here, they would be waited for a round early)
+            uint8_t ks[S::TT][S::NS], vs[S::NV];
+        };
+        auto load_keys = [&](int slot, Block& x) {
 #pragma unroll
             for (int t = 0; t < S::TT; ++t) {
                 const char* src = k_src + s_off[wave][slot][16 * t + r];
                 const uint8_t* scale = ks_src + s_scale[wave][slot][16 * t + r];
                 if constexpr (DP == 64) {
                     const uint2 w = *(const uint2*)(src + key_at[0]);
-                    kc[t][0] = w.x;
-                    kc[t][1] = w.y;
+                    x.kc[t][0] = w.x;
+                    x.kc[t][1] = w.y;
                 } else {
 #pragma unroll
                     for (int n = 0; n < S::NS; ++n) {
                         const u32x4 w = *(const u32x4*)(src + key_at[n]);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) kc[t][4 * n + e] = w[e];
+                        for (int e = 0; e < 4; ++e) x.kc[t][4 * n + e] = w[e];
                     }
                 }
 #pragma unroll
-                for (int n = 0; n < S::NS; ++n) ks[t][n] = scale[key_group[n]];
+                for (int n = 0; n < S::NS; ++n) x.ks[t][n] = scale[key_group[n]];
             }
         };
-        auto load_values = [&](int slot) {
+        auto load_values = [&](int slot, Block& x) {
 #pragma unroll
             for (int k = 0; k < S::NV; ++k) {
-                vc[k] = *(const u32x4*)(v_src + s_off[wave][slot][k * S::TPI + v_token]);
-                vs[k] = vs_src[s_scale[wave][slot][k * S::TPI + v_token]];
+                x.vc[k] = *(const u32x4*)(v_src + s_off[wave][slot][k * S::TPI + v_token]);
+                x.vs[k] = vs_src[s_scale[wave][slot][k * S::TPI + v_token]];
             }
         };
 
-        uint64_t there = publish(wave, page_of(wave), 0);
-        int page_next = page_of(wave + NW);
-        load_keys(0);
-        __builtin_amdgcn_sched_barrier(0);  // keys before values, as in the loop: their wait counts on it
-        load_values(0);
-        int slot = 0;
-        for (int round = 0; round < blocks; round += NW, slot ^= 1) {
-            __builtin_amdgcn_s_barrier();  // keeps the waves in step, see stream_kernel
-            const int blk = round + wave;
-            if (blk >= blocks) continue;
+        Block block[AHEAD];
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) {
+            block[n].there = publish(wave + n * NW, pages[n], n);
+            load_keys(n, block[n]);
+            __builtin_amdgcn_sched_barrier(0);  // keys before values, as in the loop: their wait counts on it
+            load_values(n, block[n]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        int page = pages[AHEAD], slot = 0;
+        // Block `blk`, whose places are in `slot`; x then takes the block AHEAD rounds later.
+        auto step = [&](int blk, Block& x) {
+            // A CU serves its older waves first: its first workgroup would end 7 of 45 us before its second (32 x 8192 tokens).
+            // The second goes first in every other block, which leaves 3.
+            if (younger) {
+                if (blk / NW & 1)
+                    __builtin_amdgcn_s_setprio(1);
+                else
+                    __builtin_amdgcn_s_setprio(0);
+            }
+            const int fill = slot == 0 ? AHEAD : slot - 1;  // the slot of that one
+            const uint64_t there = x.there;
             const int j0 = c0 + blk * S::TOK;
             // every row sees the whole block, or bits say which tokens
             const bool whole = there == ~0ull &&
@@ -233,17 +260,46 @@ __global__ __launch_bounds__(64 * stream4_waves(DP, RB), 1) void stream4_kernel(
                 for (int rb = 0; rb < RB; ++rb) sv[rb][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int kk = 0; kk < S::KK; ++kk) {
-                    const u32x4 keys = quant4::decode8(kc[t][kk], quant4::scale_value(ks[t][S::NS == 2 ? kk / 4 : 0]));
+                    const u32x4 keys = quant4::decode8(x.kc[t][kk], quant4::scale_value(x.ks[t][S::NS == 2 ? kk / 4 : 0]));
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
                         for (int i = 0; i < TERMS; ++i) sv[rb][t] = multiply<true>(keys, qf[rb][i][kk], sv[rb][t]);
                 }
             }
-            // the next block's keys set out
-            const uint64_t there_next = publish(blk + NW, page_next, slot ^ 1);
-            load_keys(slot ^ 1);
-            page_next = page_of(blk + 2 * NW);
+            // the later block's keys set out
+            x.there = publish(blk + AHEAD * NW, page, fill);
+            load_keys(fill, x);
+            page = page_of(blk + (AHEAD + 1) * NW);
+            // A row's weight 0 times a NaN value that the row does not see would be NaN: where rows differ in what they see,
+            // such groups are taken out, and a second product puts infinity where a row does see one.
+            bool odd = false;
+            if (!whole) {
+                bool any = false;
+#pragma unroll
+                for (int k = 0; k < S::NV; ++k) {
+                    const bool gone = !((there >> (k * S::TPI + v_token)) & 1u), nan = x.vs[k] > quant4::kMost;
+                    any |= nan && !gone;
+                    if (gone || nan) {
+                        x.vc[k] = u32x4{0, 0, 0, 0};
+                        x.vs[k] = 127;
+                    }
+                }
+                odd = __any(any);
+            }
+            auto piece_at = [&](int k) {  // of the half's buffer
+                return s_v + ((k % (S::NV / 2) * S::TPI + v_token) * S::PITCH + v_group * 32) * 2;
+            };
+            auto write_values = [&](int h) {
+#pragma unroll
+                for (int k = h * S::NV / 2; k < (h + 1) * S::NV / 2; ++k) {
+                    const float by = quant4::scale_value(x.vs[k]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) *(u32x4*)(piece_at(k) + 16 * e) = quant4::decode8(x.vc[k][e], by);
+                }
+                wave_sync();
+            };
+            write_values(0);  // beside the softmax
             u32x4 w[RB][2][TERMS];
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
@@ -278,80 +334,72 @@ __global__ __launch_bounds__(64 * stream4_waves(DP, RB), 1) void stream4_kernel(
                     for (int db = 0; db < DB; ++db) o[rb][db] *= by;
                 }
                 const float base = m[rb] == kNoScore ? 0.f : m[rb];
+                f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int t = 0; t < S::TT; ++t)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         sv[rb][t][e] = exp2_hw(sv[rb][t][e] - base);
-                        l[rb] += sv[rb][t][e];
+                        sum[e] += sv[rb][t][e];
                     }
+                l[rb] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float x = sv[rb][2 * h + e / 2][2 * (e % 2)], y = sv[rb][2 * h + e / 2][2 * (e % 2) + 1];
+                        const float w0 = sv[rb][2 * h + e / 2][2 * (e % 2)], w1 = sv[rb][2 * h + e / 2][2 * (e % 2) + 1];
                         if constexpr (BF16) {
-                            w[rb][h][0][e] = pack_bf16(x, y);
+                            w[rb][h][0][e] = pack_bf16(w0, w1);
                         } else {
                             float u[TERMS], v[TERMS];
-                            split(x, u);
-                            split(y, v);
+                            split(w0, u);
+                            split(w1, v);
 #pragma unroll
                             for (int i = 0; i < TERMS; ++i) w[rb][h][i][e] = upper(u[i], v[i]);
                         }
                     }
             }
 
-            // A row's weight 0 times a NaN value that the row does not see would be NaN: where rows differ in what they see,
-            // such groups are taken out, and a second product puts infinity where a row does see one.
-            bool odd = false;
-            if (!whole) {
-                bool any = false;
-#pragma unroll
-                for (int k = 0; k < S::NV; ++k) {
-                    const bool gone = !((there >> (k * S::TPI + v_token)) & 1u), nan = vs[k] > quant4::kMost;
-                    any |= nan && !gone;
-                    if (gone || nan) {
-                        vc[k] = u32x4{0, 0, 0, 0};
-                        vs[k] = 127;
-                    }
-                }
-                odd = __any(any);
-            }
-            // o += V^T of 16 dimensions (this lane's dimension of the tokens of its weights) times the weights of half h
+            // o += V^T of 16 dimensions (this lane's dimension of the tokens of its weights) times the weights of half h;
+            // LANES pieces of values are on their way from LDS while those before them are multiplied
+            constexpr int LANES = DB < 4 ? DB : 4;
             auto add_values = [&](int h) {
+                u32x4 v[2][LANES];
+                auto read = [&](int group, u32x4 (&into)[LANES]) {
 #pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    char* at = s_v + ((4 * q + r / 4) * S::PITCH + db * 16 + (r % 4) * 4) * 2;
-                    union {
-                        s16x4 half[2];
-                        u32x4 all;
-                    } both;
-                    both.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at));
-                    both.half[1] =
-                        __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 16 * S::PITCH * 2));
+                    for (int i = 0; i < LANES; ++i) {
+                        char* at = s_v + ((4 * q + r / 4) * S::PITCH + (group * LANES + i) * 16 + (r % 4) * 4) * 2;
+                        union {
+                            s16x4 half[2];
+                            u32x4 all;
+                        } both;
+                        both.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at));
+                        both.half[1] =
+                            __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + 16 * S::PITCH * 2));
+                        into[i] = both.all;
+                    }
+                };
+                read(0, v[0]);
 #pragma unroll
-                    for (int rb = 0; rb < RB; ++rb)
+                for (int n = 0; n < DB / LANES; ++n) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (n + 1 < DB / LANES) read(n + 1, v[(n + 1) & 1]);
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int i = 0; i < TERMS; ++i) o[rb][db] = multiply<true>(both.all, w[rb][h][i], o[rb][db]);
+                    for (int i = 0; i < LANES; ++i)
+#pragma unroll
+                        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                            for (int t = 0; t < TERMS; ++t)
+                                o[rb][n * LANES + i] = multiply<true>(v[n & 1][i], w[rb][h][t], o[rb][n * LANES + i]);
                 }
             };
-            auto piece_at = [&](int k) {  // of the half's buffer
-                return s_v + ((k % (S::NV / 2) * S::TPI + v_token) * S::PITCH + v_group * 32) * 2;
-            };
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int k = h * S::NV / 2; k < (h + 1) * S::NV / 2; ++k) {
-                    const float by = quant4::scale_value(vs[k]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) *(u32x4*)(piece_at(k) + 16 * e) = quant4::decode8(vc[k][e], by);
-                }
-                wave_sync();
-                if (h == 1) load_values(slot ^ 1);
-                add_values(h);
-                wave_sync();
-            }
+            add_values(0);
+            wave_sync();
+            write_values(1);
+            load_values(fill, x);
+            add_values(1);
+            wave_sync();
             if (odd) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -380,20 +428,25 @@ __global__ __launch_bounds__(64 * stream4_waves(DP, RB), 1) void stream4_kernel(
                     wave_sync();
                 }
             }
-            there = there_next;
+            slot = slot == AHEAD ? 0 : slot + 1;
+        };
+        for (int round = 0; round < blocks; round += AHEAD * NW) {
+#pragma unroll
+            for (int n = 0; n < AHEAD; ++n) {
+                const int blk = round + n * NW + wave;
+                if (blk < blocks) step(blk, block[n]);
+            }
         }
-        finish_item<BF16, DP, RB, NT>(a, p, sh, s_mem, st, Item{s, row0, rows, before, n_units, from, to}, wg, g, o, m, l);
+        finish_item<BF16, DP, RB, NT, 4>(a, p, sh, s_mem, st, Item{s, row0, rows, before, n_units, from, to}, wg, g, o, m, l);
     }
 }
 
 template <bool BF16, int DP>
 void launch_stream4(const Attention4Args& a, const Plan& p, dim3 grid, hipStream_t stream) {
     if (p.tile_rows == 16)
-        hipLaunchKernelGGL((stream4_kernel<BF16, DP, 1>), grid, dim3(64 * stream4_waves(DP, 1)), 0, stream, a, p);
-    else if (p.tile_rows == 32)
-        hipLaunchKernelGGL((stream4_kernel<BF16, DP, 2>), grid, dim3(64 * stream4_waves(DP, 2)), 0, stream, a, p);
-    else if constexpr (BF16 && DP <= 128)
-        hipLaunchKernelGGL((stream4_kernel<BF16, DP, 4>), grid, dim3(64 * stream4_waves(DP, 4)), 0, stream, a, p);
+        hipLaunchKernelGGL((stream4_kernel<BF16, DP, 1>), grid, dim3(64 * kWaves4), 0, stream, a, p);
+    else
+        hipLaunchKernelGGL((stream4_kernel<BF16, DP, 2>), grid, dim3(64 * kWaves4), 0, stream, a, p);
 }
 
 template <int DP>

@@ -108,6 +108,7 @@ template <int NT, int ROWS>
 struct StreamShared {
     float m[NT / 64][ROWS], l[NT / 64][ROWS], top[ROWS], sum[ROWS];
     int units[NT + 1], wave[NT / 64], longest[NT / 64];
+    int parts[3];  // aligned: workgroups before the item's, its own, and all
     Seq seq[NT];  // of the items, while there are no more than threads
     int chunk, last;
 };
@@ -116,7 +117,8 @@ struct StreamShared {
 // begin at `before`.
 struct Stretch {
     int items, each, u0, u1, item, before;
-    bool whole_items;
+    bool whole_items;  // (or aligned: stretches end where items end)
+    int first, parts;  // aligned: the item's first workgroup and its workgroups
     Division cut;
     template <class Shared>
     __device__ int start(const Shared& sh, int w) const {
@@ -125,8 +127,8 @@ struct Stretch {
 };
 
 // Workgroup wg's stretch, an empty one (u0 == u1) where there is none.  Lengths are known on the device alone, so each
-// workgroup scans them.
-template <int NT, int ROWS>
+// workgroup scans them.  SLACK > 0: stretches of one length that end where an item ends, where aligned_length says so.
+template <int SLACK, int NT, int ROWS>
 __device__ __forceinline__ Stretch find_stretch(const AttentionArgs& a, const Plan& p, StreamShared<NT, ROWS>& sh, int wg,
                                                 int least_units) {
     constexpr int NW = NT / 64;
@@ -167,8 +169,53 @@ __device__ __forceinline__ Stretch find_stretch(const AttentionArgs& a, const Pl
     const int units = uniform(sh.units[NT]);
     // While no item is much longer than a stretch, each workgroup takes one item whole and none is joined.
     const Division cut = divide(units, p.wgs, least_units);
-    const bool whole_items = each == 1 && items <= p.wgs && uniform(longest) <= units / p.wgs + 1 + least_units;
+    const bool whole_items = SLACK == 0 && each == 1 && items <= p.wgs && uniform(longest) <= units / p.wgs + 1 + least_units;
     Stretch st;
+    st.first = st.parts = 0;
+    if constexpr (SLACK > 0) {
+        const int most = uniform(longest);
+        const int length = each == 1 ? aligned_length(units, items, most, p.wgs, least_units, SLACK) : 0;
+        if (length > 0) {
+            st.items = items;
+            st.each = 1;
+            st.whole_items = true;
+            st.cut = cut;
+            st.u0 = st.u1 = st.item = st.before = 0;
+            if (most <= length) {  // an item each
+                if (wg >= items) return st;
+                st.item = wg;
+                st.before = st.u0 = uniform(sh.units[wg]);
+                st.u1 = uniform(sh.units[wg + 1]);
+                return st;
+            }
+            // workgroups before each item, by a scan as above
+            const int mine = tid < items ? aligned_parts(sh.units[tid + 1] - sh.units[tid], length) : 0;
+            int upto = mine;
+#pragma unroll
+            for (int k = 1; k < 64; k <<= 1) {
+                const int below = __shfl_up(upto, k);
+                if (lane >= k) upto += below;
+            }
+            if (lane == 63) sh.wave[wave] = upto;
+            __syncthreads();
+            for (int w = 0; w < wave; ++w) upto += sh.wave[w];
+            if (upto - mine <= wg && wg < upto) {
+                sh.chunk = tid;
+                sh.parts[0] = upto - mine;
+                sh.parts[1] = mine;
+            }
+            if (tid == NT - 1) sh.parts[2] = upto;
+            __syncthreads();
+            if (wg >= uniform(sh.parts[2])) return st;
+            st.item = uniform(sh.chunk);
+            st.first = uniform(sh.parts[0]);
+            st.parts = uniform(sh.parts[1]);
+            st.before = uniform(sh.units[st.item]);
+            st.u0 = st.before + (wg - st.first) * length;
+            st.u1 = min(st.u0 + length, uniform(sh.units[st.item + 1]));
+            return st;
+        }
+    }
     st.items = items;
     st.each = each;
     st.whole_items = whole_items;
@@ -195,7 +242,8 @@ struct Item {
 
 // Joins the waves' outputs o, maxima m and sums l of an item, and the parts of one that is cut; writes the rows.  A part is
 // left in the workspace, and the workgroup that leaves last joins them, in the order of the parts.
-template <bool BF16, int DP, int RB, int NT>
+// AHEAD: parts whose outputs are in flight together.
+template <bool BF16, int DP, int RB, int NT, int AHEAD = 2>
 __device__ __forceinline__ void finish_item(const AttentionArgs& a, const Plan& p, StreamShared<NT, 16 * RB>& sh, char* s_mem,
                                             const Stretch& st, const Item& it, int wg, int g, f32x4 (&o)[RB][DP / 16], float (&m)[RB],
                                             float (&l)[RB]) {
@@ -255,7 +303,9 @@ __device__ __forceinline__ void finish_item(const AttentionArgs& a, const Plan& 
     if (it.from != it.before || it.to != it.before + it.n_units) {
         // A part of an item.  What a workgroup leaves of an item that its stretch begins with goes to
         // its first slot, of one that begins later to its second.
-        const int w_first = st.cut.owner(it.before), n_parts = st.cut.owner(it.before + it.n_units - 1) - w_first + 1;
+        const bool aligned = st.parts > 0;
+        const int w_first = aligned ? st.first : st.cut.owner(it.before);
+        const int n_parts = aligned ? st.parts : st.cut.owner(it.before + it.n_units - 1) - w_first + 1;
         float* dst = slot_of(wg, it.from == st.u0 ? 0 : 1);
 #pragma unroll
         for (int i = 0; i < NP; ++i) leave2(dst + (i * NT + et) * 2, y[i].x, y[i].y);
@@ -271,20 +321,43 @@ __device__ __forceinline__ void finish_item(const AttentionArgs& a, const Plan& 
         }
         __syncthreads();
         if (!sh.last) return;  // sh.last is written again two barriers later at the earliest
-        // the parts' common maximum and sum of each row, then their outputs, kBatch parts at a time
+        // The parts' common maximum and sum of each row, then their outputs, kBatch parts at a time.  The first AHEAD parts'
+        // outputs set out before the maxima are known, each later one as one is added.
         constexpr int kSubs = NT / ROWS, kBatch = 2048 / ROWS;
-        float* s_red = (float*)s_mem;         // [kSubs][ROWS][2]
-        float* s_fac = s_red + 2 * NT;  // [kBatch][ROWS]: the parts' factors
-        const int first_slot = it.before == st.start(sh, w_first) ? 0 : 1;
+        static_assert(kBatch % AHEAD == 0, "a part's registers follow from its place in a batch");
+        float* s_red = (float*)s_mem;   // [kSubs][ROWS][2]
+        float* s_fac = s_red + 2 * NT;  // [kBatch][ROWS]: the parts' maxima, then factors
+        const int first_slot = aligned || it.before == st.start(sh, w_first) ? 0 : 1;
         auto part_slot = [&](int k) { return slot_of(w_first + k, k == 0 ? first_slot : 0); };
+        float2 x[AHEAD][NP];
+        auto fetch = [&](int k, float2 (&into)[NP]) {
+            const float* src = part_slot(min(k, n_parts - 1)) + 2 * et;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) into[i] = fetch2(src + 2 * i * NT);
+        };
         const int row = et % ROWS;
         float mm = kNoScore, ll = 0.f;
-        for (int k = et / ROWS; k < n_parts; k += kSubs) {
-            const float2 x = fetch2(part_slot(k) + ROWS * DP + 2 * row);
-            const float up = fmaxf(mm, x.x);
-            ll = add_sums(ll, mm, x.y, x.x, up);
-            mm = up;
+        constexpr int kLoads = 4;
+        for (int k0 = et / ROWS; k0 < n_parts; k0 += kLoads * kSubs) {
+            float2 ml[kLoads];
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) ml[i] = fetch2(part_slot(min(k0 + i * kSubs, n_parts - 1)) + ROWS * DP + 2 * row);
+            if (k0 == et / ROWS)
+#pragma unroll
+                for (int n = 0; n < AHEAD; ++n) fetch(n, x[n]);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int k = k0 + i * kSubs;
+                if (k >= n_parts) break;
+                const float up = fmaxf(mm, ml[i].x);
+                ll = add_sums(ll, mm, ml[i].y, ml[i].x, up);
+                mm = up;
+                if (k < kBatch) s_fac[k * ROWS + row] = ml[i].x;
+            }
         }
+        if (et / ROWS >= n_parts)
+#pragma unroll
+            for (int n = 0; n < AHEAD; ++n) fetch(n, x[n]);
         s_red[2 * et] = mm;
         s_red[2 * et + 1] = ll;
         __syncthreads();
@@ -304,28 +377,22 @@ __device__ __forceinline__ void finish_item(const AttentionArgs& a, const Plan& 
         for (int k0 = 0; k0 < n_parts; k0 += kBatch) {
             const int nk = min(kBatch, n_parts - k0);
             for (int i = et; i < nk * ROWS; i += NT) {
-                const float pm = fetch2(part_slot(k0 + i / ROWS) + ROWS * DP + 2 * (i % ROWS)).x;
+                const float pm = k0 == 0 ? s_fac[i] : fetch2(part_slot(k0 + i / ROWS) + ROWS * DP + 2 * (i % ROWS)).x;
                 s_fac[i] = pm == kNoScore ? 0.f : exp2_hw(pm - sh.top[i % ROWS]);
             }
             __syncthreads();
-            // all of a part's loads set out before one is waited for, and the next part's before this one is added
-            float2 x[NP], x_next[NP];
-            auto fetch = [&](int k, float2 (&into)[NP]) {
-                const float* src = part_slot(k0 + k) + 2 * et;
+            for (int k = 0; k < nk; k += AHEAD)
 #pragma unroll
-                for (int i = 0; i < NP; ++i) into[i] = fetch2(src + 2 * i * NT);
-            };
-            fetch(0, x);
-            for (int k = 0; k < nk; ++k) {
-                fetch(min(k + 1, nk - 1), x_next);
+                for (int n = 0; n < AHEAD; ++n) {
+                    if (k + n >= nk) break;
 #pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    const float f = s_fac[k * ROWS + (i * NT + et) * 2 / DP];
-                    y[i].x += x[i].x * f;
-                    y[i].y += x[i].y * f;
-                    x[i] = x_next[i];
+                    for (int i = 0; i < NP; ++i) {
+                        const float f = s_fac[(k + n) * ROWS + (i * NT + et) * 2 / DP];
+                        y[i].x += x[n][i].x * f;
+                        y[i].y += x[n][i].y * f;
+                    }
+                    fetch(k0 + k + n + AHEAD, x[n]);
                 }
-            }
             __syncthreads();
         }
     }

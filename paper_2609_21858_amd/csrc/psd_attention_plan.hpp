@@ -77,12 +77,16 @@ constexpr int kUnit = 128;  // cached tokens: a block of each wave (two in float
 // joins pay from one on (37 tokens of 12 heads 38 us, with 4 units 49).
 constexpr int join_units(bool bf16) { return bf16 ? 4 : 1; }
 
+// The same over a cache held in 4 bits.
+constexpr int join_units4(bool bf16) { return bf16 ? 4 : 1; }
+
 // Threads of the few-row kernel: one workgroup a CU, two waves a SIMD, or one where the rows' outputs take
 // the registers of two.
 constexpr int stream_waves(int DP, int RB) { return RB * DP >= 512 || DP == 256 ? 4 : 8; }
 
-// The same over a cache held in 4 bits, where the converted values and the wider blocks take more LDS and registers.
-constexpr int stream4_waves(int DP, int RB) { return RB * DP >= 256 ? 4 : 8; }
+// The same over a cache held in 4 bits: workgroups of four waves, two of them a CU where the registers allow.
+constexpr int kWaves4 = 4;
+constexpr int stream4_resident(int DP, int RB) { return RB * DP >= 256 ? 1 : 2; }
 
 struct Range {
     int lo, hi;  // cached positions that some row of a tile sees
@@ -139,6 +143,21 @@ PSD_HOST_DEVICE Division divide(int units, int wgs, int least_units) {
     return d;
 }
 
+// Over a cache held in 4 bits, where there are workgroups to spare: the length of stretches that end where items
+// end, or 0 for stretches that do not.  A workgroup that goes on to a second item starts a chain of its own (places, first
+// keys, join: 8 us) that takes as long as about 6 units more of bfloat16 rows of 128 dimensions, a join as long as 8: 4 sequences
+// of up to 1000 tokens 13 us, with stretches across sequences 19; 16 of them 14 and 23.
+constexpr int slack4(bool bf16, int DP) { return (bf16 ? 1024 : 512) / DP + 1; }
+PSD_HOST_DEVICE int aligned_parts(int n_units, int length) { return (n_units + length - 1) / length; }
+PSD_HOST_DEVICE int aligned_length(int units, int items, int longest, int wgs, int least_units, int slack) {
+    if (units == 0 || items > wgs) return 0;
+    const int share = units / wgs;
+    if (longest <= share + slack) return longest;
+    if (items == wgs) return 0;
+    const int length = greater((units + wgs - items - 1) / (wgs - items), least_units);  // the sum of parts stays inside wgs
+    return length <= share + 2 * slack / 3 ? length : 0;
+}
+
 // Does a workgroup whose stretch begins at unit u0 work on an item that begins at unit `before`, below the
 // stretch's end?  An item without units has no rows, wherever it lies.
 PSD_HOST_DEVICE bool works_on(int before, int n_units, int u0) { return n_units > 0 && before + n_units > u0; }
@@ -152,6 +171,21 @@ constexpr double kWide = 0.9;
 constexpr int kCus = 256;
 
 inline int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
+
+// Over a cache held in 4 bits: are `most` rows of a sequence (at most 32) better off in tile_kernel?  Its time grows faster by
+// 44 us for 2^20 tokens of all heads of 128 dimensions (30 for 32 rows), the other's with the parts that one workgroup joins of
+// a long item, 0.25 us each (0.33 of 32 rows; half as much again for heads of 256).  us there and here:
+// D=128, G=8, 4 rows, 2 x 8000 24 and 19, 1 x 32768 44 and 29, 8 x 1500 15 and 17, 16 x 4096 24 and 41, 1 x 131072 58 and 76; 20 rows,
+// 2 x 8000 33 and 20, 1 x 32768 39 and 29, 16 x 4096 33 and 43; D=64, 4 rows, 2 x 8000 21 and 14, 64 x 1024 15 and 28; D=256, G=4,
+// 4 rows, 2 x 8000 34 and 26, 16 x 4096 30 and 60; G=1, 32 rows, 1 x 131072 140 and 61.  More than 32 rows: 48 rows, 64 x 1024 67 and 44,
+// 1 x 131072 124 and 86, 64 rows of 16 sequences, up to 8192 86 and 85.
+inline bool tiles4(const CacheArgs& c, long most, long span) {
+    const int rb = most <= 16 ? 1 : 2, DP = padded(c.D), wgs = std::max(kCus * stream4_resident(DP, rb) / c.G, 1);
+    const long parts = std::min<long>(wgs / c.B, span / kUnit / join_units4(true));
+    const double tokens = (double)c.B * c.G * span * std::max(c.D, 64) / 128 / (1 << 20);
+    if (parts < 2) return false;
+    return (rb == 2 && DP == 128 ? 30 : 44) * tokens < (rb == 1 ? 0.25 * parts : 0.2 + 0.33 * parts) * (DP == 256 ? 1.5 : 1.);
+}
 
 inline Plan make_plan(const CacheArgs& c, int H, bool bf16, int span, bool q4 = false) {
     Plan p;
@@ -171,17 +205,21 @@ inline Plan make_plan(const CacheArgs& c, int H, bool bf16, int span, bool q4 = 
     const long tokens = (long)c.B * c.G * span * (c.D > 128 ? 4 : 1);
     const long units = (span + kUnit - 1) / kUnit;
     const bool alone = (long)c.B * c.G <= kCus && units <= units * c.B * c.G / kCus + 5;
-    p.many = bf16 && (most > 64 || (most > 32 ? tokens <= 1 << 20 : tokens <= 1 << 19 && !alone));
+    p.many = bf16 && (most > 64 || (most > 32 ? q4 || tokens <= 1 << 20 : q4 ? tiles4(c, most, span) : tokens <= 1 << 19 && !alone));
     p.wgs = p.parts = p.chunk = 0;
     if (!p.many) {
         // float32 rows in tiles of 32 while tiles of 64 would leave CUs without one (12 heads of 80, 37 tokens
         // of 6 sequences: 40 us and 45; 1024 new of 4096 tokens of 16 heads, CUs full: 450 and 408)
         const bool few = !bf16 && c.D > 64 && (long)c.B * c.G * ((most + 63) / 64) < kCus;
-        // (4 bits: float32 queries as three terms leave registers for 32)
-        const int limit = c.D > 128 || few || (q4 && !bf16) ? 32 : 64;
+        const int limit = c.D > 128 || few || q4 ? 32 : 64;  // (4 bits: bfloat16 rows are no more, float32 ones spill)
         p.tile_rows = most <= 16 ? 16 : most <= 32 ? 32 : limit;
         p.tiles = (int)((most + p.tile_rows - 1) / p.tile_rows);
-        p.wgs = std::max(kCus / c.G, 1);  // one a CU
+        const int resident = q4 ? stream4_resident(padded(c.D), p.tile_rows / 16) : 1;
+        p.wgs = std::max(kCus * resident / c.G, 1);  // on every CU
+        // (4 bits: no more than the bounds have work for, which the division would send home: 4 sequences of up to 512 tokens
+        // 8.9 us, with 512 workgroups 10.1)
+        const long items = (long)c.B * p.tiles;
+        if (q4) p.wgs = (int)std::min<long>(p.wgs, items * ((span + kUnit * join_units4(bf16) - 1) / (kUnit * join_units4(bf16))));
     } else {
         // Rows of a workgroup and parts of the longest range, by the time they take in 64-token blocks:
         // every round of resident workgroups takes a part and about 3 blocks to start and end; the join of
