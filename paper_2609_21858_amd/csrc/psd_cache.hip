@@ -35,6 +35,16 @@ typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 __host__ __device__ __forceinline__ const AppendArgs& rows_of(const AppendArgs& a) { return a; }
 __host__ __device__ __forceinline__ const AppendArgs& rows_of(const Append4Args& a) { return a.a; }
 
+// 1 / sqrt(x) within a few 2^-53: the hardware's estimate (about 2^-26) and two Newton steps, a fifth of the instructions of
+// a square root and a division.  Of 0, infinity and NaN the estimate is the answer.
+__device__ __forceinline__ double rsqrt64(double x) {
+    const double r0 = __builtin_amdgcn_rsq(x);
+    double r = r0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r = __builtin_fma(0.5 * r, __builtin_fma(-x * r, r, 1.), r);
+    return x > 0. && x < (double)__builtin_inf() ? r : r0;
+}
+
 // One piece of N heads at once.
 template <int N>
 struct Heads {
@@ -57,7 +67,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(std::conditional
     const AppendArgs& a = rows_of(args);
     using E = Elem<BF16>;
     constexpr int VEC = E::kVec;
-    constexpr int NQ = 4, NK = 2;  // heads of a thread whose loads are in flight together: queries; keys, values
+    // heads of a thread whose loads are in flight together: queries; keys, values (Q4: registers for four waves a SIMD)
+    constexpr int NQ = 4, NK = Q4 && TURN != kAnywhere ? 1 : 2;
     __shared__ float s_x[TURN == kAnywhere ? VEC : 1][kAppendThreads];
     const CacheArgs& c = a.c;
     const int tid = threadIdx.x;
@@ -149,6 +160,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(std::conditional
     }
 
     const float inv_d = 1.f / (float)c.D;
+    const double inv_d64 = 1. / (double)c.D;
     // Queries or keys, in the arithmetic of `zero`'s type; each head's elements go to `emit`.
     auto turn = [&](auto zero, auto& w, const RowsArgs& r, int heads, const void* norm, auto emit) {
         using T = decltype(zero);
@@ -205,7 +217,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(std::conditional
                     if constexpr (sizeof(T) == 4)
                         scale = rsqrtf(sum * inv_d + a.eps);
                     else
-                        scale = 1 / sqrt(sum / c.D + a.eps);
+                        scale = rsqrt64(sum * inv_d64 + a.eps);
                 }
                 if constexpr (TURN == kPieces) {
                     E::widen(w.other[k], y);

@@ -42,15 +42,32 @@ __device__ __forceinline__ int scale_of(const double (&z)[N]) {
     return min(max(k, -126) + 127, kMost);
 }
 
-__device__ __forceinline__ float narrowed(float x) { return x; }
-// The float next to x towards zero, with its last bit set where that is not x: rounding it again to fewer bits
-// gives what rounding x gives.
-__device__ __forceinline__ float narrowed(double x) {
-    const float f = (float)x;
-    const double back = f;
-    uint32_t w = __float_as_uint(f);
-    if (back != x) w = (fabs(back) > fabs(x) ? w - 1 : w) | 1u;
-    return __uint_as_float(w);
+// Elements as floats that round to the codes that the elements round to.
+template <int N>
+__device__ __forceinline__ void narrowed(const float (&z)[N], float (&f)[N]) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[j] = z[j];
+}
+// Rounding to float moves an element past no border between codes, but may move it onto one, where all bits of the
+// mantissa but the upper two are 0.  Where a float of the wave looks like that, each is taken next to its element towards zero,
+// with the last bit set where it is not the element itself: rounding it again gives what rounding the element gives.
+template <int N>
+__device__ __forceinline__ void narrowed(const double (&z)[N], float (&f)[N]) {
+    uint32_t least = ~0u;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        f[j] = (float)z[j];
+        least = min(least, __float_as_uint(f[j]) & 0x1FFFFFu);
+    }
+    if (__any(least == 0)) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const double back = f[j];
+            uint32_t w = __float_as_uint(f[j]);
+            if (back != z[j]) w = (fabs(back) > fabs(z[j]) ? w - 1 : w) | 1u;
+            f[j] = __uint_as_float(w);
+        }
+    }
 }
 
 __device__ __forceinline__ float scale_value(int s) { return __uint_as_float((uint32_t)s << 23); }
@@ -60,12 +77,14 @@ template <class T, int N>
 __device__ __forceinline__ uint32_t encode(const T (&z)[N], int s) {
     static_assert(N == 8 || N == 4, "pieces of 16 bytes");
     const float by = scale_value(s);
+    float f[N];
+    narrowed(z, f);
     uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, narrowed(z[0]), narrowed(z[1]), by, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, narrowed(z[2]), narrowed(z[3]), by, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[0], f[1], by, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[2], f[3], by, 1);
     if constexpr (N == 8) {
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, narrowed(z[4]), narrowed(z[5]), by, 2);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, narrowed(z[6]), narrowed(z[7]), by, 3);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[4], f[5], by, 2);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[6], f[7], by, 3);
     }
     return s == kNan ? 0 : w;
 }

@@ -749,26 +749,21 @@ def kv_reserve(pages: Pages, seqs: Seqs, n_new, kv_have, held, granted=None, row
     held (int32 [B]) and the tensors that `seqs` was made of (new_start, kv_len, table) are written, pages come from
     and go back to `pages`.  Returns {"granted" int32 [B]}, and with rows_out "row_seq", "positions" int32 [rows] and "slots"
     int64 [rows] (allocated where `out` does not hold them)."""
-    new_start, kv_len, table = seqs.tensors
     B, T = seqs.batch, seqs.rows
-    for x, what in ((n_new, "n_new"), (kv_have, "kv_have"), (held, "held")):
-        _ints(x, what, 1)
-        if x.shape[0] != B:
-            _refuse(f"{what}: int32 [{B}]")
+    if not (n_new.dtype == kv_have.dtype == held.dtype == torch.int32 and n_new.shape == kv_have.shape == held.shape == (B,)
+            and n_new.is_contiguous() and kv_have.is_contiguous() and held.is_contiguous()):
+        _refuse(f"n_new, kv_have and held: contiguous int32 [{B}]")
     o = {} if out is None else dict(out)
     if granted is not None:
         o["granted"] = granted
-    dev = n_new.device
-    names = (("granted", B, torch.int32),)
-    if rows_out:
-        names += (("row_seq", T, torch.int32), ("positions", T, torch.int32), ("slots", T, torch.int64))
-    for name, n, dt in names:
-        if name not in o:
-            o[name] = torch.empty((n,), dtype=dt, device=dev)
-        elif o[name].shape != (n,) or o[name].dtype != dt or not o[name].is_contiguous():
+    for name, n, dt in (("granted", B, torch.int32), ("row_seq", T, torch.int32), ("positions", T, torch.int32), ("slots", T, torch.int64)):
+        t = o.get(name)
+        if t is None:
+            if rows_out or name == "granted":
+                o[name] = n_new.new_empty(n, dtype=dt)
+        elif t.shape != (n,) or t.dtype != dt or not t.is_contiguous():
             _refuse(f"{name}: contiguous {dt} [{n}]")
-    r = Reservation(n_new.data_ptr(), kv_have.data_ptr(), held.data_ptr(), seqs.table, seqs.new_start, seqs.kv_len,
-                    o["granted"].data_ptr())
+    r = Reservation(n_new.data_ptr(), kv_have.data_ptr(), held.data_ptr(), seqs.table, seqs.new_start, seqs.kv_len, o["granted"].data_ptr())
     if rows_out:
         r.row_seq, r.positions, r.slots = o["row_seq"].data_ptr(), o["positions"].data_ptr(), o["slots"].data_ptr()
     _check(_lib.psd_kv_reserve(ctypes.byref(pages), ctypes.byref(seqs), ctypes.byref(r), _stream(stream)))
