@@ -4,11 +4,12 @@ A small attention model with random weights stands for the target, a table of ne
 for the drafter.  One block:
 
 1. the drafter proposes gamma tokens on each of K paths (psd.draft, or tokens of its own rows);
-2. the target scores the root and every path in one pass: psd.kv_append puts the new keys (normed,
-   turned by their position) and values into the paged cache, psd.attention lets each row see the
-   cache and its own path;
-3. psd.verify races target and drafts under the key (K paths), or psd.verify_given accepts and
-   rejects from given random numbers (one path);
+2. the target scores the root and every path in one pass: psd.kv_reserve finds pages for the new tokens and
+   takes back those that the last block's refused drafts held, psd.kv_append puts the new keys (normed,
+   turned by their position) and values into the paged cache (16 bits an element, or 4), psd.attention
+   lets each row see the cache and its own path;
+3. psd.adjust_logits (one path) takes penalties for repeated tokens into the logits; psd.verify races target
+   and drafts under the key (K paths), or psd.verify_given accepts and rejects from given random numbers (one path);
 4. psd.kv_keep moves the accepted path's keys and values behind the cache, psd.advance commits
    the tokens.
 
@@ -33,7 +34,7 @@ DEV = "cuda"
 class Target:
     """Layers of attention over a paged cache, without the rest of a real model."""
 
-    def __init__(self, vocab=500, layers=2, heads=8, kv_heads=2, dim=64, page=16, pages=512, dtype=torch.float32, seed=0):
+    def __init__(self, vocab=500, layers=2, heads=8, kv_heads=2, dim=64, page=16, pages=512, dtype=torch.float32, seed=0, bits=16):
         g = torch.Generator(device=DEV).manual_seed(seed)
         self.width = heads * dim
         self.heads, self.kv_heads, self.dim, self.dtype = heads, kv_heads, dim, dtype
@@ -48,10 +49,15 @@ class Target:
         self.norm = torch.ones(dim, device=DEV, dtype=dtype)
         angle = torch.arange(4096, device=DEV)[:, None] * 10000.0 ** (-torch.arange(dim // 2, device=DEV) * 2.0 / dim)
         self.cos, self.sin = angle.cos(), angle.sin()
-        shape = (layers, pages, page, kv_heads, dim)
-        self.k, self.v = torch.empty(shape, device=DEV, dtype=dtype), torch.empty(shape, device=DEV, dtype=dtype)
-        self.cache = [psd.make_cache(self.k[i], self.v[i]) for i in range(layers)]
-        self.all_layers = psd.make_cache(self.k, self.v)
+        self.page, self.pages = page, pages
+        if bits == 4:
+            self.all_layers = psd.new_cache4(pages, page, kv_heads, dim, layers, dtype, DEV)
+            self.cache = [psd.layer(self.all_layers, i) for i in range(layers)]
+        else:
+            shape = (layers, pages, page, kv_heads, dim)
+            self.k, self.v = torch.empty(shape, device=DEV, dtype=dtype), torch.empty(shape, device=DEV, dtype=dtype)
+            self.cache = [psd.make_cache(self.k[i], self.v[i]) for i in range(layers)]
+            self.all_layers = psd.make_cache(self.k, self.v)
         self.ws = {}
 
     def workspace(self, seqs):
@@ -100,25 +106,28 @@ class Loop:
         self.start = torch.empty((B,), dtype=torch.int64, device=DEV)
         self.prefix = torch.empty((B, params.ctx_window), dtype=torch.int32, device=DEV)
         self.active = torch.empty((1,), dtype=torch.int32, device=DEV)
-        page = target.k.shape[2]
-        width = -(-(max_len + n_new) // page)
-        self.table = torch.arange(B * width, dtype=torch.int32, device=DEV).flip(0).view(B, width).contiguous()
-        self.kv_len = torch.empty((B,), dtype=torch.int32, device=DEV)
+        width = -(-(max_len + n_new) // target.page)
+        self.pages = psd.new_pages(target.pages, target.page, DEV)
+        self.table = torch.full((B, width), -1, dtype=torch.int32, device=DEV)
+        self.held, self.have = (torch.zeros((B,), dtype=torch.int32, device=DEV) for _ in range(2))
+        self.asked = torch.full((B,), n_new, dtype=torch.int32, device=DEV)
         self.seqs = self.sequences(n_new, max_len + n_new)
         # the prompts' keys and values, all but the last token's: it is the first block's root
         if m > 1:
-            self.kv_len.fill_(m - 1)
-            target(prompts[:, :-1].reshape(-1), self.sequences(m - 1, m))
+            seqs = self.sequences(m - 1, m)
+            psd.kv_reserve(self.pages, seqs, torch.full_like(self.asked, m - 1), self.have, self.held)
+            target(prompts[:, :-1].reshape(-1), seqs)
         psd.advance(params, gamma, max_len, self.text, self.length, self.prefix, self.start, self.active)
 
     def sequences(self, n, max_kv):
-        first = torch.arange(self.B + 1, dtype=torch.int32, device=DEV) * n
-        return psd.make_seqs(first, self.kv_len, self.table, self.B * n, n, max_kv)
+        start = torch.zeros((self.B + 1,), dtype=torch.int32, device=DEV)
+        return psd.make_seqs(start, torch.zeros_like(self.asked), self.table, self.B * n, n, max_kv)
 
     def score(self, drafts, mask, depth):
         """Target logits [B][n][V] of the root and the drafts [B][n - 1]."""
         root = self.text.gather(1, (self.start - 1)[:, None])
-        self.kv_len.copy_(self.start - 1 + self.n)
+        self.have.copy_(self.start - 1)
+        psd.kv_reserve(self.pages, self.seqs, self.asked, self.have, self.held)
         positions = ((self.start - 1)[:, None] + depth).to(torch.int32).view(-1).contiguous()
         logits = self.target(torch.cat((root, drafts), 1).view(-1), self.seqs, positions, mask)
         return logits.view(self.B, self.n, -1)
@@ -163,13 +172,15 @@ def keyed(target, drafter, prompts, max_len, key=7, K=4, gamma=4):
             return loop.text, committed / (blocks * B)
 
 
-def given(target, drafter, prompts, max_len, seed=0, gamma=4):
-    """One path, accepted and rejected from given random numbers.  Returns as keyed()."""
+def given(target, drafter, prompts, max_len, seed=0, gamma=4, presence=0.0):
+    """One path, accepted and rejected from given random numbers; `presence` is taken off the logits of every token that
+    the text (or the drafts before a row) has.  Returns as keyed()."""
     B, m = prompts.shape
     V = target.embed.shape[0]
     params = psd.make_params(0, V, 1, m, 1.0, 1.0, dtype=target.dtype)
     ws = psd.new_verify_given_workspace(params, B, gamma)
     loop = Loop(target, prompts, max_len, 1 + gamma, params, gamma)
+    presence = torch.full((B,), presence, device=DEV)
     g = torch.Generator(device=DEV).manual_seed(seed)
     depth = torch.arange(gamma + 1, device=DEV)
     blocks = 0
@@ -183,9 +194,11 @@ def given(target, drafter, prompts, max_len, seed=0, gamma=4):
             last = torch.multinomial(torch.softmax(rows[:, s].float(), -1), 1, generator=g)[:, 0].to(torch.int32)
             drafts[:, s] = last
         logits = loop.score(drafts, None, depth)
+        logits = psd.adjust_logits(params, logits.contiguous(), text=loop.text, length=loop.length, draft_tokens=drafts[:, None],
+                                   presence=presence)
         u = torch.rand((B, gamma), device=DEV, generator=g)
         e = torch.empty((B, V), device=DEV).exponential_(generator=g).clamp_(min=1e-30)
-        out = psd.verify_given(params, ws, logits.contiguous(), rows, drafts, u, e)
+        out = psd.verify_given(params, ws, logits, rows, drafts, u, e)
         committed += int(out["out_len"].sum())
         loop.commit(out, depth.expand(B, -1))
         blocks += 1
@@ -209,6 +222,9 @@ def main():
           f"same text: {bool(torch.equal(a, b))}")
     _, rate = given(target, good, prompts, 100)
     print(f"given random numbers, 1 path: {rate:.2f} tokens a block")
+    text, rate = given(Target(bits=4), good, prompts, 100, presence=2.0)
+    new = [len(set(row)) for row in text.tolist()]
+    print(f"a cache in 4 bits, 2 off repeated tokens: {rate:.2f} tokens a block, {min(new)} to {max(new)} different tokens in 100")
 
 
 if __name__ == "__main__":

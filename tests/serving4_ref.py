@@ -9,14 +9,6 @@ import serving_ref as ref
 LEVELS = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]
 
 
-def scale_exponent(top):
-    """The least k in [-126, 125] with top <= 7 * 2^k, exactly; 125 where there is none."""
-    if top == 0:
-        return -126
-    m, e = math.frexp(top)          # top = m 2^e, 0.5 <= m < 1
-    return min(max(e - 3 if m <= 0.875 else e - 2, -126), 125)
-
-
 def encode(x, near=None, computed=None):
     """Codes [..., 16 n] and scale bytes [..., n] (uint8) of x [..., D] float64, n = ceil(D / 32).  near: a relative
     distance; the third result then says which groups have one of the first `computed` elements as near to a border of two
@@ -25,32 +17,26 @@ def encode(x, near=None, computed=None):
     D = x.shape[-1]
     computed = D if computed is None else computed
     n = -(-D // 32)
-    x = torch.nn.functional.pad(x, (0, 32 * n - D)).reshape(x.shape[:-1] + (n, 32))
-    flat = x.reshape(-1, 32)
-    codes = torch.zeros((flat.shape[0], 16), dtype=torch.uint8)
-    scales = torch.zeros((flat.shape[0],), dtype=torch.uint8)
-    close = torch.zeros((flat.shape[0],), dtype=torch.bool)
-    borders = torch.tensor([(a + b) / 2 for a, b in zip(LEVELS, LEVELS[1:])], dtype=torch.float64)
-    odd_above = torch.tensor([i % 2 == 0 for i in range(7)])  # the border belongs to the even code: the lower one if that is even
-    top = flat.abs().amax(-1)
-    for i in range(flat.shape[0]):
-        t = float(top[i])
-        if not math.isfinite(t) or t >= 2.0 ** 128:
-            scales[i] = 255
-            continue
-        k = scale_exponent(t)
-        scales[i] = k + 127
-        a = flat[i].abs() * 2.0 ** -k
-        past = torch.where(odd_above, a[:, None] > borders, a[:, None] >= borders).sum(-1)
-        code = past + 8 * torch.signbit(flat[i]).long()
-        codes[i] = (code[0::2] + 16 * code[1::2]).to(torch.uint8)
-        if near is not None:
-            a = a[:max(0, computed - i % n * 32)]
-            ends = torch.tensor([3.5, 7.0], dtype=torch.float64)  # the scale changes past them
-            close[i] = any(bool(((a[:, None] - x).abs() <= near * x).any()) for x in (borders, ends))
-    lead = x.shape[:-2]
-    out = codes.reshape(lead + (16 * n,)), scales.reshape(lead + (n,))
-    return out if near is None else out + (close.reshape(lead + (n,)),)
+    g = torch.nn.functional.pad(x, (0, 32 * n - D)).unflatten(-1, (n, 32))
+    top = g.abs().amax(-1)
+    none = ~torch.isfinite(top) | (top >= 2.0 ** 128)
+    m, e = torch.frexp(torch.where(none, 1.0, top))  # top = m 2^e, 0.5 <= m < 1
+    # the least k in [-126, 125] with top <= 7 * 2^k, exactly; 125 where there is none
+    k = torch.where(top > 0, torch.where(m <= 0.875, e - 3, e - 2), -126).clamp(-126, 125)
+    a = torch.where(none[..., None], 0.0, g.abs()) * (2.0 ** -k.double())[..., None]
+    borders = torch.tensor([(p + q) / 2 for p, q in zip(LEVELS, LEVELS[1:])], dtype=torch.float64)
+    code = torch.where(none[..., None], 0, 8 * torch.signbit(g).long())
+    close = torch.zeros(top.shape, dtype=torch.bool)
+    given = torch.arange(32 * n).unflatten(0, (n, 32)) >= computed
+    for i, border in enumerate(borders):
+        # the border belongs to the even code: the lower one if that is even
+        code += (a > border) if i % 2 == 0 else (a >= border)
+    if near is not None:
+        for border in borders.tolist() + [3.5, 7.0]:  # (the scale changes past the last two)
+            close |= (((a - border).abs() <= near * border) & ~given).any(-1)
+    code = code.flatten(-2)
+    out = (code[..., 0::2] + 16 * code[..., 1::2]).to(torch.uint8), torch.where(none, 255, k + 127).to(torch.uint8)
+    return out if near is None else out + (close,)
 
 
 def decode(codes, scales, D):
