@@ -52,7 +52,7 @@ class Target:
         self.page, self.pages = page, pages
         if bits == 4:
             self.all_layers = psd.new_cache4(pages, page, kv_heads, dim, layers, dtype, DEV)
-            self.cache = [psd.layer(self.all_layers, i) for i in range(layers)]
+            self.cache = [psd.cache4_layer(self.all_layers, i) for i in range(layers)]
         else:
             shape = (layers, pages, page, kv_heads, dim)
             self.k, self.v = torch.empty(shape, device=DEV, dtype=dtype), torch.empty(shape, device=DEV, dtype=dtype)

@@ -549,7 +549,8 @@ typedef struct {
  * and turned in 64 bits before that, so that a key's code is its definition's; queries in float32
  * as in psd_kv_append.
  *   k_held, v_held  [T][G][D] (dtype), nullable: the values that the cache now holds for the new
- *                   keys and values (also of tokens that have no place) */
+ *                   keys and values (also of tokens that have no place); they may be k and v
+ *                   themselves */
 psd_status psd_kv_append4(const psd_cache4 *cache, const psd_seqs *seqs, const psd_rotation *rotation,
                           const psd_rows *k, const psd_rows *v, const psd_rows *q, const psd_rows *q_out,
                           int32_t q_heads, const psd_rows *k_held, const psd_rows *v_held, hipStream_t stream);
@@ -557,7 +558,7 @@ psd_status psd_kv_append4(const psd_cache4 *cache, const psd_seqs *seqs, const p
 /* psd_attention over the values that a 4-bit cache stands for: same rows, windows, masks, outputs
  * and workspace rules.  bfloat16 rows as there; float32 rows are computed to float32's precision:
  * queries and softmax weights as three bfloat16 terms each (24 bits), whose products with codes are
- * exact, summed in float32. */
+ * exact, summed in float32 (an infinite element of a float32 query gives its row NaN). */
 psd_status psd_attention4(const psd_cache4 *cache, const psd_seqs *seqs, const psd_rows *q, int32_t q_heads, float scale,
                           int32_t window, const uint32_t *mask, int32_t mask_words, const psd_rows *out, float *lse,
                           void *workspace, size_t workspace_bytes, hipStream_t stream);

@@ -27,6 +27,7 @@ constexpr float kGone = -__builtin_inff();
 // 16 bytes at any element boundary (rows of an odd vocabulary start off the 16-byte grid).
 typedef uint32_t u32x4_f32 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x4_b16 __attribute__((ext_vector_type(4), aligned(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4), aligned(4)));
 template <bool BF16>
 struct Piece;
 template <>
@@ -35,6 +36,15 @@ struct Piece<true> {
     typedef uint16_t one;
     __device__ static float widen1(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
     __device__ static uint16_t narrow1(float x) { return (uint16_t)pack_bf16(x, x); }
+    // -inf where a bit of `may` is 0
+    __device__ static u32x4 masked(u32x4 w, uint32_t may) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t keep = (may >> 2 * i & 1 ? 0xFFFFu : 0u) | (may >> (2 * i + 1) & 1 ? 0xFFFF0000u : 0u);
+            w[i] = (w[i] & keep) | (0xFF80FF80u & ~keep);
+        }
+        return w;
+    }
 };
 template <>
 struct Piece<false> {
@@ -42,6 +52,11 @@ struct Piece<false> {
     typedef float one;
     __device__ static float widen1(float x) { return x; }
     __device__ static float narrow1(float x) { return x; }
+    __device__ static u32x4 masked(u32x4 w, uint32_t may) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = may >> i & 1 ? w[i] : 0xFF800000u;
+        return w;
+    }
 };
 
 // One workgroup: a stretch of SEG tokens of rows [r0, r1) of a sequence.  A row's next pieces are on their way while
@@ -62,6 +77,36 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
     const int b = rest / groups, r0 = (rest - b * groups) * per, r1 = min(r0 + per, R);
     const int v0 = seg * SEG, v1 = min(v0 + SEG, a.V);
 
+    const bool same = a.out == a.logits;
+    constexpr int N = SEG / (kThreads * VEC);  // pieces of a thread in a row
+    const int64_t row0 = (int64_t)b * R * a.V;
+    const typename Pc::one* src0 = (const typename Pc::one*)a.logits + row0;
+    typename Pc::one* dst0 = (typename Pc::one*)a.out + row0;
+    auto at = [&](int n) { return v0 + (n * kThreads + tid) * VEC; };
+    u32x4 next[N];
+    uint32_t may_next[N];
+    bool here_next[N];  // in place: is the piece on its way?
+    constexpr uint32_t kEvery = (1u << VEC) - 1;
+    auto load = [&](int r) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int v = at(n);
+            may_next[n] = kEvery;
+            if (v >= v1) continue;
+            if (a.allowed) may_next[n] = a.allowed[b * a.allowed_seq + r * a.allowed_row + v / 32] >> (v % 32) & kEvery;
+            // in place: pieces that the text or a bias touches (those of a mask or a draft alone are read when they are due)
+            bool wanted = !same;
+            if (same) {
+#pragma unroll
+                for (int i = 0; i < VEC; i += 4) {
+                    const u32x4 w = *(const u32x4*)(s_word + v - v0 + i);
+                    wanted |= (w[0] | w[1] | w[2] | w[3]) != 0;
+                }
+                here_next[n] = wanted;
+            }
+            if (wanted && v + VEC <= a.V) next[n] = *(const typename Pc::any*)(src0 + (int64_t)r * a.V + v);
+        }
+    };
     for (int i = tid; i < SEG / 4; i += kThreads) ((u32x4*)s_word)[i] = u32x4{0, 0, 0, 0};
     __syncthreads();
     // the stretch's biases, in the order of the list
@@ -110,40 +155,42 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
         const int32_t* text = a.text + (int64_t)b * a.text_stride;
         const int to = (int)min(a.length[b], (int64_t)a.text_max);
         const int from = a.from ? (int)min(max(a.from[b], (int64_t)0), (int64_t)a.text_max) : 0;
-        for (int i = from + tid; i < to; i += kThreads) count(text[i], 1);
+        // four tokens a load, four loads in flight
+        int i = from + tid * 4;
+        for (; i + 3 * kThreads * 4 + 4 <= to; i += 4 * kThreads * 4) {
+            i32x4 v[4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) v[n] = *(const i32x4*)(text + i + n * kThreads * 4);
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) count(v[n][e], 1);
+        }
+        for (; i < to; i += kThreads * 4) {
+            int v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = i + e < to ? text[i + e] : -1;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) count(v[e], 1);
+        }
     }
     const int32_t* drafts = a.drafts ? a.drafts + (int64_t)b * a.K * a.gamma : nullptr;
     const float rho = a.repetition ? a.repetition[b] : 1.f;
     const float presence = a.presence ? a.presence[b] : 0.f, frequency = a.frequency ? a.frequency[b] : 0.f;
-    const bool same = a.out == a.logits;
-    auto value = [&](float l, uint32_t word, bool may) {
+    const float inverse = 1.f / rho;  // (a product where a quotient is meant: one rounding more)
+    // Without a branch for the tokens that came: a wave's pieces mostly have one.
+    auto penalized = [&](float l, uint32_t word) {
         const uint32_t c = word & kCount;
-        float z = l;
-        if (c > 0) z = (l > 0.f ? l / rho : l * rho) - (frequency * (float)c + presence);
+        const float z = l * (l > 0.f ? inverse : rho) - (frequency * (float)c + presence);
+        return c > 0 ? z : l;
+    };
+    auto biased = [&](float z, uint32_t word) {
         if (word & kBiased) z += s_bias[kMaxBias - 1 - (word >> 20 & 1023)];
-        return may ? z : kGone;
+        return z;
     };
-    constexpr int N = SEG / (kThreads * VEC);  // pieces of a thread in a row
-    const int64_t row0 = (int64_t)b * R * a.V;
-    const typename Pc::one* src0 = (const typename Pc::one*)a.logits + row0;
-    typename Pc::one* dst0 = (typename Pc::one*)a.out + row0;
-    auto at = [&](int n) { return v0 + (n * kThreads + tid) * VEC; };
-    u32x4 next[N];
-    uint32_t may_next[N];
-    constexpr uint32_t kEvery = (1u << VEC) - 1;
-    auto load = [&](int r) {
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const int v = at(n);
-            may_next[n] = kEvery;
-            if (v >= v1) continue;
-            if (!same && v + VEC <= a.V) next[n] = *(const typename Pc::any*)(src0 + (int64_t)r * a.V + v);
-            if (a.allowed) may_next[n] = a.allowed[b * a.allowed_seq + r * a.allowed_row + v / 32] >> (v % 32) & kEvery;
-        }
-    };
-    load(r0);
     int path = -1, depth = 0;  // the drafts that are counted: `path`'s before `depth`
     __syncthreads();
+    load(r0);
     for (int r = r0; r < r1; ++r) {
         if (drafts) {
             const int k = r / a.S, d = a.depth0 + r - k * a.S;
@@ -157,10 +204,12 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
         }
         u32x4 now[N];
         uint32_t may[N];
+        bool here[N];
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             now[n] = next[n];
             may[n] = may_next[n];
+            here[n] = here_next[n];
         }
         if (r + 1 < r1) load(r + 1);
         const typename Pc::one* src = src0 + (int64_t)r * a.V;
@@ -183,20 +232,25 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
             const bool touched = any != 0 || may[n] != kEvery;
             if (same && !touched) continue;
             if (v + VEC <= a.V) {
-                u32x4 y;
-                if (!touched) {
-                    y = now[n];
-                } else {
+                if (same && !here[n] && may[n] != 0) now[n] = *(const typename Pc::any*)(src + v);
+                u32x4 y = now[n];
+                if (any != 0) {
                     float x[VEC];
-                    if (same && may[n] != 0) now[n] = *(const typename Pc::any*)(src + v);
-                    E::widen(now[n], x);
+                    E::widen(y, x);
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) x[i] = value(x[i], words[i], may[n] >> i & 1);
+                    for (int i = 0; i < VEC; ++i) x[i] = penalized(x[i], words[i]);
+                    if (any & kBiased)
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) x[i] = biased(x[i], words[i]);
                     y = E::narrow(x);
                 }
+                if (may[n] != kEvery) y = Pc::masked(y, may[n]);
                 *(typename Pc::any*)(dst + v) = y;
             } else {
-                for (int i = 0; v + i < a.V; ++i) dst[v + i] = Pc::narrow1(value(Pc::widen1(src[v + i]), s_word[v - v0 + i], may[n] >> i & 1));
+                for (int i = 0; v + i < a.V; ++i) {
+                    const uint32_t word = s_word[v - v0 + i];
+                    dst[v + i] = Pc::narrow1(may[n] >> i & 1 ? biased(penalized(Pc::widen1(src[v + i]), word), word) : kGone);
+                }
             }
         }
     }

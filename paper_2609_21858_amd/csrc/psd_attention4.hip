@@ -14,8 +14,8 @@ namespace psd {
 
 namespace {
 
-// x as bfloat16 terms that sum to it (float32: each the next 8 bits, cut towards zero, so that none overflows;
-// infinite and NaN ones are their first term).
+// x as bfloat16 terms that sum to it (float32: each the next 8 bits, cut towards zero, so that none overflows; infinite and
+// NaN ones come out NaN).
 template <int TERMS>
 __device__ __forceinline__ void split(float x, float (&t)[TERMS]) {
     if constexpr (TERMS == 1) {

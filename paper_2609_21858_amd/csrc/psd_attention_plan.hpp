@@ -77,8 +77,9 @@ constexpr int kUnit = 128;  // cached tokens: a block of each wave (two in float
 // joins pay from one on (37 tokens of 12 heads 38 us, with 4 units 49).
 constexpr int join_units(bool bf16) { return bf16 ? 4 : 1; }
 
-// The same over a cache held in 4 bits.
-constexpr int join_units4(bool bf16) { return bf16 ? 4 : 1; }
+// The same over a cache held in 4 bits: a block of each wave (27 float32 rows of 6 sequences of up to 1500 tokens 21 us; 1 unit 24, 4
+// units 26), two in bfloat16 (8 sequences of up to 2000 tokens 15.1 us; 2 units 16.3).
+constexpr int join_units4(bool bf16) { return bf16 ? 4 : 2; }
 
 // Threads of the few-row kernel: one workgroup a CU, two waves a SIMD, or one where the rows' outputs take
 // the registers of two.
@@ -219,7 +220,7 @@ inline Plan make_plan(const CacheArgs& c, int H, bool bf16, int span, bool q4 = 
         // (4 bits: no more than the bounds have work for, which the division would send home: 4 sequences of up to 512 tokens
         // 8.9 us, with 512 workgroups 10.1)
         const long items = (long)c.B * p.tiles;
-        if (q4) p.wgs = (int)std::min<long>(p.wgs, items * ((span + kUnit * join_units4(bf16) - 1) / (kUnit * join_units4(bf16))));
+        if (q4) p.wgs = (int)std::min<long>(p.wgs, items * (span / (kUnit * join_units4(bf16)) + 2));
     } else {
         // Rows of a workgroup and parts of the longest range, by the time they take in 64-token blocks:
         // every round of resident workgroups takes a part and about 3 blocks to start and end; the join of

@@ -577,7 +577,7 @@ def make_cache4(k, v, k_scale, v_scale, head_dim: int, dtype=torch.bfloat16) -> 
 def new_cache4(pages: int, page_tokens: int, heads: int, head_dim: int, layers: int = 0, dtype=torch.bfloat16,
                device="cuda") -> Cache4:
     """A cache of zeros in the layout that attention reads fastest: a head's page in one piece.  layers > 0: all of a
-    model's layers for kv_keep; `layer` gives each layer's own."""
+    model's layers for kv_keep; cache4_layer gives each layer's own."""
     groups = -(-head_dim // 32)
     lead = (layers,) if layers else ()
 
@@ -587,7 +587,7 @@ def new_cache4(pages: int, page_tokens: int, heads: int, head_dim: int, layers: 
     return make_cache4(pool(16 * groups, 0), pool(16 * groups, 0), pool(groups, 127), pool(groups, 127), head_dim, dtype)
 
 
-def layer(cache: Cache4, i: int) -> Cache4:
+def cache4_layer(cache: Cache4, i: int) -> Cache4:
     """Layer i of a 4-bit cache with layers, for kv_append and attention."""
     if cache.tensors[0].dim() != 5 or not 0 <= i < cache.layers:
         _refuse(f"layer {i} of {cache.layers}")
@@ -621,6 +621,13 @@ def _ref(s):
     return None if s is None else ctypes.byref(s)
 
 
+def _here(t):
+    """A call's tensor, which stands for the others, is on the current device: host memory would fault the GPU."""
+    at = t.get_device()
+    if at < 0 or at != torch.cuda.current_device():
+        _refuse("a tensor in host memory" if at < 0 else f"a tensor on device {at}, which is not the current one")
+
+
 def kv_append(cache, seqs: Seqs, k, v, q=None, q_out=None, cos=None, sin=None, interleaved: bool = False,
               positions=None, q_norm=None, k_norm=None, eps: float = 1e-6, k_held=None, v_held=None, stream=None):
     """psd_kv_append: keys (normed with k_norm, turned by cos and sin float32 [positions][R/2]) and values into the
@@ -649,6 +656,7 @@ def kv_append(cache, seqs: Seqs, k, v, q=None, q_out=None, cos=None, sin=None, i
             _refuse("q_norm and k_norm: [head dim] in the cache's dtype")
     rot = Rotation(R, 1 if interleaved else 0, P, _ptr(cos), _ptr(sin), _ptr(positions), _ptr(q_norm), _ptr(k_norm), eps)
     if type(cache) is Cache4:
+        _here(k)
         kh = None if k_held is None else _rows(k_held, "k_held", cache, rows, heads)
         vh = None if v_held is None else _rows(v_held, "v_held", cache, rows, heads)
         _check(_lib.psd_kv_append4(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(rot), ctypes.byref(rk),
@@ -699,7 +707,10 @@ def attention(cache, seqs: Seqs, q, ws, scale: float = None, window: int = 0, ma
         words = mask.shape[1]
     if scale is None:
         scale = cache.head_dim ** -0.5
-    call = _lib.psd_attention4 if type(cache) is Cache4 else _lib.psd_attention
+    call = _lib.psd_attention
+    if type(cache) is Cache4:
+        _here(q)
+        call = _lib.psd_attention4
     _check(call(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(rq), H, scale, window, _ptr(mask), words,
                 ctypes.byref(ro), _ptr(o.get("lse")), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
     return o
@@ -718,7 +729,10 @@ def kv_keep(cache, seqs: Seqs, keep, n_keep, kv_out=None, stream=None):
         kv_out = torch.empty((B,), dtype=torch.int32, device=keep.device)
     else:
         _ints(kv_out, "kv_out", 1, B)
-    call = _lib.psd_kv_keep4 if type(cache) is Cache4 else _lib.psd_kv_keep
+    call = _lib.psd_kv_keep
+    if type(cache) is Cache4:
+        _here(keep)
+        call = _lib.psd_kv_keep4
     _check(call(ctypes.byref(cache), ctypes.byref(seqs), _ptr(keep), _row_stride(keep, "keep"), keep.shape[1],
                 _ptr(n_keep), _ptr(kv_out), _stream(stream)))
     return kv_out
@@ -763,6 +777,7 @@ def kv_reserve(pages: Pages, seqs: Seqs, n_new, kv_have, held, granted=None, row
                 o[name] = n_new.new_empty(n, dtype=dt)
         elif t.shape != (n,) or t.dtype != dt or not t.is_contiguous():
             _refuse(f"{name}: contiguous {dt} [{n}]")
+    _here(n_new)
     r = Reservation(n_new.data_ptr(), kv_have.data_ptr(), held.data_ptr(), seqs.table, seqs.new_start, seqs.kv_len, o["granted"].data_ptr())
     if rows_out:
         r.row_seq, r.positions, r.slots = o["row_seq"].data_ptr(), o["positions"].data_ptr(), o["slots"].data_ptr()
@@ -835,6 +850,7 @@ def adjust_logits(params: Params, logits, text=None, length=None, text_from=None
         else:
             _refuse(f"allowed: contiguous int32 [B][{words}] or one mask a row")
         a.allowed = allowed.data_ptr()
+    _here(logits)
     _check(_lib.psd_adjust_logits(ctypes.byref(params), ctypes.byref(a), B, S, depth0, _ptr(logits), _ptr(out), _stream(stream)))
     return out
 

@@ -162,6 +162,25 @@ def test_append_tokens_without_a_place(psd, dtype):
     assert bool((held[3:] == 3.0).all()) and not bool((held[:3] == 3.0).all())
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("D,R,rows", [(128, 64, 3), (80, 40, 3), (64, 64, 1100)])
+def test_append_held_in_place(psd, D, R, rows, dtype):
+    """The held values written over the keys and values that they come from, the queries over themselves."""
+    got = []
+    for in_place in (False, True):
+        s = ref4.Sequences4([(rows, rows + 9), (2, 11)], 2, D, 16, dtype)
+        g = torch.Generator().manual_seed(8)
+        q, k, v = (torch.randn((s.rows, n, D), generator=g).to(dtype).cuda() for n in (6, 2, 2))
+        cache, seqs, pools = s.handles(psd)
+        cos, sin = (x.cuda() for x in rope_tables(rows + 20, R))
+        outs = (q, k, v) if in_place else tuple(torch.empty_like(x) for x in (q, k, v))
+        psd.kv_append(cache, seqs, k, v, q=q, q_out=outs[0], cos=cos, sin=sin, k_held=outs[1], v_held=outs[2])
+        torch.cuda.synchronize()
+        got.append([x.cpu() for x in outs] + [p.cpu() for p in pools])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
 # ---------------------------------------------------------------- attention
 
 def attention_bounds(s, out, spread, size, vmax, kv, dtype):

@@ -224,12 +224,12 @@ def test_binding_of_caches(psd):
         psd.make_cache4(k, k, s, s, 80, dtype=torch.float16)
     new = psd.new_cache4(5, 16, 2, 80, layers=3, dtype=torch.float32, device="cpu")
     assert new.layers == 3 and new.stride_token == 48 and new.stride_head == 16 * 48 and new.scale_token == 3
-    one = psd.layer(new, 2)
+    one = psd.cache4_layer(new, 2)
     assert one.layers == 1 and one.k == new.k + 2 * new.stride_layer and one.v_scale == new.v_scale + 2 * new.scale_layer
     assert one.dtype == psd.PSD_F32
     for bad in ((new, 3), (new, -1), (c, 0)):
         with pytest.raises(psd.PsdError):
-            psd.layer(*bad)
+            psd.cache4_layer(*bad)
 
 
 def test_binding_of_rows(psd):
@@ -279,3 +279,19 @@ def test_binding_of_adjustments(psd):
         with pytest.raises(psd.PsdError) as e:
             psd.adjust_logits(p, **{**dict(logits=z), **bad})
         assert e.value.status == psd.PSD_E_ARG, sorted(bad)
+
+
+def test_binding_of_host_memory(psd):
+    """Tensors in host memory, which would fault the GPU, are refused by every call."""
+    ints = lambda *n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    cache = psd.new_cache4(4, 16, 2, 64, device="cpu")
+    seqs = psd.make_seqs(ints(3), ints(2), ints(2, 5), 4, 2, 64)
+    rows = torch.zeros((4, 2, 64), dtype=torch.bfloat16)
+    z = torch.zeros((2, 1, 3, 50))
+    for call in (lambda: psd.kv_append(cache, seqs, rows, rows), lambda: psd.attention(cache, seqs, rows, None),
+                 lambda: psd.kv_keep(cache, seqs, ints(2, 3), ints(2)),
+                 lambda: psd.kv_reserve(psd.new_pages(4, 16, device="cpu"), seqs, ints(2), ints(2), ints(2)),
+                 lambda: psd.adjust_logits(psd.make_params(0, 50, 1, 0, dtype=torch.float32), z)):
+        with pytest.raises(psd.PsdError) as e:
+            call()
+        assert "host memory" in str(e.value)
