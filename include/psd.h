@@ -628,7 +628,7 @@ typedef struct {
     const int32_t *draft_tokens; /* device [B][K][gamma]: the row of depth s on path k has also seen the path's
                                     tokens before depth s */
     int32_t gamma;              /* entries of a path in draft_tokens */
-    const float *repetition;    /* device [B]: rho > 0; NULL: 1 */
+    const float *repetition;    /* device [B]: rho, 2^-126 to 2^126; NULL: 1 */
     const float *presence;      /* device [B]; NULL: 0 */
     const float *frequency;     /* device [B]; NULL: 0 */
     const int32_t *bias_tokens; /* device [B][bias_width]; one outside [0, V) is passed over */

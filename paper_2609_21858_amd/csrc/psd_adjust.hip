@@ -153,7 +153,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
     };
     if (a.text) {
         const int32_t* text = a.text + (int64_t)b * a.text_stride;
-        const int to = (int)min(a.length[b], (int64_t)a.text_max);
+        const int to = (int)min(max(a.length[b], (int64_t)0), (int64_t)a.text_max);
         const int from = a.from ? (int)min(max(a.from[b], (int64_t)0), (int64_t)a.text_max) : 0;
         // four tokens a load, four loads in flight
         int i = from + tid * 4;

@@ -51,12 +51,6 @@ struct Stream4Shape {
     static constexpr int V_BYTES = 32 * PITCH * 2;
 };
 
-// Blocks of a wave on their way into registers: two where they fit.
-template <bool BF16, int DP, int RB>
-constexpr int stream4_ahead() {
-    return 1;
-}
-
 template <int DP, int RB>
 constexpr int stream4_lds() {
     constexpr int values = kWaves4 * Stream4Shape<DP>::V_BYTES, join = kWaves4 * 16 * RB * (DP + 4) * 4;
@@ -72,8 +66,7 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
     constexpr int NW = kWaves4, NT = 64 * NW;
     constexpr int ROWS = 16 * RB;
     __shared__ __align__(16) char s_mem[stream4_lds<DP, RB>()];
-    constexpr int AHEAD = stream4_ahead<BF16, DP, RB>();
-    __shared__ int64_t s_off[NW][AHEAD + 1][S::TOK], s_scale[NW][AHEAD + 1][S::TOK];
+    __shared__ int64_t s_off[NW][2][S::TOK], s_scale[NW][2][S::TOK];
     __shared__ StreamShared<NT, ROWS> sh;
 
     const AttentionArgs& a = args.a;
@@ -127,9 +120,8 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
             const int at = j < c1 ? j : 0;
             return table[p.page_shift >= 0 ? at >> p.page_shift : at / c.P];
         };
-        int pages[AHEAD + 1];  // (set out first: the first keys wait for them)
-#pragma unroll
-        for (int n = 0; n <= AHEAD; ++n) pages[n] = page_of(wave + n * NW);
+        const int first_page = page_of(wave);  // (set out first: the first keys wait for it)
+        int page = page_of(wave + NW);
         // this lane's rows, and their queries as B operands (unconditional loads; what is not there counts as zero)
         int row_i[RB];
         u32x4 qf[RB][TERMS][S::KK];
@@ -226,18 +218,14 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
             }
         };
 
-        Block block[AHEAD];
-#pragma unroll
-        for (int n = 0; n < AHEAD; ++n) {
-            block[n].there = publish(wave + n * NW, pages[n], n);
-            load_keys(n, block[n]);
-            __builtin_amdgcn_sched_barrier(0);  // keys before values, as in the loop: their wait counts on it
-            load_values(n, block[n]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        int page = pages[AHEAD], slot = 0;
-        // Block `blk`, whose places are in `slot`; x then takes the block AHEAD rounds later.
-        auto step = [&](int blk, Block& x) {
+        Block x;
+        x.there = publish(wave, first_page, 0);
+        load_keys(0, x);
+        __builtin_amdgcn_sched_barrier(0);  // keys before values, as in the loop: their wait counts on it
+        load_values(0, x);
+        __builtin_amdgcn_sched_barrier(0);
+        // Block `blk` is in x, its places in `slot`; x takes the wave's next one as it becomes free.
+        for (int blk = wave, slot = 0; blk < blocks; blk += NW, slot ^= 1) {
             // A CU serves its older waves first: its first workgroup would end 7 of 45 us before its second (32 x 8192 tokens).
             // The second goes first in every other block, which leaves 3.
             if (younger) {
@@ -246,7 +234,6 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
                 else
                     __builtin_amdgcn_s_setprio(0);
             }
-            const int fill = slot == 0 ? AHEAD : slot - 1;  // the slot of that one
             const uint64_t there = x.there;
             const int j0 = c0 + blk * S::TOK;
             // every row sees the whole block, or bits say which tokens
@@ -267,10 +254,10 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
                         for (int i = 0; i < TERMS; ++i) sv[rb][t] = multiply<true>(keys, qf[rb][i][kk], sv[rb][t]);
                 }
             }
-            // the later block's keys set out
-            x.there = publish(blk + AHEAD * NW, page, fill);
-            load_keys(fill, x);
-            page = page_of(blk + (AHEAD + 1) * NW);
+            // the next block's keys set out
+            x.there = publish(blk + NW, page, slot ^ 1);
+            load_keys(slot ^ 1, x);
+            page = page_of(blk + 2 * NW);
             // A row's weight 0 times a NaN value that the row does not see would be NaN: where rows differ in what they see,
             // such groups are taken out, and a second product puts infinity where a row does see one.
             bool odd = false;
@@ -397,7 +384,7 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
             add_values(0);
             wave_sync();
             write_values(1);
-            load_values(fill, x);
+            load_values(slot ^ 1, x);
             add_values(1);
             wave_sync();
             if (odd) {
@@ -427,14 +414,6 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
                     add_values(h);
                     wave_sync();
                 }
-            }
-            slot = slot == AHEAD ? 0 : slot + 1;
-        };
-        for (int round = 0; round < blocks; round += AHEAD * NW) {
-#pragma unroll
-            for (int n = 0; n < AHEAD; ++n) {
-                const int blk = round + n * NW + wave;
-                if (blk < blocks) step(blk, block[n]);
             }
         }
         finish_item<BF16, DP, RB, NT, 4>(a, p, sh, s_mem, st, Item{s, row0, rows, before, n_units, from, to}, wg, g, o, m, l);

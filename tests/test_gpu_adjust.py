@@ -135,6 +135,15 @@ def test_texts(psd):
     check(psd, wide)
 
 
+def test_lengths_past_32_bits_are_bounded(psd):
+    """A length whose lower 32 bits are a count of tokens that are not there."""
+    x = inputs(4, 1, 2, 300, F32, L=70)
+    x["length"] = torch.tensor([-(1 << 32) + 5000, (1 << 32) + 3, -(1 << 63), 1 << 62])
+    check(psd, x)
+    x["text_from"] = torch.tensor([0, 60, 0, -(1 << 32) + 65])
+    check(psd, x)
+
+
 @pytest.mark.parametrize("n_bias", [1, 300, 1024])
 def test_biases_of_one_token_add_up_in_order(psd, n_bias):
     x = inputs(2, 1, 2, 9000, F32, n_bias=n_bias, few=6)
