@@ -422,10 +422,12 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
 
 template <bool BF16, int DP>
 void launch_stream4(const Attention4Args& a, const Plan& p, dim3 grid, hipStream_t stream) {
-    if (p.tile_rows == 16)
-        hipLaunchKernelGGL((stream4_kernel<BF16, DP, 1>), grid, dim3(64 * kWaves4), 0, stream, a, p);
-    else
-        hipLaunchKernelGGL((stream4_kernel<BF16, DP, 2>), grid, dim3(64 * kWaves4), 0, stream, a, p);
+    if constexpr (tile_limit4(BF16, DP) == 32)
+        if (p.tile_rows == 32) {
+            hipLaunchKernelGGL((stream4_kernel<BF16, DP, 2>), grid, dim3(64 * kWaves4), 0, stream, a, p);
+            return;
+        }
+    hipLaunchKernelGGL((stream4_kernel<BF16, DP, 1>), grid, dim3(64 * kWaves4), 0, stream, a, p);
 }
 
 template <int DP>

@@ -77,8 +77,8 @@ constexpr int kUnit = 128;  // cached tokens: a block of each wave (two in float
 // joins pay from one on (37 tokens of 12 heads 38 us, with 4 units 49).
 constexpr int join_units(bool bf16) { return bf16 ? 4 : 1; }
 
-// The same over a cache held in 4 bits: a block of each wave (27 float32 rows of 6 sequences of up to 1500 tokens 21 us; 1 unit 24, 4
-// units 26), two in bfloat16 (8 sequences of up to 2000 tokens 15.1 us; 2 units 16.3).
+// The same over a cache held in 4 bits: a block of each wave (27 float32 rows of 6 sequences of up to 1500 tokens 16 us; 1 unit 19, 4
+// units 18), two in bfloat16 (8 sequences of up to 2000 tokens 15.1 us; 2 units 16.3).
 constexpr int join_units4(bool bf16) { return bf16 ? 4 : 2; }
 
 // Threads of the few-row kernel: one workgroup a CU, two waves a SIMD, or one where the rows' outputs take
@@ -143,6 +143,12 @@ PSD_HOST_DEVICE Division divide(int units, int wgs, int least_units) {
     d.more = units - d.share * d.wgs;
     return d;
 }
+
+// Rows of a tile over a cache held in 4 bits.  bfloat16: up to 32, and more are tile_kernel's.  float32 rows of more than 64
+// dimensions: 16, since 32 leave one workgroup a CU and spill (D=128, 27 rows of 6 sequences 16 us and 20, 32 of
+// 32 sequences, up to 4096 63 and 74, 4 x 512 new tokens 261 and 306; D=256, 32 rows 87 and 163, 4 x 512 442 and 664; D=64,
+// which does not, 101 and 82).
+constexpr int tile_limit4(bool bf16, int D) { return bf16 || D <= 64 ? 32 : 16; }
 
 // Over a cache held in 4 bits, where there are workgroups to spare: the length of stretches that end where items
 // end, or 0 for stretches that do not.  A workgroup that goes on to a second item starts a chain of its own (places, first
@@ -212,8 +218,8 @@ inline Plan make_plan(const CacheArgs& c, int H, bool bf16, int span, bool q4 = 
         // float32 rows in tiles of 32 while tiles of 64 would leave CUs without one (12 heads of 80, 37 tokens
         // of 6 sequences: 40 us and 45; 1024 new of 4096 tokens of 16 heads, CUs full: 450 and 408)
         const bool few = !bf16 && c.D > 64 && (long)c.B * c.G * ((most + 63) / 64) < kCus;
-        const int limit = c.D > 128 || few || q4 ? 32 : 64;  // (4 bits: bfloat16 rows are no more, float32 ones spill)
-        p.tile_rows = most <= 16 ? 16 : most <= 32 ? 32 : limit;
+        const int limit = q4 ? tile_limit4(bf16, c.D) : c.D > 128 || few ? 32 : 64;
+        p.tile_rows = most <= 16 ? 16 : std::min(most <= 32 ? 32 : 64, limit);
         p.tiles = (int)((most + p.tile_rows - 1) / p.tile_rows);
         const int resident = q4 ? stream4_resident(padded(c.D), p.tile_rows / 16) : 1;
         p.wgs = std::max(kCus * resident / c.G, 1);  // on every CU
