@@ -51,10 +51,12 @@ struct Stream4Shape {
     static constexpr int V_BYTES = 32 * PITCH * 2;
 };
 
+// The waves' values and two blocks' places, and in their stead, behind the loop, the outputs of the join.
 template <int DP, int RB>
 constexpr int stream4_lds() {
-    constexpr int values = kWaves4 * Stream4Shape<DP>::V_BYTES, join = kWaves4 * 16 * RB * (DP + 4) * 4;
-    return values > join ? values : join;
+    using S = Stream4Shape<DP>;
+    constexpr int loop = kWaves4 * (S::V_BYTES + 2 * 2 * 8 * S::TOK), join = kWaves4 * 16 * RB * (DP + 4) * 4;
+    return loop > join ? loop : join;
 }
 
 template <bool BF16, int DP, int RB>
@@ -66,7 +68,6 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
     constexpr int NW = kWaves4, NT = 64 * NW;
     constexpr int ROWS = 16 * RB;
     __shared__ __align__(16) char s_mem[stream4_lds<DP, RB>()];
-    __shared__ int64_t s_off[NW][2][S::TOK], s_scale[NW][2][S::TOK];
     __shared__ StreamShared<NT, ROWS> sh;
 
     const AttentionArgs& a = args.a;
@@ -81,6 +82,8 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
     const float sc = a.scale * kLog2e;
     const int last_group = (c.D + 31) / 32 - 1;
     char* s_v = s_mem + wave * S::V_BYTES;
+    int64_t(*s_off)[S::TOK] = (int64_t(*)[S::TOK])(s_mem + NW * S::V_BYTES) + wave * 4;
+    int64_t(*s_scale)[S::TOK] = s_off + 2;
     // this lane's codes of a key: groups past the head's end are its last one again, which meets zeros
     int key_at[S::NS], key_group[S::NS];
 #pragma unroll
@@ -176,8 +179,8 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
             const int pi = p.page_shift >= 0 ? j >> p.page_shift : j / c.P;
             const bool there = j < c1 && (unsigned)page < (unsigned)c.pages;
             const int64_t place = j - (int64_t)pi * c.P;
-            s_off[wave][slot][lane] = there ? (int64_t)page * c.stride_page + place * c.stride_token : 0;
-            s_scale[wave][slot][lane] = there ? (int64_t)page * args.s.page + place * args.s.token : 0;
+            s_off[slot][lane] = there ? (int64_t)page * c.stride_page + place * c.stride_token : 0;
+            s_scale[slot][lane] = there ? (int64_t)page * args.s.page + place * args.s.token : 0;
             const uint64_t bits = __ballot(there);
             wave_sync();
             return bits;
@@ -192,8 +195,8 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
         auto load_keys = [&](int slot, Block& x) {
 #pragma unroll
             for (int t = 0; t < S::TT; ++t) {
-                const char* src = k_src + s_off[wave][slot][16 * t + r];
-                const uint8_t* scale = ks_src + s_scale[wave][slot][16 * t + r];
+                const char* src = k_src + s_off[slot][16 * t + r];
+                const uint8_t* scale = ks_src + s_scale[slot][16 * t + r];
                 if constexpr (DP == 64) {
                     const uint2 w = *(const uint2*)(src + key_at[0]);
                     x.kc[t][0] = w.x;
@@ -213,8 +216,8 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
         auto load_values = [&](int slot, Block& x) {
 #pragma unroll
             for (int k = 0; k < S::NV; ++k) {
-                x.vc[k] = *(const u32x4*)(v_src + s_off[wave][slot][k * S::TPI + v_token]);
-                x.vs[k] = vs_src[s_scale[wave][slot][k * S::TPI + v_token]];
+                x.vc[k] = *(const u32x4*)(v_src + s_off[slot][k * S::TPI + v_token]);
+                x.vs[k] = vs_src[s_scale[slot][k * S::TPI + v_token]];
             }
         };
 
@@ -393,7 +396,7 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
 #pragma unroll 1
                     for (int k = h * S::NV / 2; k < (h + 1) * S::NV / 2; ++k) {
                         const int t = k * S::TPI + v_token;
-                        const bool nan = there >> t & 1u && vs_src[s_scale[wave][slot][t]] > quant4::kMost;
+                        const bool nan = there >> t & 1u && vs_src[s_scale[slot][t]] > quant4::kMost;
                         const uint32_t one = nan ? 0x7F7F7F7Fu : 0u;  // the largest finite number, or nearly
 #pragma unroll
                         for (int e = 0; e < 4; ++e) *(u32x4*)(piece_at(k) + 16 * e) = u32x4{one, one, one, one};

@@ -87,7 +87,7 @@ constexpr int stream_waves(int DP, int RB) { return RB * DP >= 512 || DP == 256 
 
 // The same over a cache held in 4 bits: workgroups of four waves, two of them a CU where the registers allow.
 constexpr int kWaves4 = 4;
-constexpr int stream4_resident(int DP, int RB) { return RB * DP >= 256 ? 1 : 2; }
+constexpr int stream4_resident(int DP, int RB) { return DP == 256 ? 1 : 2; }
 
 struct Range {
     int lo, hi;  // cached positions that some row of a tile sees
