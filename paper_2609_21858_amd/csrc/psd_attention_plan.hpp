@@ -181,17 +181,20 @@ inline int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
 // Over a cache held in 4 bits: are `most` rows of a sequence (at most 32) better off in tile_kernel?  Its time grows faster by
 // 44 us for 2^20 tokens of all heads of 128 dimensions (30 for 32 rows), the other's with the parts that one workgroup joins of
-// a long item, 0.25 us each (0.33 of 32 rows; half as much again for heads of 256).  us there and here:
-// D=128, G=8, 4 rows, 2 x 8000 24 and 19, 1 x 32768 44 and 29, 8 x 1500 15 and 17, 16 x 4096 24 and 41, 1 x 131072 58 and 76; 20 rows,
-// 2 x 8000 33 and 20, 1 x 32768 39 and 29, 16 x 4096 33 and 43; D=64, 4 rows, 2 x 8000 21 and 14, 64 x 1024 15 and 28; D=256, G=4,
-// 4 rows, 2 x 8000 34 and 26, 16 x 4096 30 and 60; G=1, 32 rows, 1 x 131072 140 and 61.  More than 32 rows: 48 rows, 64 x 1024 67 and 44,
-// 1 x 131072 124 and 86, 64 rows of 16 sequences, up to 8192 86 and 85.
+// a long item, 0.25 us each; of 32 rows by 3.5 for a join and 0.275 for each part, and by 8.5 more for heads of 256, one
+// workgroup a CU.  us there and here: D=128, G=8, 4 rows, 2 x 8000 24 and 19, 1 x 32768 44 and 29, 8 x 1500 15 and 17, 16 x 4096 24
+// and 41, 1 x 131072 58 and 76; 20 rows, 4 x 500 13 and 15, 4 x 2000 18 and 16, 4 x 8000 30 and 28, 1 x 32768 42 and 30, 16 x 4096
+// 33 and 43, 1 x 131072 62 and 76, 32 x 1000 19 and 31; D=64, 4 rows, 2 x 8000 21 and 14, 64 x 1024 15 and 28, 20 rows, 4 x 2000
+// 19 and 14; D=256, G=4, 4 rows, 2 x 8000 34 and 26, 16 x 4096 30 and 60, 20 rows, 4 x 500 25 and 23, 16 x 1000 33 and 25,
+// 16 x 4096 51 and 61, 1 x 131072 104 and 116.  Over 126 calls of 17 to 32 rows the faster of the two but for 0.5 % in
+// the mean.  More than 32 rows: 48 rows, 64 x 1024 67 and 44, 1 x 131072 124 and 86.
 inline bool tiles4(const CacheArgs& c, long most, long span) {
     const int rb = most <= 16 ? 1 : 2, DP = padded(c.D), wgs = std::max(kCus * stream4_resident(DP, rb) / c.G, 1);
     const long parts = std::min<long>(wgs / c.B, span / kUnit / join_units4(true));
     const double tokens = (double)c.B * c.G * span * std::max(c.D, 64) / 128 / (1 << 20);
-    if (parts < 2) return false;
-    return (rb == 2 && DP == 128 ? 30 : 44) * tokens < (rb == 1 ? 0.25 * parts : 0.2 + 0.33 * parts) * (DP == 256 ? 1.5 : 1.);
+    const double ahead = rb == 1 ? (parts < 2 ? 0. : (DP == 256 ? 0.375 : 0.25) * parts)
+                                 : (parts < 2 ? 0. : 3.5 + 0.275 * parts) + (DP == 256 ? 8.5 : 0.);
+    return (rb == 2 && DP == 128 ? 30 : 44) * tokens < ahead;
 }
 
 inline Plan make_plan(const CacheArgs& c, int H, bool bf16, int span, bool q4 = false) {
