@@ -94,6 +94,10 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
     auto dim_of = [&](int kk) { return DP == 64 ? 16 * q + 8 * kk : 32 * (q + 4 * (kk / 4)) + 8 * (kk % 4); };
     const int v_group = lane % S::GROUPS, v_token = lane / S::GROUPS;
     const int v_held = min(v_group, last_group);
+    // (eight lanes store together: all groups of a token, 64 bytes apart, of 128 in a round of the banks; 32 sequences of up
+    // to 16384 tokens 84.5 us, in one order 92.  Two tokens of 4 groups lose less to the banks than turning them takes: 32 float32
+    // rows, 98 us and 101)
+    const int v_turn = DP == 256 ? v_group >> 1 & 3 : 0;
     const char* k_src = (const char*)c.k + (int64_t)g * c.stride_head;
     const char* v_src = (const char*)c.v + (int64_t)g * c.stride_head + v_held * 16;
     const uint8_t* ks_src = (const uint8_t*)args.s.k + (int64_t)g * args.s.head;
@@ -283,9 +287,7 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
             auto write_values = [&](int h) {
 #pragma unroll
                 for (int k = h * S::NV / 2; k < (h + 1) * S::NV / 2; ++k) {
-                    const float by = quant4::scale_value(x.vs[k]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) *(u32x4*)(piece_at(k) + 16 * e) = quant4::decode8(x.vc[k][e], by);
+                    quant4::decode_group(piece_at(k), x.vc[k], quant4::scale_value(x.vs[k]), v_turn);
                 }
                 wave_sync();
             };

@@ -97,6 +97,15 @@ __device__ __forceinline__ u32x4 decode8(uint32_t w, float by) {
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, by, 3))};
 }
 
+// A group as bfloat16 into 64 bytes of LDS, 16 at a time, of which the (e ^ turn)th is the e-th to go: lanes whose groups begin
+// on the same banks take different turns.
+__device__ __forceinline__ void decode_group(char* to, u32x4 w, float by, int turn) {
+    w = turn & 1 ? u32x4{w[1], w[0], w[3], w[2]} : w;
+    w = turn & 2 ? u32x4{w[2], w[3], w[0], w[1]} : w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) *(u32x4*)(to + 16 * (e ^ turn)) = decode8(w[e], by);
+}
+
 // 16 bytes of elements: 8 bfloat16, or 4 float32 from the lower half.
 template <bool BF16>
 __device__ __forceinline__ u32x4 decode(uint32_t w, int s) {
