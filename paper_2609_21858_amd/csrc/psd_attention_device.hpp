@@ -168,7 +168,7 @@ __device__ __forceinline__ Stretch find_stretch(const AttentionArgs& a, const Pl
     __syncthreads();
     const int units = uniform(sh.units[NT]);
     // While no item is much longer than a stretch, each workgroup takes one item whole and none is joined.
-    const Division cut = divide(units, p.wgs, least_units);
+    const Division cut = divide(units, p.wgs, SLACK > 0 ? least_units4(least_units, uniform(longest)) : least_units);
     const bool whole_items = SLACK == 0 && each == 1 && items <= p.wgs && uniform(longest) <= units / p.wgs + 1 + least_units;
     Stretch st;
     st.first = st.parts = 0;

@@ -80,6 +80,9 @@ constexpr int join_units(bool bf16) { return bf16 ? 4 : 1; }
 // The same over a cache held in 4 bits: a block of each wave (27 float32 rows of 6 sequences of up to 1500 tokens 16 us; 1 unit 19, 4
 // units 18), two in bfloat16 (8 sequences of up to 2000 tokens 15.1 us; 2 units 16.3).
 constexpr int join_units4(bool bf16) { return bf16 ? 4 : 2; }
+// A stretch's least units there: no more than the longest item has, since items that end with it leave nothing to join (48 and
+// 96 sequences of 5 tokens, 16 heads of 64: 11 and 15 us, with stretches of 4 units 17 and 19).
+PSD_HOST_DEVICE int least_units4(int least_units, int longest) { return lesser(least_units, greater(longest, 1)); }
 
 // Threads of the few-row kernel: one workgroup a CU, two waves a SIMD, or one where the rows' outputs take
 // the registers of two.

@@ -44,7 +44,7 @@ int main() {
                 before_chunk[t + 1] = units;
             }
             unit_start[items] = units;
-            const Division cut = divide(units, p.wgs, least);
+            const Division cut = divide(units, p.wgs, least_units4(least, longest));
             const int length = each == 1 ? aligned_length(units, items, longest, p.wgs, least, slack4(bf16, DP)) : 0;
             aligned = length > 0;
             std::vector<int> done(units, 0);
