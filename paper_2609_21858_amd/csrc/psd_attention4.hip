@@ -38,6 +38,15 @@ __device__ __forceinline__ uint32_t upper(float lo, float hi) {
 // gives each lane whole pieces of codes: of a token, lane q of four has the 4 DP / 32 words from dimension
 // DP / 4 q on (DP = 256: 32 dimensions from 32 q and from 128 + 32 q on), one scale byte to each 32 dimensions, and the
 // queries are laid out to match.  Values become bfloat16 on their way into the wave's LDS, 32 tokens at a time.
+//
+// Memory bounds long caches, (D/2 + D/32) 2 G bytes a token, and chains of dependent loads short ones (start, division,
+// places, keys, join of waves, join of parts: about 18 us in all).  H=32, G=8, D=128: 1 token of 32 sequences, up to
+// 16384 cached, 363 MB, 80 us, 4.5 TB/s (5.85 for each token more), float32 rows 86 - 96; heads of 64 52, 4 heads of 256
+// 85 - 92.  1 token of 64 sequences, up to 4096, 52 us, 5 tokens 63 - 70, float32 96 - 103; 1 token of 4 sequences, up
+// to 512, 8.4; behind 131072 46.  float32 rows are bound by products, three for one: 4 x 512 tokens to 2048 264 us,
+// 433 TFLOP/s of bfloat16 products.
+// Four waves a workgroup and two workgroups a CU, so that one's chains lie under the other's loads; 201 - 256 registers
+// a lane (heads of 256: one, with 356 - 416).
 template <int DP>
 struct Stream4Shape {
     static constexpr int TOK = 64;

@@ -16,6 +16,8 @@ __device__ __forceinline__ const AttentionArgs& rows_of(const Attention4Args& a)
 
 namespace {
 
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
 // One workgroup: 32 NW rows of one (sequence, key/value head), 32 a wave, over one part of its cache.
 // Blocks of 64 tokens go through LDS, which all waves read: 32x32x16 products, 64 x 32
 // scores a wave in 32 registers, the outputs in D/2 more.  Two buffers, one barrier a block: while
@@ -27,11 +29,10 @@ namespace {
 // buffers of 20 KB of values and 17 of keys.  Other heads, the same tokens: D=64 368 - 418 us; D=80, 96 and 112, padded to
 // 128, 534 - 557; D=192, padded to 256, 1652; D=256 1625 - 1672 (one workgroup a CU, 24 registers spilled).  Window 4096,
 // D=128: 157.  One token of 64 sequences, up to 4096 cached, window 1000, 263 MB: 46.
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
 //
 // Q4, over a cache held in 4 bits: a thread's pieces are a group's 16 bytes of codes and its scale byte, which become
-// 64 bytes of bfloat16 on their way into LDS; from there on everything is the same.
+// 64 bytes of bfloat16 on their way into LDS; from there on everything is the same.  2048 new tokens behind 14336: D=128
+// 511 - 529 us, 974 - 1010 TFLOP/s, products busy 44 %; D=64 367; D=256 1407.
 template <bool Q4, int DP, int NW>
 struct TileShape {
     static constexpr int TOK = 64;
@@ -165,8 +166,8 @@ __global__ __launch_bounds__(64 * NW, (DP == 256 || NW == 8 ? 1 : 2)) void tile_
         u32x4 k[S::N], v[S::N];
     };
     // Eight lanes store together: groups of a token begin 64 bytes apart, the next token's 16 (keys) or 64 (values) bytes
-    // further on, of 128 in a round of the banks.  2048 tokens behind 14336, D=256 1550 us without turns, 1407 with them, D=128 537 and
-    // 529: a fourth of all LDS cycles was waiting for banks, none is.
+    // further on, of 128 in a round of the banks.  2048 tokens behind 14336, D=256 1550 us without turns, 1407 with them,
+    // D=128 537 and 529: a fourth of all LDS cycles was waiting for banks, none is.
     auto turn_of = [&](int k) {
         if (DP == 256) return group_of(k) >> 1 & 3;
         if (of_values(k)) return DP == 64 ? token_of(k) & 3 : (group_of(k) & 2) | (token_of(k) & 1);

