@@ -240,6 +240,16 @@ def test_attention_shapes(psd, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128, 192])
+def test_attention_more_short_sequences_than_workgroups(psd, D, dtype):
+    """Sequences below a stretch's least length, some without rows, more of them than threads."""
+    check_attention(psd, [(1, 5)] * 40, 16, 16, D, 16, dtype)
+    check_attention(psd, [(b % 3, b % 3 + 7 * b % 140) for b in range(36)], 32, 16, D, 16, dtype)
+    check_attention(psd, [(1, 1 + b % 9) for b in range(260)] + [(2, 300)], 4, 2, D, 16, dtype)
+    check_attention(psd, [(9, 9 + 11 * b % 130) for b in range(34)], 48, 16, D, 16, dtype)  # 27 rows
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("window", [1, 2, 31, 64, 100, 5000])
 def test_attention_windows(psd, window, dtype):
     check_attention(psd, [(1, 300), (5, 333), (40, 200), (1, 1)], 8, 2, 128, 16, dtype, window=window)
