@@ -41,7 +41,8 @@ struct Piece<true> {
     __device__ static u32x4 masked(u32x4 w, uint32_t may) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t keep = (may >> 2 * i & 1 ? 0xFFFFu : 0u) | (may >> (2 * i + 1) & 1 ? 0xFFFF0000u : 0u);
+            const uint32_t lo = __builtin_amdgcn_sbfe(may, 2 * i, 1), hi = __builtin_amdgcn_sbfe(may, 2 * i + 1, 1);
+            const uint32_t keep = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
             w[i] = (w[i] & keep) | (0xFF80FF80u & ~keep);
         }
         return w;
@@ -55,7 +56,10 @@ struct Piece<false> {
     __device__ static float narrow1(float x) { return x; }
     __device__ static u32x4 masked(u32x4 w, uint32_t may) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = may >> i & 1 ? w[i] : 0xFF800000u;
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t keep = __builtin_amdgcn_sbfe(may, i, 1);
+            w[i] = (w[i] & keep) | (0xFF800000u & ~keep);
+        }
         return w;
     }
 };
@@ -95,8 +99,8 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
             may_next[n] = kEvery;
             if (v >= v1) continue;
             if (a.allowed) may_next[n] = a.allowed[b * a.allowed_seq + r * a.allowed_row + v / 32] >> (v % 32) & kEvery;
-            // in place: pieces that the text or a bias touches (those of a mask or a draft alone are read when they are due)
-            bool wanted = !same;
+            // in place without a mask: pieces that the text or a bias touches (those of a draft alone are read when they are due)
+            bool wanted = !same || a.allowed != nullptr;
             if (same) {
 #pragma unroll
                 for (int i = 0; i < VEC; i += 4) {
