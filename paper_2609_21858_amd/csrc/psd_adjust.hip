@@ -89,16 +89,16 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
     typename Pc::one* dst0 = (typename Pc::one*)a.out + row0;
     auto at = [&](int n) { return v0 + (n * kThreads + tid) * VEC; };
     u32x4 next[N];
-    uint32_t may_next[N];
+    uint32_t allowed_next[N];  // (words as loaded: shifted here, they would be waited for before the row)
     bool here_next[N];  // in place: is the piece on its way?
     constexpr uint32_t kEvery = (1u << VEC) - 1;
     auto load = [&](int r) {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int v = at(n);
-            may_next[n] = kEvery;
+            allowed_next[n] = ~0u;
             if (v >= v1) continue;
-            if (a.allowed) may_next[n] = a.allowed[b * a.allowed_seq + r * a.allowed_row + v / 32] >> (v % 32) & kEvery;
+            if (a.allowed) allowed_next[n] = a.allowed[b * a.allowed_seq + r * a.allowed_row + v / 32];
             // in place without a mask: pieces that the text or a bias touches (those of a draft alone are read when they are due)
             bool wanted = !same || a.allowed != nullptr;
             if (same) {
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             now[n] = next[n];
-            may[n] = may_next[n];
+            may[n] = allowed_next[n] >> (at(n) % 32) & kEvery;
             here[n] = here_next[n];
         }
         if (r + 1 < r1) load(r + 1);
