@@ -4,8 +4,9 @@
 //   z + sum of the token's biases;  -inf where the mask's bit is 0
 // with c the token's count in the sequence's text and among the row's own earlier drafts.  Memory
 // bounds it: every logit is read and written once; the texts are counted by each workgroup for its own
-// stretch of the vocabulary.  1280 rows of 128256 bfloat16 logits of 64 sequences, texts of 2048 tokens, 657 MB: 146 us, 4.5 TB/s
-// (a device copy 4.9); in place, where most pieces only pass, 108; 1152 float32 rows of 151936 293; 5 rows of 1024 5.
+// stretch of the vocabulary.  1280 rows of 128256 bfloat16 logits of 64 sequences, texts of 2048 tokens, 657 MB: 146 us,
+// 4.5 TB/s (a device copy 4.9), with a mask a row 152; in place, where most pieces only pass, 108, with masks 160; 1152 float32
+// rows of 151936 293; 5 rows of 1024 5.
 #include <hip/hip_runtime.h>
 
 #include "psd_serve.hpp"
