@@ -75,6 +75,7 @@ class Cache(ctypes.Structure):
 
 class Cache4(ctypes.Structure):
     """psd_cache4: keys and values in pages of 4-bit codes (make_cache4, new_cache4)."""
+    device = None
     _fields_ = [
         ("k", ctypes.c_void_p),
         ("v", ctypes.c_void_p),
@@ -99,6 +100,7 @@ class Cache4(ctypes.Structure):
 
 class Seqs(ctypes.Structure):
     """psd_seqs: the sequences of one call (make_seqs)."""
+    device = None
     _fields_ = [
         ("batch", ctypes.c_int32),
         ("rows", ctypes.c_int32),
@@ -134,6 +136,7 @@ class Rotation(ctypes.Structure):
 
 class Pages(ctypes.Structure):
     """psd_pages: the free pages of a pool (make_pages, new_pages)."""
+    device = None
     _fields_ = [("page_tokens", ctypes.c_int32), ("pages", ctypes.c_int32), ("ring", ctypes.c_void_p), ("state", ctypes.c_void_p)]
 
 
@@ -571,6 +574,7 @@ def make_cache4(k, v, k_scale, v_scale, head_dim: int, dtype=torch.bfloat16) -> 
     c = Cache4(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), d, heads, head_dim, page, pages,
                k.shape[0] if five else 1, st[0] if five else 0, st[-4], st[-3], st[-2], ss[0] if five else 0, ss[-4], ss[-3], ss[-2])
     c.tensors = (k, v, k_scale, v_scale)
+    c.device = _device_of(c.tensors)
     return c
 
 
@@ -606,6 +610,7 @@ def make_seqs(new_start, kv_len, table, rows: int, max_new: int, max_kv: int) ->
     s = Seqs(B, int(rows), int(max_new), int(max_kv), table.shape[1], _row_stride(table, "table"),
              new_start.data_ptr(), kv_len.data_ptr(), table.data_ptr())
     s.tensors = (new_start, kv_len, table)
+    s.device = _device_of(s.tensors)
     return s
 
 
@@ -621,11 +626,24 @@ def _ref(s):
     return None if s is None else ctypes.byref(s)
 
 
-def _here(t):
-    """A call's tensor, which stands for the others, is on the current device: host memory would fault the GPU."""
-    at = t.get_device()
+def _device_of(tensors) -> int:
+    """The device that a structure's tensors are on; -1: in host memory, or not all on one."""
+    at = tensors[0].get_device()
+    return at if all(t.get_device() == at for t in tensors) else -1
+
+
+def _here(structs, first, *others):
+    """All that a call hands to the GPU is on the current device: an address in host memory would fault it.  A structure made
+    without its make_ function has no device to compare."""
+    at = first.get_device()
     if at < 0 or at != torch.cuda.current_device():
         _refuse("a tensor in host memory" if at < 0 else f"a tensor on device {at}, which is not the current one")
+    for x in others:
+        if x is not None and x.get_device() != at:
+            _refuse("a tensor in host memory" if x.get_device() < 0 else f"tensors on devices {at} and {x.get_device()}")
+    for s in structs:
+        if s.device is not None and s.device != at:
+            _refuse(f"{type(s).__name__}: tensors in host memory or not all on device {at}")
 
 
 def kv_append(cache, seqs: Seqs, k, v, q=None, q_out=None, cos=None, sin=None, interleaved: bool = False,
@@ -656,7 +674,7 @@ def kv_append(cache, seqs: Seqs, k, v, q=None, q_out=None, cos=None, sin=None, i
             _refuse("q_norm and k_norm: [head dim] in the cache's dtype")
     rot = Rotation(R, 1 if interleaved else 0, P, _ptr(cos), _ptr(sin), _ptr(positions), _ptr(q_norm), _ptr(k_norm), eps)
     if type(cache) is Cache4:
-        _here(k)
+        _here((cache, seqs), k, v, q, q_out, cos, sin, positions, q_norm, k_norm, k_held, v_held)
         kh = None if k_held is None else _rows(k_held, "k_held", cache, rows, heads)
         vh = None if v_held is None else _rows(v_held, "v_held", cache, rows, heads)
         _check(_lib.psd_kv_append4(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(rot), ctypes.byref(rk),
@@ -709,7 +727,7 @@ def attention(cache, seqs: Seqs, q, ws, scale: float = None, window: int = 0, ma
         scale = cache.head_dim ** -0.5
     call = _lib.psd_attention
     if type(cache) is Cache4:
-        _here(q)
+        _here((cache, seqs), q, o["out"], o.get("lse"), mask, ws)
         call = _lib.psd_attention4
     _check(call(ctypes.byref(cache), ctypes.byref(seqs), ctypes.byref(rq), H, scale, window, _ptr(mask), words,
                 ctypes.byref(ro), _ptr(o.get("lse")), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
@@ -731,7 +749,7 @@ def kv_keep(cache, seqs: Seqs, keep, n_keep, kv_out=None, stream=None):
         _ints(kv_out, "kv_out", 1, B)
     call = _lib.psd_kv_keep
     if type(cache) is Cache4:
-        _here(keep)
+        _here((cache, seqs), keep, n_keep, kv_out)
         call = _lib.psd_kv_keep4
     _check(call(ctypes.byref(cache), ctypes.byref(seqs), _ptr(keep), _row_stride(keep, "keep"), keep.shape[1],
                 _ptr(n_keep), _ptr(kv_out), _stream(stream)))
@@ -749,6 +767,7 @@ def make_pages(ring, state, page_tokens: int) -> Pages:
         _refuse("state: int32 [4]")
     p = Pages(int(page_tokens), ring.shape[0], ring.data_ptr(), state.data_ptr())
     p.tensors = (ring, state)
+    p.device = _device_of(p.tensors)
     return p
 
 
@@ -777,7 +796,7 @@ def kv_reserve(pages: Pages, seqs: Seqs, n_new, kv_have, held, granted=None, row
                 o[name] = n_new.new_empty(n, dtype=dt)
         elif t.shape != (n,) or t.dtype != dt or not t.is_contiguous():
             _refuse(f"{name}: contiguous {dt} [{n}]")
-    _here(n_new)
+    _here((pages, seqs), n_new, kv_have, held, o["granted"], o.get("row_seq"), o.get("positions"), o.get("slots"))
     r = Reservation(n_new.data_ptr(), kv_have.data_ptr(), held.data_ptr(), seqs.table, seqs.new_start, seqs.kv_len, o["granted"].data_ptr())
     if rows_out:
         r.row_seq, r.positions, r.slots = o["row_seq"].data_ptr(), o["positions"].data_ptr(), o["slots"].data_ptr()
@@ -850,7 +869,7 @@ def adjust_logits(params: Params, logits, text=None, length=None, text_from=None
         else:
             _refuse(f"allowed: contiguous int32 [B][{words}] or one mask a row")
         a.allowed = allowed.data_ptr()
-    _here(logits)
+    _here((), logits, out, text, length, text_from, draft_tokens, repetition, presence, frequency, bias_tokens, bias, allowed)
     _check(_lib.psd_adjust_logits(ctypes.byref(params), ctypes.byref(a), B, S, depth0, _ptr(logits), _ptr(out), _stream(stream)))
     return out
 
