@@ -865,7 +865,7 @@ def adjust_logits(params: Params, logits, text=None, length=None, text_from=None
         if allowed.dim() == 2:
             a.allowed_seq = words
         elif allowed.shape[:-1] == shape[:-1]:
-            a.allowed_seq, a.allowed_row = allowed.numel() // B, words
+            a.allowed_seq, a.allowed_row = K * S * words, words
         else:
             _refuse(f"allowed: contiguous int32 [B][{words}] or one mask a row")
         a.allowed = allowed.data_ptr()

@@ -111,3 +111,10 @@ def test_structures_without_their_make_function(psd, calls):
     cache = psd.Cache4(256, 256, 256, 256, psd.PSD_BF16, 2, 64, 16, 4, 1, 0, 1024, 64, 32, 0, 64, 4, 2)
     psd.kv_keep(cache, psd.Seqs(2, 4, 2, 64, 5, 5, 256, 256, 256), keep, n_keep, kv_out)
     assert calls.seen == ["psd_kv_keep4"]
+
+
+def test_no_sequences_with_masks(psd):
+    """A batch of nothing is refused as any other bad batch, whatever its masks."""
+    with pytest.raises(psd.PsdError) as e:
+        psd.adjust_logits(psd.make_params(0, 100, 2, 0, dtype=torch.float32), torch.zeros((0, 2, 4, 100)), allowed=ints(0, 2, 4, 4))
+    assert e.value.status == psd.PSD_E_ARG
