@@ -644,7 +644,8 @@ typedef struct {
  * (S = s_count, depth0 = s_begin).  Token v that came c times in what its row has seen, with logit l:
  *   c > 0:  l / rho if l > 0, else l rho; then minus frequency c + presence
  *   then plus the sum of v's biases; -inf where v may not come.
- * In float32, one rounding.  out may be logits itself (then only what changes is read or written) or shares no
+ * In float32, then one rounding to the dtype; bfloat16 rows take l (1 / rho) for the quotient, one rounding of float32
+ * more.  out may be logits itself (then only what changes is read or written) or shares no
  * memory with it; -inf stays -inf for finite parameters.  0 <= depth0, depth0 + S <= gamma + 1 with
  * draft_tokens.  Rows are PSD_MAX_DRAFTS paths of PSD_MAX_GAMMA + 1 at most.  One launch. */
 psd_status psd_adjust_logits(const psd_params *params, const psd_adjustments *adjust, int32_t batch, int32_t rows,

@@ -183,11 +183,14 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
     const int32_t* drafts = a.drafts ? a.drafts + (int64_t)b * a.K * a.gamma : nullptr;
     const float rho = a.repetition ? a.repetition[b] : 1.f;
     const float presence = a.presence ? a.presence[b] : 0.f, frequency = a.frequency ? a.frequency[b] : 0.f;
-    const float inverse = 1.f / rho;  // (a product where a quotient is meant: one rounding more)
+    // bfloat16: a product with 1 / rho where a quotient is meant, 2^-24 more of what is rounded to 2^-8 (148 us instead of 154,
+    // in place 108 and 120).  A float32 quotient is the definition's, and costs nothing there (293 us).
+    const float inverse = 1.f / rho;
     // Without a branch for the tokens that came: a wave's pieces mostly have one.
     auto penalized = [&](float l, uint32_t word) {
         const uint32_t c = word & kCount;
-        const float z = l * (l > 0.f ? inverse : rho) - (frequency * (float)c + presence);
+        const float scaled = BF16 ? l * (l > 0.f ? inverse : rho) : l > 0.f ? l / rho : l * rho;
+        const float z = scaled - (frequency * (float)c + presence);
         return c > 0 ? z : l;
     };
     auto biased = [&](float z, uint32_t word) {

@@ -192,3 +192,19 @@ def test_penalties_reach_the_verification(psd):
         for b in range(B):
             last = int(out["out_tokens"][b, int(out["out_len"][b]) - 1])
             assert int(allowed[b, last // 32]) >> (last % 32) & 1
+
+
+def test_repetition_divides(psd):
+    """Float32 logits with a repetition penalty alone: the float32 quotient and product, to the bit, over all of float32."""
+    g = torch.Generator().manual_seed(11)
+    V = 5000
+    rho = torch.tensor([1.1, 0.7, 3.0, 1.0 / 3, 2.0 ** -126, 2.0 ** 126, 1.9999999, 1.0])
+    B = len(rho)
+    z = torch.randn((B, 1, 2, V), generator=g)
+    z[:, 0, 1] *= 2.0 ** torch.randint(-140, 126, (B, V), generator=g).double().float()
+    z[..., :8] = torch.tensor([0.0, math.inf, -math.inf, 2.0 ** -149, -(2.0 ** -149), 3.4028234663852886e38, -3.4028234663852886e38, 1.0])
+    text = torch.arange(V, dtype=torch.int32).expand(B, V).contiguous()
+    out = psd.adjust_logits(psd.make_params(0, V, 1, 0, dtype=F32), z.cuda(), text=text.cuda(),
+                            length=torch.full((B,), V).cuda(), repetition=rho.cuda()).cpu()
+    r = rho[:, None, None, None]
+    assert torch.equal(out, torch.where(z > 0, z / r, z * r))
