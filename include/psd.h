@@ -645,9 +645,9 @@ typedef struct {
  *   c > 0:  l / rho if l > 0, else l rho; then minus frequency c + presence
  *   then plus the sum of v's biases; -inf where v may not come.
  * In float32, then one rounding to the dtype; bfloat16 rows take l (1 / rho) for the quotient, one rounding of float32
- * more.  out may be logits itself (then only what changes is read or written) or shares no
- * memory with it; -inf stays -inf for finite parameters.  0 <= depth0, depth0 + S <= gamma + 1 with
- * draft_tokens.  Rows are PSD_MAX_DRAFTS paths of PSD_MAX_GAMMA + 1 at most.  One launch. */
+ * more.  out may be logits itself (then only what changes is written, and without `allowed` only that is read) or shares
+ * no memory with it; -inf stays -inf for finite parameters.  0 <= depth0, depth0 + S <= gamma + 1 with draft_tokens.
+ * Rows are PSD_MAX_DRAFTS paths of PSD_MAX_GAMMA + 1 at most.  One launch. */
 psd_status psd_adjust_logits(const psd_params *params, const psd_adjustments *adjust, int32_t batch, int32_t rows,
                              int32_t depth0, const void *logits, void *out, hipStream_t stream);
 

@@ -66,7 +66,8 @@ struct Piece<false> {
 };
 
 // One workgroup: a stretch of SEG tokens of rows [r0, r1) of a sequence.  A row's next pieces are on their way while
-// this one's are computed; pieces that nothing touches pass through as they are (in place: are not read).
+// this one's are computed.  Pieces that nothing touches pass through as they are; in place they are not written, and without
+// a mask not read.
 template <bool BF16, int SEG>
 __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segments, int per) {
     using E = Elem<BF16>;
@@ -241,7 +242,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
             const bool touched = any != 0 || may[n] != kEvery;
             if (same && !touched) continue;
             if (v + VEC <= a.V) {
-                if (same && !here[n] && may[n] != 0) now[n] = *(const typename Pc::any*)(src + v);
+                if (same && !here[n]) now[n] = *(const typename Pc::any*)(src + v);
                 u32x4 y = now[n];
                 if (any != 0) {
                     float x[VEC];
