@@ -9,6 +9,7 @@
 // rows of 151936 293; 5 rows of 1024 5.
 #include <hip/hip_runtime.h>
 
+#include "psd_adjust_plan.hpp"
 #include "psd_serve.hpp"
 #include "psd_serve_device.hpp"
 
@@ -19,9 +20,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kMaxBias = 1024;
-// A workgroup's stretch where there are many: 16 KB of bfloat16 or float32, four pieces a thread.
-constexpr int stretch(bool bf16) { return bf16 ? 8192 : 4096; }
-constexpr int short_stretch(bool bf16) { return stretch(bf16) / 4; }
 // A token's word: bit 31 where it has biases, their place in the list, and its count below.
 constexpr uint32_t kBiased = 1u << 31, kCount = (1u << 20) - 1;
 constexpr float kGone = -__builtin_inff();
@@ -266,44 +264,25 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int segm
     }
 }
 
-// Workgroups: a long stretch and all rows of a sequence each, so that its text is counted once a stretch; fewer
-// rows, then a short stretch, while there are too few to fill the device.
-struct Cut {
-    int seg, segments, per;
-};
-constexpr long kFill = 768;
-inline Cut cut(const AdjustArgs& a, bool bf16) {
-    Cut c;
-    c.seg = stretch(bf16);
-    c.segments = (a.V + c.seg - 1) / c.seg;
-    const int R = a.K * a.S;
-    c.per = R;
-    while (c.per > 1 && (long)c.segments * a.B * ((R + c.per - 1) / c.per) < kFill) c.per = (c.per + 1) / 2;
-    if (c.per == 1 && (long)c.segments * a.B * R < kFill) {
-        c.seg = short_stretch(bf16);
-        c.segments = (a.V + c.seg - 1) / c.seg;
-    }
-    return c;
-}
-
 template <bool BF16>
-void launch(const AdjustArgs& a, const Cut& c, hipStream_t stream) {
-    const dim3 grid((unsigned)((long)c.segments * a.B * ((a.K * a.S + c.per - 1) / c.per)));
-    if (c.seg == short_stretch(BF16))
-        hipLaunchKernelGGL((adjust_kernel<BF16, short_stretch(BF16)>), grid, dim3(kThreads), 0, stream, a, c.segments, c.per);
+void launch(const AdjustArgs& a, const AdjustCut& c, hipStream_t stream) {
+    const dim3 grid((unsigned)c.wgs(a.B, a.K * a.S));
+    constexpr int kLong = adjust_stretch(BF16), kShort = adjust_short_stretch(BF16);
+    if (c.seg == kShort)
+        hipLaunchKernelGGL((adjust_kernel<BF16, kShort>), grid, dim3(kThreads), 0, stream, a, c.segments, c.per);
     else
-        hipLaunchKernelGGL((adjust_kernel<BF16, stretch(BF16)>), grid, dim3(kThreads), 0, stream, a, c.segments, c.per);
+        hipLaunchKernelGGL((adjust_kernel<BF16, kLong>), grid, dim3(kThreads), 0, stream, a, c.segments, c.per);
 }
 
 }  // namespace
 
 bool adjust_fits(const AdjustArgs& a, bool bf16) {
-    const Cut c = cut(a, bf16);
-    return (long)c.segments * a.B * ((a.K * a.S + c.per - 1) / c.per) < 1L << 23;
+    const int R = a.K * a.S;
+    return adjust_cut(a.B, R, a.V, bf16).wgs(a.B, R) < 1L << 23;
 }
 
 hipError_t launch_adjust(const AdjustArgs& a, bool bf16, hipStream_t stream) {
-    const Cut c = cut(a, bf16);
+    const AdjustCut c = adjust_cut(a.B, a.K * a.S, a.V, bf16);
     if (bf16)
         launch<true>(a, c, stream);
     else
