@@ -144,3 +144,57 @@ def test_captured_and_replayed_on_another_stream(psd):
         both.check(out, n, h)
         h = [rng.randint(0, x) for x in both.kv.tolist()]
     assert none.tolist() == [0] * B
+
+
+@pytest.mark.parametrize("captured", [False, True], ids=["eager", "graph"])
+def test_reserve_and_trim_back_to_back_on_another_stream(psd, captured):
+    """A reservation and the trim of what does not stay, on one ring and table with nothing of the host in between, several
+    workgroups each; as a graph replayed on a stream of its own.  Both calls are the plain form's every time."""
+    B, P, width, rows = 200, 16, 20, 20000
+    order = list(range(1500))
+    random.Random(8).shuffle(order)
+    plain = ref4.Pool(1500, P, B, width, order, 700)
+    pages = psd.make_pages(ints(plain.ring), ints([700, 1500, 0, 0]), P)
+    table, held = torch.full((B, width), -1, dtype=torch.int32, device="cuda"), ints([0] * B)
+    (start, kv), (start2, kv2) = ((ints([7] * (B + 1)), ints([7] * B)) for _ in range(2))
+    seqs, after = psd.make_seqs(start, kv, table, rows, 130, 320), psd.make_seqs(start2, kv2, table, rows, 130, 320)
+    n_new, have, stay, kept, none = (ints([0] * B) for _ in range(5))
+    out, trimmed = {}, {}
+
+    def step():
+        out.update(psd.kv_reserve(pages, seqs, n_new, have, held, out=out))
+        torch.minimum(kv, stay, out=kept)
+        trimmed.update(psd.kv_reserve(pages, after, none, kept, held, out=trimmed))
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()  # (nothing asked)
+    torch.cuda.synchronize()
+    plain.reserve([0] * B, [0] * B, rows, 130, 320)
+    graph = torch.cuda.CUDAGraph()
+    if captured:
+        with torch.cuda.graph(graph):
+            step()
+    rng = random.Random(5)
+    h = [0] * B
+    for i in range(8):
+        n = [rng.randint(0, 130) for _ in range(B)]
+        st = [rng.choice([0, x + rng.randint(0, 130), 400]) for x in h]
+        for t, x in ((n_new, n), (have, h), (stay, st)):
+            t.copy_(ints(x))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            graph.replay() if captured else step()
+        torch.cuda.synchronize()
+        granted, first, lens, seq, pos, slot = plain.reserve(n, h, rows, 130, 320)
+        assert out["granted"].tolist() == granted and start.tolist() == first and kv.tolist() == lens
+        assert out["row_seq"].tolist() == seq and out["positions"].tolist() == pos and out["slots"].tolist() == slot
+        h = [min(a, b) for a, b in zip(lens, st)]
+        assert kept.tolist() == h
+        granted, first, lens, seq, pos, slot = plain.reserve([0] * B, h, rows, 130, 320)
+        assert trimmed["granted"].tolist() == granted == [0] * B and start2.tolist() == first and kv2.tolist() == lens == h
+        assert held.tolist() == plain.held and table.tolist() == plain.table
+        ring, state = (t.tolist() for t in pages.tensors)
+        assert state == [plain.first, len(plain.free), 0, 0]
+        assert [ring[(state[0] + j) % 1500] for j in range(state[1])] == plain.free

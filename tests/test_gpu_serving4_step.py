@@ -142,3 +142,87 @@ def test_example_over_4_bits(block):
     assert not all(len(set(row)) == 60 for row in a.tolist())
     d, _ = block.keyed(target, good, prompts, 40)
     assert bool(((d >= 0) & (d < 500)).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_captured_steps(block, dtype):
+    """The whole step in one graph, replayed with other requests, rows and random numbers: state and outputs are those of
+    the same calls made one by one (which test_serving_steps compares with their plain forms)."""
+    psd = block.psd
+    B, H, G, D, P, V, gamma, width, pages = 5, 4, 2, 80, 8, 900, 3, 12, 36
+    max_new, rows = 20, B * 20
+    params = psd.make_params(0, V, 1, 0, 0.9, 1.1, dtype=dtype)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    ints = lambda *n: torch.zeros(n, dtype=torch.int32, device="cuda")  # noqa: E731
+    normal = lambda *n: torch.randn(n, generator=g, device="cuda").to(dtype)  # noqa: E731
+
+    class Server:
+        def __init__(self):
+            self.cache, self.pages = psd.new_cache4(pages, P, G, D, dtype=dtype), psd.new_pages(pages, P)
+            self.table, self.held = torch.full((B, width), -1, dtype=torch.int32, device="cuda"), ints(B)
+            self.seqs = psd.make_seqs(ints(B + 1), ints(B), self.table, rows, max_new, width * P)
+            self.ws, self.vws = psd.new_attention_workspace(self.cache, self.seqs, H), psd.new_verify_given_workspace(params, B, gamma)
+            self.n_new, self.have, self.kept = ints(B), ints(B), ints(B)
+            self.q, self.k, self.v = (torch.zeros((rows, n, D), dtype=dtype, device="cuda") for n in (H, G, G))
+            self.weights = torch.zeros((gamma + 1, V), dtype=torch.float32, device="cuda")
+            self.text, self.length = ints(B, 100), torch.zeros(B, dtype=torch.int64, device="cuda")
+            self.drafts, self.draft_rows = ints(B, gamma), torch.zeros((B, gamma, V), dtype=dtype, device="cuda")
+            self.u, self.e = torch.zeros((B, gamma), device="cuda"), torch.ones((B, V), device="cuda")
+            self.presence = torch.ones(B, device="cuda")
+            self.last = torch.arange(gamma + 1, device="cuda")
+            self.index = torch.arange(max_new, dtype=torch.int32, device="cuda").expand(B, -1).contiguous()
+            self.places, self.out, self.attended, self.z = {}, {}, {}, None
+
+        def step(self):
+            self.places.update(psd.kv_reserve(self.pages, self.seqs, self.n_new, self.have, self.held, out=self.places))
+            psd.kv_append(self.cache, self.seqs, self.k, self.v)
+            self.attended.update(psd.attention(self.cache, self.seqs, self.q, self.ws, out=self.attended.get("out"), want_lse=True,
+                                               lse=self.attended.get("lse")))
+            start = self.seqs.tensors[0]
+            at = (start[1:, None] - gamma - 1 + self.last).clamp(min=0)
+            logits = (self.attended["out"].float()[at][:, :, 0, :1] * self.weights).to(dtype)  # (no library product in a graph)
+            self.z = psd.adjust_logits(params, logits, text=self.text, length=self.length, draft_tokens=self.drafts[:, None],
+                                       presence=self.presence, out=logits)
+            self.out.update(psd.verify_given(params, self.vws, self.z, self.draft_rows, self.drafts, self.u, self.e, out=self.out))
+            n = torch.minimum(self.out["out_len"], self.places["granted"])
+            psd.kv_keep(self.cache, self.seqs, self.index, n, kv_out=self.kept)
+
+        def fill(self, of):
+            for name, t in of.items():
+                getattr(self, name).copy_(t)
+
+        def all(self):
+            return [*self.cache.tensors, *self.pages.tensors, self.table, self.held, *self.seqs.tensors, self.kept, self.z,
+                    *self.attended.values(), *self.places.values(), *self.out.values()]
+
+    eager, captured = Server(), Server()
+    for s in (eager, captured):
+        s.step()  # (nothing asked)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured.step()
+    have = torch.zeros(B, dtype=torch.int32, device="cuda")
+    moved = 0
+    for i in range(8):
+        n_new = torch.where(have > 0, gamma + 1, torch.randint(gamma + 1, max_new + 1, (B,), generator=g, device="cuda")).to(torch.int32)
+        of = dict(n_new=n_new, have=have, q=normal(rows, H, D), k=normal(rows, G, D), v=normal(rows, G, D),
+                  weights=normal(gamma + 1, V).float(), text=torch.randint(0, V, (B, 100), generator=g, device="cuda"),
+                  length=torch.randint(0, 101, (B,), generator=g, device="cuda"),
+                  drafts=torch.randint(0, V, (B, gamma), generator=g, device="cuda"), draft_rows=normal(B, gamma, V),
+                  u=torch.rand((B, gamma), generator=g, device="cuda"),
+                  e=torch.empty((B, V), device="cuda").exponential_(generator=g).clamp_(min=1e-30))
+        for s in (eager, captured):
+            s.fill(of)
+        eager.step()
+        graph.replay()
+        torch.cuda.synchronize()
+        T = int(eager.seqs.tensors[0][-1])
+        for a, b in zip(eager.all(), captured.all()):
+            assert a.dtype == b.dtype
+            if a.shape[:1] == (rows,) and a.dtype in (dtype, torch.float32):  # attention's rows behind the last are left as they were
+                a, b = a[:T], b[:T]
+            assert torch.equal(a, b), i
+        moved += int(eager.kept.sum())
+        have = torch.where(torch.rand(B, generator=g, device="cuda") < 0.15, 0, eager.kept).to(torch.int32)
+    assert moved > 0
