@@ -434,3 +434,38 @@ def test_keep(psd, D, G, P, layers, heads_first):
     for p, w in zip(pools, want):
         assert torch.equal(p.cpu(), w)
     assert kv.tolist() == [s.first(b) + len(r) for b, r in enumerate(rows)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("D,R,interleaved", [(64, 64, False), (64, 64, True), (96, 24, False), (256, 256, False)])
+def test_append_next_to_borders(psd, D, R, interleaved, dtype):
+    """Turned keys that are no floats and whose nearest float is a border between two codes, or two scales: the code is that of
+    the key itself, which a sum of a border and a far smaller product has exactly in 64 bits."""
+    half, n_pos = R // 2, 6
+    borders = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0])
+    cos = torch.ones((n_pos, half))
+    sin = torch.tensor([2.0 ** -28, -(2.0 ** -28), 2.0 ** -40, -(2.0 ** -40), 2.0 ** -28, -(2.0 ** -28)])[:, None].expand(-1, half).contiguous()
+    k = torch.zeros((n_pos, 2, D))
+    r = torch.arange(half)
+    a, b = (2 * r, 2 * r + 1) if interleaved else (r, r + half)
+    for t in range(n_pos):
+        for h in range(2):
+            k[t, h, a] = borders[(r + t) % 7] * torch.where(r % 2 > 0, -1.0, 1.0)
+            k[t, h, b] = torch.where(r % 3 > 0, 1.0, -1.0)
+            k[t, h, a[::8]] = 6.0 if t < 4 else 7.0  # the group's scale, and next to the border of two
+    k[:, 1, R:] = 2.5  # (not turned: a tie)
+    k[4:, 1] *= 2.0 ** 120
+    k = k.to(dtype)
+    exact = torch.stack([ref.norm_rotate(k[t].double(), None, 0.0, cos[t].double(), sin[t].double(), interleaved)[0] for t in range(n_pos)])
+    codes, scales = ref4.encode(exact)
+    rounded = ref4.encode(exact.float().double())
+    assert all(bool((rounded[0][t] != codes[t]).any()) for t in range(n_pos)), "these keys tell nothing"
+    assert bool((rounded[1] != scales).any())
+    s = ref4.Sequences4([(n_pos, n_pos)], 2, D, 16, dtype)
+    cache, seqs, pools = s.handles(psd)
+    held = torch.empty((n_pos, 2, D), dtype=dtype, device="cuda")
+    psd.kv_append(cache, seqs, k.cuda(), k.cuda(), cos=cos.cuda(), sin=sin.cuda(), interleaved=interleaved, k_held=held)
+    torch.cuda.synchronize()
+    page = int(s.table[0, 0])
+    assert torch.equal(pools[0][page, :n_pos].cpu(), codes) and torch.equal(pools[2][page, :n_pos].cpu(), scales)
+    assert torch.equal(held.cpu().double(), ref4.decode(codes, scales, D))
