@@ -510,7 +510,7 @@ psd_status psd_kv_keep(const psd_cache *cache, const psd_seqs *seqs, const int32
  *   dimension d is the nibble d % 2 (0: the low one) of byte d / 2 of its head's codes,
  *   code c stands for the (c & 7)th of 0, 0.5, 1, 1.5, 2, 3, 4, 6, negative with c & 8,
  *   times 2^(s - 127) for scale byte s; s = 255 makes the whole group NaN (253 and 254, whose
- *   larger codes pass float32's range, are never written and count as no finite number).
+ *   larger codes pass float32's range, are never written, and what they stand for is not defined).
  * A quarter and a bit of bfloat16's bytes; every value is exact in bfloat16, and gfx950
  * converts two codes in one instruction.  With groups = ceil(D / 32), the codes of (layer l,
  * page p, place i, head g) are the 16 groups bytes at l * stride_layer + p * stride_page +

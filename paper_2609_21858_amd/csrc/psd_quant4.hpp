@@ -14,7 +14,7 @@ namespace psd {
 namespace quant4 {
 
 constexpr int kNan = 255;   // scale byte
-constexpr int kMost = 252;  // the largest that is written: 6 2^125; a group above has no finite number
+constexpr int kMost = 252;  // the largest that is written, 6 2^125; the two above it stand for nothing that is defined
 
 // The scale byte that elements z alone would have: k + 127 with the least k in [-126, 125] such that all are at most
 // 7 2^k (1.75 2^(k+2): the exponent, and one more where the mantissa passes 0.75).  It grows with the largest

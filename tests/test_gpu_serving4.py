@@ -469,3 +469,52 @@ def test_append_next_to_borders(psd, D, R, interleaved, dtype):
     page = int(s.table[0, 0])
     assert torch.equal(pools[0][page, :n_pos].cpu(), codes) and torch.equal(pools[2][page, :n_pos].cpu(), scales)
     assert torch.equal(held.cpu().double(), ref4.decode(codes, scales, D))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("rows,kv", [(1, 1), (1, 64), (5, 5), (40, 40), (130, 64)])
+def test_attention_reads_every_scale_byte(psd, rows, kv, D, dtype):
+    """Every scale byte that is defined and all 16 codes, a scale to a sequence: rows that weigh all tokens alike have the first's
+    values over their number, and where a row sees one token alone, one product is its lse; 255 is NaN, whatever the code.  In
+    blocks that rows see whole and in others."""
+    n, P, B = D // 32, 64, 256
+    table = torch.randperm(B, generator=torch.Generator().manual_seed(D + kv)).to(torch.int32).view(B, 1)
+    at = table[:, 0].long()
+    start = torch.arange(B + 1, dtype=torch.int32) * rows
+    seqs = psd.make_seqs(start.cuda(), torch.full((B,), kv, dtype=torch.int32).cuda(), table.cuda(), B * rows, rows, kv)
+    every = torch.arange(256, dtype=torch.uint8)[:, None].expand(-1, n)
+
+    def first(codes, scales):
+        """Pools whose first tokens hold these codes and scales, the others zeros."""
+        c, s = torch.zeros((B, P, 1, 16 * n), dtype=torch.uint8), torch.full((B, P, 1, n), 127, dtype=torch.uint8)
+        c[at, 0, 0], s[at, 0, 0] = codes, scales
+        return c.cuda(), s.cuda()
+
+    def attend(keys, values, q):
+        cache = psd.make_cache4(keys[0], values[0], keys[1], values[1], D, dtype=dtype)
+        o = psd.attention(cache, seqs, q.to(dtype).cuda(), psd.new_attention_workspace(cache, seqs, 1), scale=1.0, want_lse=True)
+        return o["out"].cpu().double().view(B, rows, D), o["lse"].cpu().double().view(B, rows)
+
+    zeros = first(torch.zeros(16 * n, dtype=torch.uint8), torch.full((n,), 127, dtype=torch.uint8))
+    q = torch.zeros((B * rows, 1, D))
+    code = (torch.arange(D) % 16).to(torch.uint8)
+    out, _ = attend(zeros, first(code[0::2] + 16 * code[1::2], every), q)
+    value = torch.tensor(ref4.LEVELS + [-x for x in ref4.LEVELS], dtype=torch.float64)[code.long()] * 2.0 ** (torch.arange(256).double() - 127)[:, None]
+    # one rounding, of which 2^-133 (bfloat16) or 2^-149 may be the least step, and the quotient's
+    step = 2.0 ** -133 if dtype == BF16 else 2.0 ** -149
+    for i in range(rows):
+        seen = kv - rows + i + 1
+        if seen > 0:
+            want = value[:253] / seen
+            off = (out[:253, i] - want).abs()
+            assert bool((off <= (HALF[dtype] + 4 * ULP) * want.abs() + step).all()), (i, (off / want.abs().clamp(min=step)).max())
+            assert not bool(torch.isfinite(out[255, i]).any()), (i, out[255, i, :16].tolist())
+    if kv == rows:
+        q[:, 0, D // 2 + 1] = 1
+        for c in range(16):
+            _, lse = attend(first(torch.full((16 * n,), 17 * c, dtype=torch.uint8), every), zeros, q)
+            want = (ref4.LEVELS[c & 7] * (-1 if c & 8 else 1)) * 2.0 ** (torch.arange(253).double() - 127)
+            off, fine = (lse[:253, 0] - want).abs(), want.abs() * 1.45 < 2.0 ** 128  # (in units of ln 2)
+            assert bool((off <= 4 * ULP * want.abs() + 2.0 ** -148)[fine].all()), (c, float((off / want.abs())[fine].max()))
+            assert bool(torch.isnan(lse[255, 0])), (c, float(lse[255, 0]))
