@@ -624,7 +624,8 @@ typedef struct {
     int64_t text_stride;        /* >= text_max */
     int32_t text_max;           /* 0..PSD_MAX_TEXT: upper bound of length (longer ones are cut) */
     const int64_t *length;      /* device [B] (with text): text[b][from[b] .. length[b]) counts */
-    const int64_t *from;        /* device [B]: first token that counts; NULL: 0 */
+    const int64_t *from;        /* device [B]: first token that counts, for all three penalties (repetition over a prompt too and
+                                    the others over the output alone: two calls); NULL: 0 */
     const int32_t *draft_tokens; /* device [B][K][gamma]: the row of depth s on path k has also seen the path's
                                     tokens before depth s */
     int32_t gamma;              /* entries of a path in draft_tokens */

@@ -6,7 +6,8 @@
 // bounds it: every logit is read and written once; the texts are counted by each workgroup for its own
 // stretch of the vocabulary.  1280 rows of 128256 bfloat16 logits of 64 sequences, texts of 2048 tokens, 657 MB: 146 us,
 // 4.5 TB/s (a device copy 4.9), with a mask a row 152; in place, where most pieces only pass, 108, with masks 160; 1152 float32
-// rows of 151936 293; 5 rows of 1024 5.
+// rows of 151936 293; 5 rows of 1024 5.  Every workgroup of a sequence counts its whole text: with texts of up to 16384, 131072 and
+// 1000000 tokens 148, 176 and 430 us, 5 rows of 1 sequence 7, 22 and 200 (none: 143 and 4.7).
 #include <hip/hip_runtime.h>
 
 #include "psd_adjust_plan.hpp"

@@ -39,14 +39,16 @@ __device__ __forceinline__ uint32_t upper(float lo, float hi) {
 // DP / 4 q on (DP = 256: 32 dimensions from 32 q and from 128 + 32 q on), one scale byte to each 32 dimensions, and the
 // queries are laid out to match.  Values become bfloat16 on their way into the wave's LDS, 32 tokens at a time.
 //
-// Memory bounds long caches, (D/2 + D/32) 2 G bytes a token, and chains of dependent loads short ones (start, division,
-// places, keys, join of waves, join of parts: about 18 us in all).  H=32, G=8, D=128: 1 token of 32 sequences, up to
-// 16384 cached, 363 MB, 80 us, 4.5 TB/s (5.85 for each token more), float32 rows 86 - 96; heads of 64 52, 4 heads of 256
-// 85 - 92.  1 token of 64 sequences, up to 4096, 52 us, 5 tokens 63 - 70, float32 96 - 103; 1 token of 4 sequences, up
-// to 512, 8.4; behind 131072 46.  float32 rows are bound by products, three for one: 4 x 512 tokens to 2048 264 us,
-// 433 TFLOP/s of bfloat16 products.
-// Four waves a workgroup and two workgroups a CU, so that one's chains lie under the other's loads; 201 - 256 registers
-// a lane (heads of 256: one, with 356 - 416).
+// Memory bounds long caches, (D/2 + D/32) 2 G bytes a token, and a chain of dependent loads short ones (start, division,
+// places, keys, join of waves).  H=32, G=8, D=128: 1 token of 32 sequences, up to 16384 cached, 363 MB, 80 us, 4.5 TB/s,
+// float32 rows 86 - 96; heads of 64 52, 4 heads of 256 83 - 92.  1 token of 64 sequences, up to 4096, 52 us, 5 tokens
+// 62 - 70, float32 96 - 103; 1 token of 4 sequences, up to 512, 8.4 (the chain); behind 131072 46.  Of the 80 us, each
+// token more goes by at 5.85 TB/s, the chain takes 8, and 10 are not accounted for: half of the vector loads move one byte a
+// lane (scales), a third of the active LDS cycles wait for banks, products are busy 13 %.  float32 rows are bound by products,
+// three for one: 4 x 512 tokens to 2048 264 us, 433 TFLOP/s of bfloat16 products.
+// Four waves a workgroup and two workgroups a CU, so that one's chain lies under the other's loads; 143 - 256 registers a
+// lane (heads of 256: one workgroup, with 356 - 512).  Tiles of 32 bfloat16 rows spill 10 of them, 50 with heads of 256;
+// 64 - 117 scalar ones are spilled into lanes of vector registers in every form.
 template <int DP>
 struct Stream4Shape {
     static constexpr int TOK = 64;
@@ -350,6 +352,8 @@ __global__ __launch_bounds__(64 * kWaves4, stream4_resident(DP, RB)) void stream
                     for (int e = 0; e < 4; ++e) {
                         const float w0 = sv[rb][2 * h + e / 2][2 * (e % 2)], w1 = sv[rb][2 * h + e / 2][2 * (e % 2) + 1];
                         if constexpr (BF16) {
+                            // Weights are rounded as psd_attention's, 2^-8 of each at most: a second term would be a second
+                            // product.  Outputs 2.1e-3 to 2.3e-3 of their size from 64 bits (the result's own rounding: 1.7e-3).
                             w[rb][h][0][e] = pack_bf16(w0, w1);
                         } else {
                             float u[TERMS], v[TERMS];

@@ -77,8 +77,10 @@ constexpr int kUnit = 128;  // cached tokens: a block of each wave (two in float
 // joins pay from one on (37 tokens of 12 heads 38 us, with 4 units 49).
 constexpr int join_units(bool bf16) { return bf16 ? 4 : 1; }
 
-// The same over a cache held in 4 bits: a block of each wave (27 float32 rows of 6 sequences of up to 1500 tokens 16 us; 1 unit 19, 4
-// units 18), two in bfloat16 (8 sequences of up to 2000 tokens 15.1 us; 2 units 16.3).
+// The same over a cache held in 4 bits: a block of each wave in float32, two in bfloat16 (8 sequences of up to 2000 tokens 15.1 us;
+// 2 units 16.3).  Float32, 1, 2 and 4 units: 27 rows of 6 sequences of up to 1500 tokens 19, 16 and 18 us, 1 row of 4 sequences to 2000
+// 18, 15 and 16, 27 rows of 12 to 800 16, 16 and 17; 32 rows of 6 to 1500 20, 20 and 18; over 26 calls of 1 to 512 tokens of 1 to 64
+// sequences, heads of 64 to 256, 1 unit takes 2.5 % more and 4 units 0.9 %.
 constexpr int join_units4(bool bf16) { return bf16 ? 4 : 2; }
 // A stretch's least units there: no more than the longest item has, since items that end with it leave nothing to join (48 and
 // 96 sequences of 5 tokens, 16 heads of 64: 11 and 15 us, with stretches of 4 units 17 and 19).
